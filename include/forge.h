@@ -272,6 +272,84 @@ forge_status forge_rope_apply(forge_bf16* qkv, int64_t ld, const float* rope_cos
                               forge_stream stream);
 
 /*
+ * LayerNorm forward, for models whose norms centre their rows: per row t,
+ * mean[t] = mean_j x[t,j], rstd[t] = 1 / sqrt(mean_j (x[t,j] - mean[t])^2 +
+ * eps) in fp32, y[t,j] = bf16((x[t,j] - mean[t]) * rstd[t] * g[j] + b[j]).
+ * x, y [T, h] bf16 (y must not overlap x), g [h] bf16, b [h] bf16 or NULL (no
+ * bias), mean, rstd [T] fp32. 8 <= h <= 8192, h % 8 == 0.
+ */
+forge_status forge_layernorm_fwd(const forge_bf16* x, const forge_bf16* g, const forge_bf16* b,
+                                 forge_bf16* y, float* mean, float* rstd, int32_t tokens,
+                                 int32_t hidden, float eps, forge_stream stream);
+
+/* Scratch bytes of forge_layernorm_bwd (per-block gain and bias gradient
+ * partials). Host only. */
+forge_status forge_layernorm_bwd_workspace_bytes(int32_t tokens, int32_t hidden, size_t* bytes);
+
+/*
+ * LayerNorm backward: with y as above, mean and rstd the forward's and dy
+ * [T, h] bf16, dx = d<y, dy>/dx (+ resid when resid is non-NULL: a residual
+ * stream's gradient passing the norm), written as bf16 [T, h]; the gain
+ * gradient sum_t dy (x - mean) rstd and the bias gradient sum_t dy are added
+ * to dg and db [h] fp32 (accumulate != 0) or stored (accumulate == 0), summed
+ * over fixed row blocks in a fixed order. db may be NULL (no bias). dx must
+ * not overlap x, dy or resid, nor dg db. tokens == 0: dg and db alone. Limits
+ * as the forward.
+ */
+forge_status forge_layernorm_bwd(const forge_bf16* x, const forge_bf16* g, const float* mean,
+                                 const float* rstd, const forge_bf16* dy,
+                                 const forge_bf16* resid, forge_bf16* dx, float* dg, float* db,
+                                 int32_t accumulate, int32_t tokens, int32_t hidden,
+                                 void* workspace, forge_stream stream);
+
+/*
+ * Rotary positions with several axes (time, height and width of the tokens of
+ * images and video): the head_dim / 2 rotate-half pairs (i, i + head_dim/2)
+ * are shared out to n_axes axes, pairs[a] of them to axis a, and a token has
+ * one position per axis.
+ *   interleaved == 0: the first pairs[0] pairs belong to axis 0, the next
+ *     pairs[1] to axis 1, ...
+ *   interleaved != 0: the pairs are dealt to the axes in turn, an axis that has
+ *     its share being passed over.
+ *   own_ladder == 0: pair i turns by base^(-2i/head_dim) per position, whatever
+ *     its axis (a text token, its position the same on every axis, is rotated
+ *     as forge_rope_apply rotates it).
+ *   own_ladder != 0: the l-th pair (from 0) of axis a turns by
+ *     base^(-l/pairs[a]): every axis has all frequencies.
+ * Rules (else INVALID_ARG): 1 <= n_axes <= 4; pairs[a] >= 1 for a < n_axes,
+ * their sum head_dim / 2; head_dim a multiple of 16, 16 <= head_dim <= 512.
+ */
+#define FORGE_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t head_dim, n_axes;
+  int32_t pairs[FORGE_ROPE_MAX_AXES];
+  int32_t interleaved, own_ladder;
+} forge_rope_axes_cfg;
+
+/*
+ * Tables [n_positions, head_dim/2] fp32 of cos and sin of position p's angle
+ * for pair i, computed in fp64. Fill once per configuration and base.
+ * n_positions * head_dim / 2 < 2^31.
+ */
+forge_status forge_rope_axes_table(const forge_rope_axes_cfg* cfg, int32_t n_positions, float base,
+                                   float* cos_out, float* sin_out, forge_stream stream);
+
+/*
+ * Rotates the first n_rot heads of each row of x [T, ldx] bf16 (head r at
+ * columns r*head_dim ..) into the same heads of y [T, ldy]; other columns of y
+ * are left as they are. y may be x (in place, ldy == ldx), else the two must
+ * not overlap. positions: device int32 [n_axes, T], axis a's position of every
+ * token, clamped to [0, n_positions). inverse != 0 rotates back (the backward:
+ * x the gradient). ldx, ldy % 8 == 0 and >= n_rot * head_dim; T * n_rot *
+ * head_dim / 16 < 2^31; positions 4-byte aligned.
+ */
+forge_status forge_rope_axes_apply(const forge_rope_axes_cfg* cfg, const forge_bf16* x,
+                                   int64_t ldx, forge_bf16* y, int64_t ldy, const float* rope_cos,
+                                   const float* rope_sin, const int32_t* positions,
+                                   int32_t tokens, int32_t n_positions, int32_t n_rot,
+                                   int32_t inverse, forge_stream stream);
+
+/*
  * SwiGLU (App. B): gu [T, 2f] bf16 holds the gate G (columns 0..f-1) and up
  * U (columns f..2f-1) of each row; a [T, f] bf16 = bf16(silu(G) * U) with
  * silu(z) = z / (1 + exp(-z)) in fp32. f % 8 == 0; a must not overlap gu.
@@ -639,6 +717,50 @@ forge_status forge_attention_bwd(const forge_attn_cfg* cfg, const forge_bf16* qk
                                  const forge_bf16* o, const float* lse,
                                  const forge_bf16* d_o, forge_bf16* d_qkv,
                                  void* workspace, forge_stream stream);
+
+/*
+ * Attention with a sliding window and sinks, for layers that look back a
+ * bounded number of tokens: key j is visible to query i of its batch row iff
+ *   j <= i  and  (i - j < window  or  j < sinks),
+ * the last `window` tokens, the query's own among them, and the row's first
+ * `sinks` tokens. Rules: those of forge_attn_cfg; window >= 1, sinks >= 0
+ * (values beyond seq are as seq; window >= seq is causal attention); seq <=
+ * 2^23, batch * n_heads * seq < 2^28, (n_heads + 2 n_kv_heads) * head_dim <=
+ * 2^22 (else UNSUPPORTED).
+ */
+typedef struct {
+  int32_t batch, seq, n_heads, n_kv_heads, head_dim;
+  int32_t window, sinks;
+} forge_attn_window_cfg;
+
+/*
+ * Forward: qkv, o and lse laid out as in forge_attention_fwd (o must not
+ * overlap qkv). seq_lens: device int32 [batch], the tokens of each batch row (a
+ * padded batch), clamped to [0, seq]; NULL: seq each. Padding rows of qkv are
+ * not read and visible to no query; their rows of o are written as zeros and
+ * their lse as -infinity. (Among the tokens of a row, a NaN or an infinity in
+ * v may reach rows that do not see it, as 0 * NaN.) One token is a valid row.
+ */
+forge_status forge_attention_window_fwd(const forge_attn_window_cfg* cfg, const forge_bf16* qkv,
+                                        const int32_t* seq_lens, forge_bf16* o, float* lse,
+                                        forge_stream stream);
+
+/* Scratch bytes of forge_attention_window_bwd: per-query statistics and the
+ * score gradient in bf16, of each head a band of about seq x (window + 64) and
+ * seq for each of ceil(sinks / 64) * 64 keys. Host only. */
+forge_status forge_attention_window_bwd_workspace_bytes(const forge_attn_window_cfg* cfg,
+                                                        size_t* bytes);
+
+/*
+ * Backward, as forge_attention_bwd over the visible pairs: from d_o [T, hq]
+ * bf16 and the forward's qkv, seq_lens, o, lse, writes d_qkv [T, hq+2hkv] bf16
+ * (=), which must not overlap qkv, o or d_o. Padding rows of d_o are not used,
+ * those of d_qkv are written as zeros. No atomics: bitwise deterministic.
+ */
+forge_status forge_attention_window_bwd(const forge_attn_window_cfg* cfg, const forge_bf16* qkv,
+                                        const int32_t* seq_lens, const forge_bf16* o,
+                                        const float* lse, const forge_bf16* d_o,
+                                        forge_bf16* d_qkv, void* workspace, forge_stream stream);
 
 /* Scratch bytes of forge_moe_route. Host only. */
 forge_status forge_moe_route_workspace_bytes(int32_t tokens, int32_t n_experts, int32_t top_k,

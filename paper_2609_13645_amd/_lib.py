@@ -91,6 +91,19 @@ class AttnCfg(ctypes.Structure):
                 ("batch", "seq", "n_heads", "n_kv_heads", "head_dim")]
 
 
+class AttnWindowCfg(ctypes.Structure):
+    _fields_ = AttnCfg._fields_ + [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
+ROPE_MAX_AXES = 4
+
+
+class RopeAxesCfg(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("pairs", ctypes.c_int32 * ROPE_MAX_AXES), ("interleaved", ctypes.c_int32),
+                ("own_ladder", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -131,6 +144,13 @@ def load():
         "forge_rmsnorm_bwd_workspace_bytes": (ctypes.c_int, [I32, I32, ctypes.POINTER(ctypes.c_size_t)]),
         "forge_rmsnorm_bwd": (ctypes.c_int, [P, P, P, P, P, P, P, I32, I32, I32, P, P]),
         "forge_rope_apply": (ctypes.c_int, [P, I64, P, P, P, I32, I32, I32, I32, I32, P]),
+        "forge_layernorm_fwd": (ctypes.c_int, [P, P, P, P, P, P, I32, I32, F32, P]),
+        "forge_layernorm_bwd_workspace_bytes": (ctypes.c_int, [I32, I32, SZ]),
+        "forge_layernorm_bwd": (ctypes.c_int, [P, P, P, P, P, P, P, P, P, I32, I32, I32, P, P]),
+        "forge_rope_axes_table": (ctypes.c_int, [ctypes.POINTER(RopeAxesCfg), I32, F32, P, P,
+                                                 P]),
+        "forge_rope_axes_apply": (ctypes.c_int, [ctypes.POINTER(RopeAxesCfg), P, I64, P, I64, P,
+                                                 P, P, I32, I32, I32, I32, P]),
         "forge_swiglu_fwd": (ctypes.c_int, [P, P, I32, I32, P]),
         "forge_swiglu_bwd": (ctypes.c_int, [P, P, P, I32, I32, P]),
         "forge_embed_bwd": (ctypes.c_int, [P, P, P, I32, I32, I32, F32, P]),
@@ -163,6 +183,12 @@ def load():
                                                 [ctypes.POINTER(AttnCfg), SZ]),
         "forge_attention_bwd": (ctypes.c_int, [ctypes.POINTER(AttnCfg), P, P, P, P, P,
                                                P, P]),
+        "forge_attention_window_fwd": (ctypes.c_int, [ctypes.POINTER(AttnWindowCfg), P, P, P, P,
+                                                      P]),
+        "forge_attention_window_bwd_workspace_bytes": (ctypes.c_int,
+                                                       [ctypes.POINTER(AttnWindowCfg), SZ]),
+        "forge_attention_window_bwd": (ctypes.c_int, [ctypes.POINTER(AttnWindowCfg), P, P, P, P,
+                                                      P, P, P, P]),
         "forge_moe_route_workspace_bytes": (ctypes.c_int, [I32, I32, I32, SZ]),
         "forge_moe_route": (ctypes.c_int, [P, I32, I32, I32, P, P, P, P, P, P, P, P]),
         "forge_moe_route_noalloc": (ctypes.c_int, [P, I32, I32, I32, P, P, P, P, P, P, P]),
@@ -239,6 +265,20 @@ def layer_optim(t: dict) -> LayerOptim:
 
 def attn_cfg(c: dict) -> AttnCfg:
     return AttnCfg(c["batch"], c["seq"], c["n_heads"], c["n_kv_heads"], c["head_dim"])
+
+
+def attn_window_cfg(c: dict) -> AttnWindowCfg:
+    return AttnWindowCfg(c["batch"], c["seq"], c["n_heads"], c["n_kv_heads"], c["head_dim"],
+                         c["window"], c.get("sinks", 0))
+
+
+def rope_axes_cfg(c: dict) -> RopeAxesCfg:
+    """c: head_dim, pairs (pairs per axis), and optionally interleaved, own_ladder."""
+    pairs = list(c["pairs"])
+    if len(pairs) > ROPE_MAX_AXES:
+        raise ValueError(f"at most {ROPE_MAX_AXES} axes (got {len(pairs)})")
+    return RopeAxesCfg(c["head_dim"], len(pairs), (ctypes.c_int32 * ROPE_MAX_AXES)(*pairs),
+                       int(bool(c.get("interleaved", 0))), int(bool(c.get("own_ladder", 0))))
 
 
 # ---------------------------------------------------------------- calls ----
@@ -344,6 +384,37 @@ def forge_rope_apply(qkv, ld, rope_cos, rope_sin, positions, tokens, seq, n_rot,
                                    int(bool(inverse)), _stream(stream)))
 
 
+def forge_layernorm_fwd(x, g, b, y, mean, rstd, tokens, hidden, eps, stream=None):
+    _check(load().forge_layernorm_fwd(_ptr(x), _ptr(g), _ptr(b), _ptr(y), _ptr(mean), _ptr(rstd),
+                                      tokens, hidden, float(eps), _stream(stream)))
+
+
+def forge_layernorm_bwd_workspace_bytes(tokens, hidden) -> int:
+    n = ctypes.c_size_t()
+    _check(load().forge_layernorm_bwd_workspace_bytes(tokens, hidden, ctypes.byref(n)))
+    return n.value
+
+
+def forge_layernorm_bwd(x, g, mean, rstd, dy, resid, dx, dg, db, accumulate, tokens, hidden,
+                        workspace, stream=None):
+    _check(load().forge_layernorm_bwd(_ptr(x), _ptr(g), _ptr(mean), _ptr(rstd), _ptr(dy),
+                                      _ptr(resid), _ptr(dx), _ptr(dg), _ptr(db),
+                                      int(bool(accumulate)), tokens, hidden, _ptr(workspace),
+                                      _stream(stream)))
+
+
+def forge_rope_axes_table(cfg: RopeAxesCfg, n_positions, base, cos_out, sin_out, stream=None):
+    _check(load().forge_rope_axes_table(ctypes.byref(cfg), n_positions, float(base),
+                                        _ptr(cos_out), _ptr(sin_out), _stream(stream)))
+
+
+def forge_rope_axes_apply(cfg: RopeAxesCfg, x, ldx, y, ldy, rope_cos, rope_sin, positions, tokens,
+                          n_positions, n_rot, inverse=False, stream=None):
+    _check(load().forge_rope_axes_apply(ctypes.byref(cfg), _ptr(x), int(ldx), _ptr(y), int(ldy),
+                                        _ptr(rope_cos), _ptr(rope_sin), _ptr(positions), tokens,
+                                        n_positions, n_rot, int(bool(inverse)), _stream(stream)))
+
+
 def forge_swiglu_fwd(gu, a, tokens, ffn, stream=None):
     _check(load().forge_swiglu_fwd(_ptr(gu), _ptr(a), tokens, ffn, _stream(stream)))
 
@@ -444,6 +515,24 @@ def forge_attention_bwd(cfg: AttnCfg, qkv, o, lse, d_o, d_qkv, workspace, stream
     _check(load().forge_attention_bwd(ctypes.byref(cfg), _ptr(qkv), _ptr(o), _ptr(lse),
                                       _ptr(d_o), _ptr(d_qkv), _ptr(workspace),
                                       _stream(stream)))
+
+
+def forge_attention_window_fwd(cfg: AttnWindowCfg, qkv, seq_lens, o, lse, stream=None):
+    _check(load().forge_attention_window_fwd(ctypes.byref(cfg), _ptr(qkv), _ptr(seq_lens), _ptr(o),
+                                             _ptr(lse), _stream(stream)))
+
+
+def forge_attention_window_bwd_workspace_bytes(cfg: AttnWindowCfg) -> int:
+    n = ctypes.c_size_t()
+    _check(load().forge_attention_window_bwd_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def forge_attention_window_bwd(cfg: AttnWindowCfg, qkv, seq_lens, o, lse, d_o, d_qkv, workspace,
+                               stream=None):
+    _check(load().forge_attention_window_bwd(ctypes.byref(cfg), _ptr(qkv), _ptr(seq_lens), _ptr(o),
+                                             _ptr(lse), _ptr(d_o), _ptr(d_qkv), _ptr(workspace),
+                                             _stream(stream)))
 
 
 def forge_moe_route_workspace_bytes(tokens, n_experts, top_k) -> int:

@@ -147,6 +147,35 @@ __device__ __forceinline__ bf16x8_t gload_frag(const bf16_t* p, bool ok) {
                                          : make_uint4(0, 0, 0, 0));
 }
 
+// ------------------------------------------------------ sliding window ----
+// The kernels' WIN form (arguments AttnWindowArgs): key j is visible to query i iff j <= i and (j > i -
+// window or j < sinks), both below the batch row's length. The key tiles of a
+// query block are those of the sinks that lie before its window, then the
+// window's up to the diagonal; a key tile's queries are those of its window,
+// of a sink tile all behind it. Rows at or past the length are not read and
+// get zeros (and a log-sum-exp of -inf).
+template <typename Args>
+constexpr bool kWindow = std::is_same_v<Args, AttnWindowArgs>;
+__device__ __forceinline__ int row_len(const AttnArgs& a, int) { return a.seq; }
+__device__ __forceinline__ int row_len(const AttnWindowArgs& a, int b) {
+  return a.lens ? min(max(a.lens[b], 0), a.seq) : a.seq;
+}
+// The rows of a batch row, of which `len` are its tokens.
+__device__ __forceinline__ int seq_of(const AttnArgs&, int len) { return len; }
+__device__ __forceinline__ int seq_of(const AttnWindowArgs& a, int) { return a.seq; }
+struct WindowTiles {
+  int sinks, skip, count;   // sink tiles before the window, tiles between, tiles in all
+  // queries [q0, end) with key tiles of 64
+  template <typename Args>
+  __device__ __forceinline__ WindowTiles(const Args& a, int q0, int end) {
+    const int w0 = max(0, q0 - a.window + 1) / 64;
+    sinks = min((a.sinks + 63) / 64, w0);
+    skip = w0 - sinks;
+    count = (end - 1) / 64 + 1 - skip;
+  }
+  __device__ __forceinline__ int operator()(int j) const { return j < sinks ? j : j + skip; }
+};
+
 __device__ __forceinline__ void zero(f32x16_t& a) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) a[e] = 0.0f;
@@ -249,9 +278,10 @@ __device__ __forceinline__ float sum_xor32(float v) {
 }
 }  // namespace fa
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a, bf16_t* __restrict__ o,
+template <int D, typename Args>
+__global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict__ o,
                                                          float* __restrict__ lse) {
+  constexpr bool WIN = kWindow<Args>;
   constexpr int BQ = 128, BKV = 64, NAT = BKV * D / 8, KK = D / 16, DB = D / 32;
   constexpr int TILE_B = NAT * 16;       // bytes of one K or V tile
   constexpr int HALF_B = TILE_B / 2;     // rows 32..63 of a tile
@@ -277,6 +307,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a, bf16_t* __restr
   const int qt = nqt - 1 - level;
   const int n = L % a.n_heads, b = L / a.n_heads;
   const int m = n / (a.n_heads / a.n_kv_heads);
+  const int E = WIN ? row_len(a, b) : S;   // end of the batch row's tokens
   const long rb = (long)b * S;
   const bf16_t* Qg = a.q + rb * a.ld_qkv + (long)n * D;
   const bf16_t* Kg = a.k + rb * a.ld_qkv + (long)m * D;
@@ -289,16 +320,25 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a, bf16_t* __restr
   bf16x8_t qf[KK];
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk)
-    qf[kk] = gload_frag(Qg + (long)q * a.ld_qkv + kk * 16 + hh * 8, q < S);
+    qf[kk] = gload_frag(Qg + (long)q * a.ld_qkv + kk * 16 + hh * 8, q < E);
   f32x16_t oacc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) zero(oacc[db]);
-  float mrow = -INFINITY, lrow = 0.0f;
+  // (WIN: a tile may hide all its keys from a row, whose maximum is then still
+  // the first value: finite, so that the scores' -inf minus it stays -inf)
+  float mrow = WIN ? -3e38f : -INFINITY, lrow = 0.0f;
   const float c = a.scale * kLog2e;
-  const int q_last = min(qt * BQ + BQ, S) - 1;
-  const int nkt = q_last / BKV + 1;
+  const int q_last = min(qt * BQ + BQ, E) - 1;
+  const WindowTiles win(a, qt * BQ, q_last + 1);
+  const int nkt = WIN ? win.count : q_last / BKV + 1;
+  const auto tile_of = [&](int j) __attribute__((always_inline)) { return WIN ? win(j) : j; };
   // the wave's last key tile (its queries end at q0w + 31)
-  const int lw = min(q0w + 31, S - 1) / BKV;
+  const int lw = min(q0w + 31, E - 1) / BKV;
+  // whether the wave's queries see a key of tile j
+  const auto sees = [&](int j) __attribute__((always_inline)) {
+    const int k0 = tile_of(j) * BKV;
+    return k0 <= lw * BKV && (k0 < a.sinks || k0 + BKV - 1 > q0w - a.window);
+  };
 
   // per-lane byte addresses in K slot 0 / V slot 0: K row fragment of slice
   // kk (rows 0..31), V^T fragment of column block db (rows 0..15, both row
@@ -320,11 +360,11 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a, bf16_t* __restr
 
   uint32_t doff[DmaPlan<D, 4>::PER];
   dma_offsets<D, 4>(a.ld_qkv, wave, lane, doff);
-  auto dma_k = [&](int kt) __attribute__((always_inline)) {
-    dma_tile_at<D, 4>(Kg, a.ld_qkv, kt * BKV, S, smem + (kt & 1) * NAT, wave, doff);
+  auto dma_k = [&](int j) __attribute__((always_inline)) {
+    dma_tile_at<D, 4>(Kg, a.ld_qkv, tile_of(j) * BKV, E, smem + (j & 1) * NAT, wave, doff);
   };
-  auto dma_v = [&](int kt) __attribute__((always_inline)) {
-    dma_tile_at<D, 4>(Vg, a.ld_qkv, kt * BKV, S, smem + (2 + (kt & 1)) * NAT, wave, doff);
+  auto dma_v = [&](int j) __attribute__((always_inline)) {
+    dma_tile_at<D, 4>(Vg, a.ld_qkv, tile_of(j) * BKV, E, smem + (2 + (j & 1)) * NAT, wave, doff);
   };
 
   // S^T of a tile (K slot KS) into sc: K fragments KW steps ahead, each MFMA
@@ -365,8 +405,8 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a, bf16_t* __restr
 
   // causal mask of a tile that straddles the wave's diagonal, then the row
   // max, the lazy rescale; returns -running max (log2 units)
-  auto softmax_head = [&](f32x16_t (&s)[2], int kt) __attribute__((always_inline)) {
-    const int k0 = kt * BKV;
+  auto softmax_head = [&](f32x16_t (&s)[2], int j) __attribute__((always_inline)) {
+    const int k0 = tile_of(j) * BKV;
     if (k0 + BKV - 1 > q0w) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -375,6 +415,19 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a, bf16_t* __restr
           const int key = k0 + kb * 32 + (i >> 2) * 8 + hh * 4 + (i & 3);
           if (key > q) s[kb][i] = -INFINITY;
         }
+    }
+    if constexpr (WIN) {
+      // the same of a tile that the window's far edge crosses
+      if (k0 <= q0w + 31 - a.window && k0 + BKV - 1 >= a.sinks) {
+        const int far = q - a.window - k0 - hh * 4, sink = a.sinks - k0 - hh * 4;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = kb * 32 + (i >> 2) * 8 + (i & 3);
+            if (key <= far && key >= sink) s[kb][i] = -INFINITY;
+          }
+      }
     }
     // two running-max chains over the lane's 32 scores (the compiler forms
     // v_max3 without quieting every operand first)
@@ -454,9 +507,14 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a, bf16_t* __restr
     fa::sync_block();
     if (j + 2 < nkt) dma_k(j + 2);
     if (j + 1 < nkt) dma_v(j + 1);
-    if (j > lw) return;   // every query of this wave is before the tile
+    const bool next = WIN ? j + 1 < nkt && sees(j + 1) : j < lw;
+    // no query of this wave sees a key of the tile: all are before it (WIN: or
+    // past its window; the last such tile runs all the same, its scores hidden
+    // whatever they hold, since the next one's are due now: as a branch of its
+    // own that product costs 500 spilled registers)
+    if (WIN ? !sees(j) && !next : j > lw) return;
     const float nm = softmax_head(scur, j);
-    if (j < lw) {
+    if (next) {
       // the 8 exp steps of 4 spread over the KK MFMA steps of the next
       // tile's scores
       static_assert(8 % KK == 0, "exp steps per MFMA step");
@@ -475,29 +533,51 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a, bf16_t* __restr
     pv(fa::ic<P>{}, scur);
   };
 
+  const long orow_ld = (long)(a.n_heads * D);
+  if (WIN && qt * BQ >= E) {
+    // no tokens: zeros
+    if (q < S) {
+      bf16_t* orow = o + (rb + q) * orow_ld + (long)n * D;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<uint2*>(orow + db * 32 + g * 8 + hh * 4) = make_uint2(0, 0);
+      if (hh == 0) lse[((long)b * a.n_heads + n) * S + q] = -INFINITY;
+    }
+    return;
+  }
   dma_k(0);
   dma_v(0);
   if (nkt > 1) dma_k(1);
   fa::sync_block();
   scores(fa::ic<0>{}, sa, no_hook);
+  if constexpr (WIN) {
+    zero(sb[0]);
+    zero(sb[1]);
+  }
   for (int j = 0; j < nkt; j += 2) {
     iteration(fa::ic<0>{}, sa, sb, j);
     if (j + 1 < nkt) iteration(fa::ic<1>{}, sb, sa, j + 1);
   }
   lrow = fa::sum_xor32(lrow);
   if (q < S) {
+    // (WIN: rows past the tokens' end get zeros and -inf)
+    const bool none = WIN && q >= E;
     const float inv = 1.0f / lrow;
-    bf16_t* orow = o + (rb + q) * (long)(a.n_heads * D) + (long)n * D;
+    bf16_t* orow = o + (rb + q) * orow_ld + (long)n * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int dd = db * 32 + g * 8 + hh * 4;
         *reinterpret_cast<uint2*>(orow + dd) =
-            make_uint2(pack2(oacc[db][g * 4 + 0] * inv, oacc[db][g * 4 + 1] * inv),
-                       pack2(oacc[db][g * 4 + 2] * inv, oacc[db][g * 4 + 3] * inv));
+            none ? make_uint2(0, 0)
+                 : make_uint2(pack2(oacc[db][g * 4 + 0] * inv, oacc[db][g * 4 + 1] * inv),
+                              pack2(oacc[db][g * 4 + 2] * inv, oacc[db][g * 4 + 3] * inv));
       }
-    if (hh == 0) lse[((long)b * a.n_heads + n) * S + q] = (mrow + log2f(lrow)) * kLn2;
+    if (hh == 0)
+      lse[((long)b * a.n_heads + n) * S + q] = none ? -INFINITY : (mrow + log2f(lrow)) * kLn2;
   }
 }
 
@@ -539,6 +619,29 @@ struct DsLayout {
   __host__ __device__ long tile(int kt) const { return 2048L * ((long)kt * ns - (long)kt * (kt - 1)); }
   __host__ __device__ long block(int kt, int j) const { return tile(kt) + 2048L * (j - 2 * kt); }
 };
+
+// WIN: a sink tile (kt < nst) has a block for every slab of the sequence, the
+// others for the nwin slabs from 2 kt on that its keys' windows can reach.
+struct DsWindow {
+  int ns, nst, nwin;
+  long head;
+  __host__ __device__ explicit DsWindow(const AttnWindowArgs& a) {
+    ns = (a.seq + 31) / 32;
+    nst = (a.sinks + 63) / 64;
+    nwin = (62 + a.window) / 32 + 1;
+    if (nwin > ns) nwin = ns;
+    head = 2048L * ((long)nst * ns + (long)((a.seq + 63) / 64 - nst) * nwin);
+  }
+  // the tile's first block and the slab it belongs to
+  __host__ __device__ long tile(int kt) const {
+    return 2048L * (kt < nst ? (long)kt * ns : (long)nst * ns + (long)(kt - nst) * nwin);
+  }
+  __host__ __device__ int first(int kt) const { return kt < nst ? 0 : 2 * kt; }
+  __host__ __device__ long block(int kt, int j) const { return tile(kt) + 2048L * (j - first(kt)); }
+};
+
+__device__ __forceinline__ DsLayout ds_layout(const AttnArgs& a) { return DsLayout(a.seq); }
+__device__ __forceinline__ DsWindow ds_layout(const AttnWindowArgs& a) { return DsWindow(a); }
 
 // 1. -delta and -LSE log2(e) of every (batch, head, query): D / 8 lanes per
 // (token, head) row of dO and O, 16-byte loads (the heads of a token are
@@ -740,8 +843,8 @@ __device__ __forceinline__ f32x16_t rows16(const bf16x8_t (&r)[4]) {
   return x;
 }
 
-template <int D>
-__global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(AttnArgs a,
+template <int D, typename Args>
+__global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
                                                        const bf16_t* __restrict__ dout,
                                                        const float* __restrict__ delta,
                                                        bf16_t* __restrict__ ds,
@@ -751,27 +854,34 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(AttnArgs a,
                                                        float* __restrict__ pk, int splits) {
   using P = KvPlan<D>;
   using B = KvBuf<D>;
+  constexpr bool WIN = kWindow<Args>;
   constexpr bool VL = kVInLds<D>;
   constexpr int BK = P::BK, BQ = P::BQ, SLAB = P::SLAB, KK = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(256))) uint4 sm[B::ARR];
 
-  const int S = a.seq;
+  int S = a.seq;                               // tokens of the batch row
   const int grp = a.n_heads / a.n_kv_heads;
   // block order: key tile slowest, so the low key tiles (the most work)
   // are dispatched first
   const KvBlock kb_(a, splits);
   const int kt = kb_.kt, m = kb_.m, b = kb_.b;
   const int k0 = kt * BK;
+  if constexpr (WIN) S = row_len(a, b);
   const int j0 = k0 / BQ;                      // first slab holding a query >= k0
-  const int ns = (S + BQ - 1) / BQ - j0;       // slabs per query head
+  // slabs per query head (WIN: those that see the keys, none without tokens)
+  int ns = (S + BQ - 1) / BQ - j0;
+  if constexpr (WIN) {
+    const DsWindow L(a);
+    ns = max(0, kt < L.nst ? ns : min(ns, L.nwin));
+  }
   const int total = grp * ns;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5, l32 = lane & 31;
-  const long rb = (long)b * S;
+  const long rb = (long)b * seq_of(a, S);
   const long ldo = (long)a.n_heads * D;
-  const long nrows = (long)a.batch * a.n_heads * S;
-  const DsLayout L(S);
+  const long nrows = (long)a.batch * a.n_heads * seq_of(a, S);
+  const auto L = ds_layout(a);
 
   // K and V rows of the lane's two keys k0 + l32 and k0 + 32 + l32: the
   // B operands of S and dP
@@ -873,7 +983,7 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(AttnArgs a,
       dma_16(w.o, rows * orb, base + SLAB + j * 64,
              orow + (c0 ^ fsw<D>(j * P::RPI) * 16) + (j * P::RPI * orb + z));
     } else {
-      const long li = ((long)b * a.n_heads + w.n) * S + w.q0 + l32;
+      const long li = ((long)b * a.n_heads + w.n) * seq_of(a, S) + w.q0 + l32;
       dma_4(delta, base + 2 * SLAB,
             w.q0 + l32 < S ? (uint32_t)(((hh ? 0 : nrows) + li) * 4) : kOOB);
     }
@@ -1065,6 +1175,7 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(AttnArgs a,
         // causal mask and sequence tail (diagonal and last slabs only), once S
         // is complete: -inf scores, so exp2 gives 0
         if constexpr (i == KK && kb == 0) {
+          // (WIN: and where the window's far edge crosses the block)
           if (q0 < k0 + BK - 1 || q0 + BQ > S) {
 #pragma unroll
             for (int mb = 0; mb < 2; ++mb)
@@ -1073,6 +1184,17 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(AttnArgs a,
                 const int q = q0 + (e >> 2) * 8 + hh * 4 + (e & 3);
                 if (k0 + mb * 32 + l32 > q || q >= S) sc[mb][e] = -INFINITY;
               }
+          }
+          if constexpr (WIN) {
+            if (k0 <= q0 + BQ - 1 - a.window && k0 + BK - 1 >= a.sinks) {
+#pragma unroll
+              for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const int q = q0 + (e >> 2) * 8 + hh * 4 + (e & 3), key = k0 + mb * 32 + l32;
+                  if (key <= q - a.window && key >= a.sinks) sc[mb][e] = -INFINITY;
+                }
+            }
           }
         }
         under(fa::ic<2 * i + kb>{});
@@ -1086,7 +1208,8 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(AttnArgs a,
   uint4* mine = sm + wave * 2 * B::WBUF;
   int cur = 0;
   Pair w = pair_at(min(p0, total - 1));
-  static_for<B::DMA>([&](auto I) __attribute__((always_inline)) { dma(I, w, 0, mine); });
+  if (!WIN || total > 0)
+    static_for<B::DMA>([&](auto I) __attribute__((always_inline)) { dma(I, w, 0, mine); });
   for (int p = p0; p < total; p += step) {
     const Pair wn = p + step < total ? advance(w) : w;
     pair(mine + cur * B::WBUF, w, mine + (cur ^ 1) * B::WBUF, wn);
@@ -1096,10 +1219,10 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(AttnArgs a,
   }
   if (dsblk) store_ds();
   kv_reduce_store<D>(acc, sm, sm + 2 * P::RED, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D,
-                     ld_d, kv_part<D>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D, S - k0);
+                     ld_d, kv_part<D>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D, seq_of(a, S) - k0);
   kv_reduce_store<D>(acck, sm, sm + 2 * P::RED, wave, lane, a.scale,
                      dk + (rb + k0) * ld_d + (long)m * D, ld_d,
-                     kv_part<D>(a, pk, kb_, rb + k0), (long)a.n_kv_heads * D, S - k0);
+                     kv_part<D>(a, pk, kb_, rb + k0), (long)a.n_kv_heads * D, seq_of(a, S) - k0);
 }
 
 // dK and dV from the splits' partial sums, added in split order; eight columns
@@ -1149,10 +1272,11 @@ struct DqPlan {
   static constexpr int MEM = DmaPlan<D, NW>::PER + NDS / 64 / NW;   // DMA per wave per tile
 };
 
-template <int D>
-__global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(AttnArgs a, const bf16_t* __restrict__ ds,
+template <int D, typename Args>
+__global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(Args a, const bf16_t* __restrict__ ds,
                                                        bf16_t* __restrict__ dq, long ld_d) {
   using Q = DqPlan<D>;
+  constexpr bool WIN = kWindow<Args>;
   constexpr int BQ = Q::BQ, BKV = Q::BKV, NAT = Q::NAT, NW = Q::NW, NST = Q::NST, DB = D / 32;
   __shared__ uint4 sm[NST * Q::STAGE];
   const int S = a.seq;
@@ -1167,7 +1291,8 @@ __global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(AttnArgs a, const bf16_t
   const int b = id / a.n_kv_heads / grp % a.batch;
   const int qt = nqt - 1 - id / (a.n_kv_heads * grp * a.batch);
   const long rb = (long)b * S;
-  const DsLayout L(S);
+  const int E = WIN ? row_len(a, b) : S;   // end of the batch row's tokens
+  const auto L = ds_layout(a);
   const bf16_t* Kg = a.k + rb * a.ld_qkv + (long)m * D;
   const bf16_t* dsh = ds + ((long)b * a.n_heads + n) * L.head;
   const int lane = threadIdx.x & 63;
@@ -1179,8 +1304,10 @@ __global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(AttnArgs a, const bf16_t
   f32x16_t dqa[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) zero(dqa[db]);
-  const int q_last = min(qb0 + BQ, S) - 1;
-  const int nkt = q_last / BKV + 1;
+  const int q_last = min(qb0 + BQ, E) - 1;
+  const WindowTiles win(a, qb0, q_last + 1);
+  const int nkt = !WIN ? q_last / BKV + 1 : qb0 < E ? win.count : 0;
+  const auto tile_of = [&](int j) __attribute__((always_inline)) { return WIN ? win(j) : j; };
   uint32_t koff[DmaPlan<D, NW>::PER];
   dma_offsets<D, NW>(a.ld_qkv, wave, lane, koff);
   // dS: instruction t of wave w copies KB c = 8 t + w of the tile, the
@@ -1188,9 +1315,17 @@ __global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(AttnArgs a, const bf16_t
   // sequence end lie past the tile's extent and read as zeros
   auto dma = [&](int kt, int st) __attribute__((always_inline)) {
     uint4* stg = sm + st * Q::STAGE;
-    dma_tile_at<D, NW>(Kg, a.ld_qkv, kt * BKV, S, stg, wave, koff);
-    const int jb = qb0 / 32 - 2 * kt;   // block of slab qb0 / 32 in the tile (>= -6)
-    const __amdgpu_buffer_rsrc_t r = rsrc_n(dsh + L.tile(kt), 4096L * (L.ns - 2 * kt));
+    dma_tile_at<D, NW>(Kg, a.ld_qkv, kt * BKV, E, stg, wave, koff);
+    // block of slab qb0 / 32 in the tile (>= -6), first block and blocks of it
+    int jb = qb0 / 32 - 2 * kt, lo = 0, nb = L.ns - 2 * kt;
+    if constexpr (WIN) {
+      const int first = L.first(kt);
+      jb = qb0 / 32 - first;
+      lo = 2 * kt - first;
+      nb = (E + 31) / 32 - first;
+      if (kt >= L.nst) nb = min(nb, L.nwin);
+    }
+    const __amdgpu_buffer_rsrc_t r = rsrc_n(dsh + L.tile(kt), 4096L * nb);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int c = t * NW + wave;
@@ -1198,7 +1333,7 @@ __global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(AttnArgs a, const bf16_t
       // non-temporal (cache policy 2): dS is read once here; K stays in L2
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           r, (lds_ptr_t)(stg + NAT + c * 64), 16,
-          blk < 0 ? kOOB : (uint32_t)((2048 * blk + ((c & 3) * 64 + lane) * 8) * 2), 0, 0, 2);
+          blk < lo ? kOOB : (uint32_t)((2048 * blk + ((c & 3) * 64 + lane) * 8) * 2), 0, 0, 2);
     }
   };
   // per-lane offsets: K^T fragments of column block db; the wave's dS^T
@@ -1243,6 +1378,9 @@ __global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(AttnArgs a, const bf16_t
   };
   auto tile = [&](int kt, int st) __attribute__((always_inline)) {
     if (kt * BKV > q0w + 31) return;   // every query of this wave precedes the tile
+    if constexpr (WIN) {
+      if (kt >= L.nst && kt * BKV + BKV - 1 <= q0w - a.window) return;   // or is past its window
+    }
     const uint32_t sb = smb + st * Q::STAGE * 16;
     constexpr int NRS = 2 * (DB + 1);   // reads of one key step
     bf16x8_t bt[4], at[4][DB];
@@ -1271,17 +1409,25 @@ __global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(AttnArgs a, const bf16_t
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
   };
-  dma(0, 0);
-  if (nkt > 1) dma(1, 1);
-  sync(nkt > 1);
+  if (!WIN || nkt > 0) {
+    dma(tile_of(0), 0);
+    if (nkt > 1) dma(tile_of(1), 1);
+    sync(nkt > 1);
+  }
   int st = 0;
-  for (int kt = 0; kt < nkt; ++kt) {
-    if (kt + 2 < nkt) dma(kt + 2, st == 0 ? 2 : st - 1);
-    tile(kt, st);
-    if (kt + 1 < nkt) sync(kt + 2 < nkt);
+  for (int j = 0; j < nkt; ++j) {
+    if (j + 2 < nkt) dma(tile_of(j + 2), st == 0 ? 2 : st - 1);
+    tile(tile_of(j), st);
+    if (j + 1 < nkt) sync(j + 2 < nkt);
     st = st == NST - 1 ? 0 : st + 1;
   }
   if (q < S) {
+    // (WIN: rows past the tokens' end have no dS and no tiles of their own, but
+    // share a block's with those before it)
+    if (WIN && q >= E) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) zero(dqa[db]);
+    }
     bf16_t* dqr = dq + (rb + q) * ld_d + (long)n * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -1297,16 +1443,29 @@ __global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(AttnArgs a, const bf16_t
 
 }  // namespace
 
-hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s) {
+namespace {
+template <typename Args>
+hipError_t attn_fwd_any(const Args& a, uint16_t* o, float* lse, hipStream_t s) {
   const dim3 grid((unsigned)((a.seq + 127) / 128 * a.n_heads * a.batch)), block(256);
-  if (a.d == 128) hipLaunchKernelGGL(attn_fwd_k<128>, grid, block, 0, s, a, o, lse);
-  else if (a.d == 64) hipLaunchKernelGGL(attn_fwd_k<64>, grid, block, 0, s, a, o, lse);
+  if (a.d == 128) hipLaunchKernelGGL((attn_fwd_k<128, Args>), grid, block, 0, s, a, o, lse);
+  else if (a.d == 64) hipLaunchKernelGGL((attn_fwd_k<64, Args>), grid, block, 0, s, a, o, lse);
   else return hipErrorInvalidValue;
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s) {
+  return attn_fwd_any(a, o, lse, s);
+}
+hipError_t attn_window_fwd(const AttnWindowArgs& a, uint16_t* o, float* lse, hipStream_t s) {
+  return attn_fwd_any(a, o, lse, s);
 }
 
 size_t attn_bwd_ds_bytes(const AttnArgs& a) {
   return (size_t)a.batch * a.n_heads * DsLayout(a.seq).head * 2;
+}
+size_t attn_window_bwd_ds_bytes(const AttnWindowArgs& a) {
+  return (size_t)a.batch * a.n_heads * DsWindow(a).head * 2;
 }
 
 // Splits of a key-owned block's pairs: the smallest estimate of the kv pass. One
@@ -1352,9 +1511,12 @@ size_t attn_bwd_part_bytes(const AttnArgs& a) {
   return z > 1 ? (size_t)2 * z * a.batch * a.seq * a.n_kv_heads * a.d * 4 : 0;
 }
 
+static int kv_splits(const AttnWindowArgs&) { return 1; }
+size_t attn_window_bwd_part_bytes(const AttnWindowArgs&) { return 0; }
+
 namespace {
-template <int D>
-hipError_t attn_bwd_d(const AttnArgs& a, const uint16_t* o, const uint16_t* dout, const float* lse,
+template <int D, typename Args>
+hipError_t attn_bwd_d(const Args& a, const uint16_t* o, const uint16_t* dout, const float* lse,
                       float* delta, uint16_t* ds, float* part, uint16_t* dq, uint16_t* dk,
                       uint16_t* dv, long ld_d, hipStream_t s) {
   const long T = (long)a.batch * a.seq, rows = T * a.n_heads;
@@ -1367,14 +1529,14 @@ hipError_t attn_bwd_d(const AttnArgs& a, const uint16_t* o, const uint16_t* dout
   const dim3 qgrid((unsigned)((a.seq + 255) / 256 * a.n_heads * a.batch));
   hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
                      a.seq);
-  hipLaunchKernelGGL(attn_bwd_kv_k<D>, kgrid, block, 0, s, a, dout, delta, ds, dv, dk, ld_d, pv, pk,
+  hipLaunchKernelGGL((attn_bwd_kv_k<D, Args>), kgrid, block, 0, s, a, dout, delta, ds, dv, dk, ld_d, pv, pk,
                      z);
   if (z > 1) {
     const dim3 sgrid((unsigned)((T * (width / 8) + 255) / 256), 2);
     hipLaunchKernelGGL(attn_bwd_kv_sum_k, sgrid, block, 0, s, pk, pv, z, T, width, a.scale, dk, dv,
                        ld_d);
   }
-  hipLaunchKernelGGL(attn_bwd_dq_k<D>, qgrid, dim3(512), 0, s, a, ds, dq, ld_d);
+  hipLaunchKernelGGL((attn_bwd_dq_k<D, Args>), qgrid, dim3(512), 0, s, a, ds, dq, ld_d);
   return hipGetLastError();
 }
 }  // namespace
@@ -1382,6 +1544,13 @@ hipError_t attn_bwd_d(const AttnArgs& a, const uint16_t* o, const uint16_t* dout
 hipError_t attn_bwd(const AttnArgs& a, const uint16_t* o, const uint16_t* dout, const float* lse,
                     float* delta, uint16_t* ds, float* part, uint16_t* dq, uint16_t* dk,
                     uint16_t* dv, long ld_d, hipStream_t s) {
+  if (a.d == 128) return attn_bwd_d<128>(a, o, dout, lse, delta, ds, part, dq, dk, dv, ld_d, s);
+  if (a.d == 64) return attn_bwd_d<64>(a, o, dout, lse, delta, ds, part, dq, dk, dv, ld_d, s);
+  return hipErrorInvalidValue;
+}
+hipError_t attn_window_bwd(const AttnWindowArgs& a, const uint16_t* o, const uint16_t* dout,
+                           const float* lse, float* delta, uint16_t* ds, float* part, uint16_t* dq,
+                           uint16_t* dk, uint16_t* dv, long ld_d, hipStream_t s) {
   if (a.d == 128) return attn_bwd_d<128>(a, o, dout, lse, delta, ds, part, dq, dk, dv, ld_d, s);
   if (a.d == 64) return attn_bwd_d<64>(a, o, dout, lse, delta, ds, part, dq, dk, dv, ld_d, s);
   return hipErrorInvalidValue;

@@ -937,6 +937,151 @@ forge_status forge_rope_apply(forge_bf16* qkv, int64_t ld, const float* rope_cos
   return ok();
 }
 
+forge_status forge_layernorm_fwd(const forge_bf16* x, const forge_bf16* g, const forge_bf16* b,
+                                 forge_bf16* y, float* mean, float* rstd, int32_t tokens,
+                                 int32_t hidden, float eps, forge_stream stream) {
+  if (forge_status s = check_rows(tokens, hidden)) return s;
+  FORGE_CHECK(eps >= 0.0f && std::isfinite(eps), FORGE_ERR_INVALID_ARG, "eps must be >= 0");
+  if (tokens == 0) return ok();
+  FORGE_PTR(x);
+  FORGE_PTR(g);
+  if (b) FORGE_PTR(b);
+  FORGE_PTR(y);
+  FORGE_PTR(mean);
+  FORGE_PTR(rstd);
+  const size_t n = (size_t)tokens * hidden * 2;
+  FORGE_CHECK(!overlap(x, n, y, n), FORGE_ERR_INVALID_ARG, "y overlaps x");
+  FORGE_HIP(forge::layernorm_fwd(x, g, b, y, mean, rstd, tokens, hidden, eps,
+                                 (hipStream_t)stream));
+  return ok();
+}
+
+forge_status forge_layernorm_bwd_workspace_bytes(int32_t tokens, int32_t hidden, size_t* bytes) {
+  if (forge_status s = check_rows(tokens, hidden)) return s;
+  FORGE_CHECK(bytes != nullptr, FORGE_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = (size_t)forge::layernorm_bwd_blocks(tokens, hidden) * 2 * hidden * 4;
+  return ok();
+}
+
+forge_status forge_layernorm_bwd(const forge_bf16* x, const forge_bf16* g, const float* mean,
+                                 const float* rstd, const forge_bf16* dy,
+                                 const forge_bf16* resid, forge_bf16* dx, float* dg, float* db,
+                                 int32_t accumulate, int32_t tokens, int32_t hidden,
+                                 void* workspace, forge_stream stream) {
+  if (forge_status s = check_rows(tokens, hidden)) return s;
+  FORGE_PTR(dg);
+  if (db) FORGE_PTR(db);
+  FORGE_CHECK(!overlap(dg, (size_t)hidden * 4, db, (size_t)hidden * 4), FORGE_ERR_INVALID_ARG,
+              "dg overlaps db");
+  // no rows: the gradients are empty sums, the stored ones zeros
+  if (tokens == 0 && accumulate) return ok();
+  if (tokens > 0) {
+    FORGE_PTR(x);
+    FORGE_PTR(g);
+    FORGE_PTR(mean);
+    FORGE_PTR(rstd);
+    FORGE_PTR(dy);
+    FORGE_PTR(dx);
+    FORGE_PTR(workspace);
+    if (resid) FORGE_PTR(resid);
+    const size_t n = (size_t)tokens * hidden * 2;
+    FORGE_CHECK(!overlap(dx, n, x, n) && !overlap(dx, n, dy, n) && !overlap(dx, n, resid, n),
+                FORGE_ERR_INVALID_ARG, "dx overlaps an input");
+  }
+  FORGE_HIP(forge::layernorm_bwd(x, g, mean, rstd, dy, resid, dx, dg, db, accumulate != 0,
+                                 static_cast<float*>(workspace), tokens, hidden,
+                                 (hipStream_t)stream));
+  return ok();
+}
+
+namespace {
+forge_status check_rope_axes(const forge_rope_axes_cfg* c) {
+  FORGE_CHECK(c != nullptr, FORGE_ERR_INVALID_ARG, "cfg is NULL");
+  FORGE_CHECK(c->head_dim >= 16 && c->head_dim % 16 == 0 &&
+                  c->head_dim / 2 <= forge::kRopeMaxPairs,
+              FORGE_ERR_INVALID_ARG, "head_dim must be a multiple of 16 in [16, %d] (got %d)",
+              2 * forge::kRopeMaxPairs, c->head_dim);
+  FORGE_CHECK(c->n_axes >= 1 && c->n_axes <= FORGE_ROPE_MAX_AXES, FORGE_ERR_INVALID_ARG,
+              "n_axes must be in [1, %d] (got %d)", FORGE_ROPE_MAX_AXES, c->n_axes);
+  int64_t sum = 0;
+  for (int a = 0; a < c->n_axes; ++a) {
+    FORGE_CHECK(c->pairs[a] >= 1, FORGE_ERR_INVALID_ARG, "pairs[%d] must be >= 1 (got %d)", a,
+                c->pairs[a]);
+    sum += c->pairs[a];
+  }
+  FORGE_CHECK(sum == c->head_dim / 2, FORGE_ERR_INVALID_ARG,
+              "the axes' pairs must add up to head_dim / 2 = %d", c->head_dim / 2);
+  return ok();
+}
+// The axis of every pair, and which pair of its axis it is.
+struct PairAxes {
+  int axis[forge::kRopeMaxPairs], index[forge::kRopeMaxPairs];
+  explicit PairAxes(const forge_rope_axes_cfg& c) {
+    int dealt[FORGE_ROPE_MAX_AXES] = {};
+    for (int i = 0, a = 0; i < c.head_dim / 2; ++i) {
+      while (dealt[a] == c.pairs[a]) a = a + 1 == c.n_axes ? 0 : a + 1;
+      axis[i] = a;
+      index[i] = dealt[a]++;
+      if (c.interleaved) a = a + 1 == c.n_axes ? 0 : a + 1;
+    }
+  }
+};
+}  // namespace
+
+forge_status forge_rope_axes_table(const forge_rope_axes_cfg* cfg, int32_t n_positions, float base,
+                                   float* cos_out, float* sin_out, forge_stream stream) {
+  if (forge_status s = check_rope_axes(cfg)) return s;
+  FORGE_CHECK(n_positions >= 1, FORGE_ERR_INVALID_ARG, "n_positions must be >= 1");
+  FORGE_CHECK((int64_t)n_positions * (cfg->head_dim / 2) < (1LL << 31), FORGE_ERR_UNSUPPORTED,
+              "a table exceeds 2^31 elements");
+  FORGE_CHECK(base > 0.0f && std::isfinite(base), FORGE_ERR_INVALID_ARG, "base must be > 0");
+  FORGE_PTR(cos_out);
+  FORGE_PTR(sin_out);
+  const PairAxes pa(*cfg);
+  forge::RopeFreqs f{};
+  for (int i = 0; i < cfg->head_dim / 2; ++i)
+    f.w[i] = std::pow((double)base, cfg->own_ladder
+                                        ? -(double)pa.index[i] / cfg->pairs[pa.axis[i]]
+                                        : -2.0 * i / cfg->head_dim);
+  FORGE_HIP(forge::rope_axes_table(f, n_positions, cfg->head_dim, cos_out, sin_out,
+                                   (hipStream_t)stream));
+  return ok();
+}
+
+forge_status forge_rope_axes_apply(const forge_rope_axes_cfg* cfg, const forge_bf16* x,
+                                   int64_t ldx, forge_bf16* y, int64_t ldy, const float* rope_cos,
+                                   const float* rope_sin, const int32_t* positions,
+                                   int32_t tokens, int32_t n_positions, int32_t n_rot,
+                                   int32_t inverse, forge_stream stream) {
+  if (forge_status s = check_rope_axes(cfg)) return s;
+  FORGE_CHECK(tokens >= 0 && n_positions >= 1 && n_rot >= 0, FORGE_ERR_INVALID_ARG,
+              "bad tokens / n_positions / n_rot");
+  const int64_t width = (int64_t)n_rot * cfg->head_dim;
+  FORGE_CHECK(ldx % 8 == 0 && ldy % 8 == 0 && width <= ldx && width <= ldy, FORGE_ERR_INVALID_ARG,
+              "ldx and ldy must be multiples of 8 holding n_rot heads");
+  if (tokens == 0 || n_rot == 0) return ok();
+  FORGE_CHECK(width / 16 < (1LL << 31) && (int64_t)tokens * (width / 16) < (1LL << 31),
+              FORGE_ERR_UNSUPPORTED, "tokens * n_rot * head_dim / 16 exceeds 2^31");
+  FORGE_PTR(x);
+  FORGE_PTR(y);
+  FORGE_PTR(rope_cos);
+  FORGE_PTR(rope_sin);
+  FORGE_CHECK(positions != nullptr, FORGE_ERR_INVALID_ARG, "positions is NULL");
+  FORGE_CHECK((reinterpret_cast<uintptr_t>(positions) & 3u) == 0, FORGE_ERR_ALIGNMENT,
+              "positions is not 4-byte aligned");
+  const auto extent = [&](int64_t ld) { return ((size_t)(tokens - 1) * ld + width) * 2; };
+  FORGE_CHECK((x == y && ldx == ldy) || !overlap(x, extent(ldx), y, extent(ldy)),
+              FORGE_ERR_INVALID_ARG, "y overlaps x");
+  const PairAxes pa(*cfg);
+  forge::RopeAxes ax{};
+  for (int i = 0; i < cfg->head_dim / 2; ++i)
+    ax.axis[i / 16] |= (uint32_t)pa.axis[i] << 2 * (i % 16);
+  FORGE_HIP(forge::rope_axes(ax, x, ldx, y, ldy, rope_cos, rope_sin, positions, tokens,
+                             n_positions, n_rot, cfg->head_dim, inverse != 0,
+                             (hipStream_t)stream));
+  return ok();
+}
+
 forge_status forge_swiglu_fwd(const forge_bf16* gu, forge_bf16* a, int32_t tokens, int32_t ffn,
                               forge_stream stream) {
   FORGE_CHECK(tokens >= 0 && ffn >= 8 && ffn % 8 == 0, FORGE_ERR_INVALID_ARG,
@@ -1755,6 +1900,91 @@ forge_status forge_attention_bwd(const forge_attn_cfg* cfg, const forge_bf16* qk
   float* part = at<float>(workspace, ds_off + up(forge::attn_bwd_ds_bytes(aa)));
   FORGE_HIP(forge::attn_bwd(aa, o, d_o, lse, delta, ds, part, d_qkv, d_qkv + d.hq,
                             d_qkv + d.hq + d.hkv, d.qkv, s));
+  return ok();
+}
+
+namespace {
+forge_status check_attn_window(const forge_attn_window_cfg* c) {
+  FORGE_CHECK(c != nullptr, FORGE_ERR_INVALID_ARG, "cfg is NULL");
+  const forge_attn_cfg a{c->batch, c->seq, c->n_heads, c->n_kv_heads, c->head_dim};
+  if (forge_status s = check_attn(&a)) return s;
+  FORGE_CHECK(c->window >= 1, FORGE_ERR_INVALID_ARG, "window must be >= 1 (got %d)", c->window);
+  FORGE_CHECK(c->sinks >= 0, FORGE_ERR_INVALID_ARG, "sinks must be >= 0 (got %d)", c->sinks);
+  // 32-bit offsets of the kernels' buffer accesses: a tile's rows, a sink tile's
+  // score gradient, the per-query statistics
+  FORGE_CHECK(c->seq <= 1 << 23, FORGE_ERR_UNSUPPORTED, "seq > 2^23 (got %d)", c->seq);
+  FORGE_CHECK((int64_t)c->n_heads + 2 * (int64_t)c->n_kv_heads <= (1 << 22) / c->head_dim,
+              FORGE_ERR_UNSUPPORTED, "a row of qkv exceeds 2^22 elements");
+  FORGE_CHECK((int64_t)c->batch * c->seq < (1 << 28) &&
+                  (int64_t)c->batch * c->seq * c->n_heads < (1 << 28),
+              FORGE_ERR_UNSUPPORTED, "batch * n_heads * seq exceeds 2^28");
+  return FORGE_OK;
+}
+struct WindowArgs : forge::AttnWindowArgs {
+  WindowArgs(const forge_attn_window_cfg& c, const uint16_t* qkv, const int32_t* seq_lens) {
+    const forge_attn_cfg a{c.batch, c.seq, c.n_heads, c.n_kv_heads, c.head_dim};
+    static_cast<forge::AttnArgs&>(*this) = attn_args(attn_dims(a), qkv);
+    window = std::min(c.window, c.seq);
+    sinks = std::min(c.sinks, c.seq);
+    lens = seq_lens;
+  }
+};
+}  // namespace
+
+forge_status forge_attention_window_fwd(const forge_attn_window_cfg* cfg, const forge_bf16* qkv,
+                                        const int32_t* seq_lens, forge_bf16* o, float* lse,
+                                        forge_stream stream) {
+  if (forge_status s = check_attn_window(cfg)) return s;
+  FORGE_PTR(qkv);
+  FORGE_PTR(o);
+  FORGE_PTR(lse);
+  FORGE_CHECK((reinterpret_cast<uintptr_t>(seq_lens) & 3u) == 0, FORGE_ERR_ALIGNMENT,
+              "seq_lens is not 4-byte aligned");
+  const WindowArgs a(*cfg, qkv, seq_lens);
+  const size_t rows = (size_t)cfg->batch * cfg->seq * 2;
+  FORGE_CHECK(!overlap(o, rows * cfg->n_heads * cfg->head_dim, qkv, rows * a.ld_qkv),
+              FORGE_ERR_INVALID_ARG, "o overlaps qkv");
+  FORGE_HIP(forge::attn_window_fwd(a, o, lse, (hipStream_t)stream));
+  return ok();
+}
+
+forge_status forge_attention_window_bwd_workspace_bytes(const forge_attn_window_cfg* cfg,
+                                                        size_t* bytes) {
+  if (forge_status s = check_attn_window(cfg)) return s;
+  FORGE_CHECK(bytes != nullptr, FORGE_ERR_INVALID_ARG, "bytes is NULL");
+  const WindowArgs a(*cfg, nullptr, nullptr);
+  *bytes = up(2 * (size_t)cfg->batch * cfg->n_heads * cfg->seq * 4) +
+           up(forge::attn_window_bwd_ds_bytes(a)) + up(forge::attn_window_bwd_part_bytes(a));
+  return ok();
+}
+
+forge_status forge_attention_window_bwd(const forge_attn_window_cfg* cfg, const forge_bf16* qkv,
+                                        const int32_t* seq_lens, const forge_bf16* o,
+                                        const float* lse, const forge_bf16* d_o,
+                                        forge_bf16* d_qkv, void* workspace, forge_stream stream) {
+  if (forge_status s = check_attn_window(cfg)) return s;
+  FORGE_PTR(qkv);
+  FORGE_PTR(o);
+  FORGE_PTR(lse);
+  FORGE_PTR(d_o);
+  FORGE_PTR(d_qkv);
+  FORGE_PTR(workspace);
+  FORGE_CHECK((reinterpret_cast<uintptr_t>(seq_lens) & 3u) == 0, FORGE_ERR_ALIGNMENT,
+              "seq_lens is not 4-byte aligned");
+  const WindowArgs a(*cfg, qkv, seq_lens);
+  const size_t rows = (size_t)cfg->batch * cfg->seq * 2;
+  const size_t n = rows * a.ld_qkv, no = rows * cfg->n_heads * cfg->head_dim;
+  FORGE_CHECK(!overlap(d_qkv, n, qkv, n) && !overlap(d_qkv, n, o, no) &&
+                  !overlap(d_qkv, n, d_o, no),
+              FORGE_ERR_INVALID_ARG, "d_qkv overlaps an input");
+  const long hq = (long)cfg->n_heads * cfg->head_dim, hkv = (long)cfg->n_kv_heads * cfg->head_dim;
+  const size_t ds_off = up(2 * (size_t)cfg->batch * cfg->n_heads * cfg->seq * 4);
+  FORGE_HIP(forge::attn_window_bwd(a, o, d_o, lse, static_cast<float*>(workspace),
+                                   at<uint16_t>(workspace, ds_off),
+                                   at<float>(workspace,
+                                             ds_off + up(forge::attn_window_bwd_ds_bytes(a))),
+                                   d_qkv, d_qkv + hq, d_qkv + hq + hkv, a.ld_qkv,
+                                   (hipStream_t)stream));
   return ok();
 }
 

@@ -133,6 +133,32 @@ hipError_t sumsq_finish(const float* partials, float* accum, hipStream_t s);
 hipError_t clip_coeff(const float* norm_sq, float max_norm, float eps, float* scalars,
                       hipStream_t s);
 
+// ----------------------------------------------------------- LayerNorm ----
+hipError_t layernorm_fwd(const uint16_t* x, const uint16_t* g, const uint16_t* b, uint16_t* y,
+                         float* mean, float* rstd, int T, int h, float eps, hipStream_t s);
+// dx (+ resid if non-null), dg and db (db may be null), added to or stored; part:
+// layernorm_bwd_blocks(T, h) * 2 * h floats of scratch. T == 0: dg and db alone.
+int layernorm_bwd_blocks(int T, int h);
+hipError_t layernorm_bwd(const uint16_t* x, const uint16_t* g, const float* mean,
+                         const float* rstd, const uint16_t* dy, const uint16_t* resid,
+                         uint16_t* dx, float* dg, float* db, bool accumulate, float* part, int T,
+                         int h, hipStream_t s);
+
+// ----------------------------------------- rotary positions, several axes ----
+constexpr int kRopeMaxPairs = 256;
+struct RopeFreqs {
+  double w[kRopeMaxPairs];            // angle of pair i per position
+};
+struct RopeAxes {
+  uint32_t axis[kRopeMaxPairs / 16];  // the axis of pair i: bits 2 (i % 16) of word i / 16
+};
+hipError_t rope_axes_table(const RopeFreqs& f, int rows, int d, float* cos_t, float* sin_t,
+                           hipStream_t s);
+// y = x rotated on the first nrot heads of each row (y may be x); pos [axes][T].
+hipError_t rope_axes(const RopeAxes& ax, const uint16_t* x, long ldx, uint16_t* y, long ldy,
+                     const float* cos_t, const float* sin_t, const int32_t* pos, int T, int rows,
+                     int nrot, int d, bool inverse, hipStream_t s);
+
 // ----------------------------------------------------------- attention ----
 struct AttnArgs {
   const uint16_t* q;    // [T, *] rows, head n at column n*d, row stride ld_qkv
@@ -141,9 +167,21 @@ struct AttnArgs {
   long ld_qkv;
   int batch, seq, n_heads, n_kv_heads, d;
   float scale;          // 1/sqrt(d)
+  // (what AttnWindowArgs adds; the causal kernels have no such arguments)
+  static constexpr int window = 0, sinks = 0;
+  static constexpr const int32_t* lens = nullptr;
+};
+// Sliding window: key j is visible to query i iff j <= i and (j > i - window or
+// j < sinks); 1 <= window <= seq, 0 <= sinks <= seq. lens (device int32 [batch],
+// may be NULL): tokens of each batch row, clamped to [0, seq]; the rows behind
+// them are neither read nor visible, and their outputs are zeros (lse -inf).
+struct AttnWindowArgs : AttnArgs {
+  int window, sinks;
+  const int32_t* lens;
 };
 // o [T, n_heads*d] bf16; lse [batch, n_heads, seq] fp32 (natural log).
 hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s);
+hipError_t attn_window_fwd(const AttnWindowArgs& a, uint16_t* o, float* lse, hipStream_t s);
 // Backward. delta: 2 * batch * n_heads * seq fp32 scratch ([b,n,i] =
 // -sum_d dO*O, then [b,n,i] = -lse * log2(e)); ds: attn_bwd_ds_bytes scratch
 // (dS in bf16, the causal half per (batch, head)); part: attn_bwd_part_bytes
@@ -156,6 +194,12 @@ size_t attn_bwd_part_bytes(const AttnArgs& a);
 hipError_t attn_bwd(const AttnArgs& a, const uint16_t* o, const uint16_t* dout, const float* lse,
                     float* delta, uint16_t* ds, float* part, uint16_t* dq, uint16_t* dk,
                     uint16_t* dv, long ld_dqkv, hipStream_t s);
+// The same of a sliding window, its dS a band (and, for the sinks, whole rows).
+size_t attn_window_bwd_ds_bytes(const AttnWindowArgs& a);
+size_t attn_window_bwd_part_bytes(const AttnWindowArgs& a);
+hipError_t attn_window_bwd(const AttnWindowArgs& a, const uint16_t* o, const uint16_t* dout,
+                           const float* lse, float* delta, uint16_t* ds, float* part, uint16_t* dq,
+                           uint16_t* dk, uint16_t* dv, long ld_dqkv, hipStream_t s);
 
 // ----------------------------------------------------------------- MoE ----
 // Routing of fp32 logits [T, E] (E <= 256): idx / gates [T, k], probs [T, E];
