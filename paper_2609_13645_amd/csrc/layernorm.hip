@@ -74,111 +74,161 @@ __global__ __launch_bounds__(256) void layernorm_fwd_k(const bf16_t* __restrict_
   }
 }
 
-// One wave per row, rows strided over the waves of the grid; the workgroup's
-// gain and bias sums go to part [gridDim.x][2][h].
-constexpr int kBwdWaves = 4, kBwdMaxBlocks = 512;
-
-template <int MAXCH>
-__global__ __launch_bounds__(64 * kBwdWaves) void layernorm_bwd_k(
+// A row belongs to WPR waves with CH chunks per lane, so that a row of any width
+// keeps few registers (the columns' shares of dg and db, the row and the next one,
+// whose loads are in flight while this one is reduced); a workgroup's NW / WPR row
+// groups take rows grid-strided and end with their sums in part [gridDim.x][2][h].
+// Bound by HBM: 16384 x 4096, residual included, 103 us for 537 MB (5.2 TB/s; with a
+// wave per row, whose 8 chunks a lane left one row's loads in flight, 233 us).
+// Narrow rows come near the vector units: 12 operations an element, as few as xh by
+// one fma and dx by two leave.
+template <int CH, int WPR, int NW>
+__global__ __launch_bounds__(64 * NW) void layernorm_bwd_k(
     const bf16_t* __restrict__ x, const bf16_t* __restrict__ g, const float* __restrict__ mean,
     const float* __restrict__ rstd, const bf16_t* __restrict__ dy,
     const bf16_t* __restrict__ resid, bf16_t* __restrict__ dx, float* __restrict__ part, int T,
     int h) {
-  __shared__ float red[kBwdWaves][512];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int RG = NW / WPR, LANES = 64 * WPR;
+  __shared__ float2 sums[2][NW];
+  __shared__ float red[RG > 1 ? RG : 1][RG > 1 ? LANES * 8 : 1];
+  const int grp = threadIdx.x / LANES, col = threadIdx.x % LANES;
   const int nch = h / 8;
-  const uint4* gr = reinterpret_cast<const uint4*>(g);
-  float dga[MAXCH][8], dba[MAXCH][8];
+  const float inv_h = 1.0f / (float)h;
+  float w[CH][8], dga[CH][8], dba[CH][8];
 #pragma unroll
-  for (int i = 0; i < MAXCH; ++i)
+  for (int i = 0; i < CH; ++i) {
+    const int c = col + i * LANES;
+    uint4 gv = make_uint4(0, 0, 0, 0);
+    if (c < nch) gv = reinterpret_cast<const uint4*>(g)[c];
+    unpack8(gv, w[i]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dga[i][e] = dba[i][e] = 0.0f;
-
-  for (long row = (long)blockIdx.x * kBwdWaves + wave; row < T;
-       row += (long)gridDim.x * kBwdWaves) {
-    const uint4* xr = reinterpret_cast<const uint4*>(x + row * h);
-    const uint4* dyr = reinterpret_cast<const uint4*>(dy + row * h);
-    const uint4* rr = resid ? reinterpret_cast<const uint4*>(resid + row * h) : nullptr;
-    const float m = mean[row], r = rstd[row];
-    uint4 xv[MAXCH], dv[MAXCH];
-    float s1 = 0.0f, s2 = 0.0f;
+  }
+  struct Row {
+    uint4 x[CH], dy[CH], res[CH];
+    float m, r;
+  };
+  // (a row past the end, and chunks past the width, read as zeros)
+  const auto load = [&](long row) {
+    Row v;
+    const bool ok = row < T;
+    v.m = ok ? mean[row] : 0.0f;
+    v.r = ok ? rstd[row] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < MAXCH; ++i) {
-      const int c = lane + i * 64;
-      if (c < nch) {
-        xv[i] = xr[c];
-        dv[i] = dyr[c];
-        float xf[8], df[8], w[8];
-        unpack8(xv[i], xf);
-        unpack8(dv[i], df);
-        unpack8(gr[c], w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float xh = (xf[e] - m) * r, u = w[e] * df[e];
-          s1 += u;
-          s2 += u * xh;
-          dga[i][e] += df[e] * xh;
-          dba[i][e] += df[e];
-        }
+    for (int i = 0; i < CH; ++i) {
+      const int c = col + i * LANES;
+      const bool in = ok && c < nch;
+      v.x[i] = v.dy[i] = v.res[i] = make_uint4(0, 0, 0, 0);
+      if (in) {
+        v.x[i] = reinterpret_cast<const uint4*>(x + row * h)[c];
+        v.dy[i] = reinterpret_cast<const uint4*>(dy + row * h)[c];
+        if (resid) v.res[i] = reinterpret_cast<const uint4*>(resid + row * h)[c];
       }
     }
-    const float c1 = wave_sum(s1) / (float)h, c2 = wave_sum(s2) / (float)h;
-    uint4* dxr = reinterpret_cast<uint4*>(dx + row * h);
+    return v;
+  };
+  const long step = (long)gridDim.x * RG;
+  int buf = 0;
+  long row = (long)blockIdx.x * RG + grp;
+  Row v = load(row);
+  // (every wave of a workgroup makes the same number of turns: the barriers)
+  for (long base = (long)blockIdx.x * RG; base < T; base += step, row += step) {
+    const Row next = load(row + step);
+    // xh as one fma each: m r is off by 2^-24 |m| r, as x - m is by m's rounding
+    float xh[CH][8], u[CH][8], s1 = 0.0f, s2 = 0.0f;
+    const float mr = -v.m * v.r;
 #pragma unroll
-    for (int i = 0; i < MAXCH; ++i) {
-      const int c = lane + i * 64;
-      if (c < nch) {
-        float xf[8], df[8], w[8], o[8];
-        unpack8(xv[i], xf);
-        unpack8(dv[i], df);
-        unpack8(gr[c], w);
+    for (int i = 0; i < CH; ++i) {
+      float df[8];
+      unpack8(v.x[i], xh[i]);
+      unpack8(v.dy[i], df);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        xh[i][e] = __builtin_fmaf(xh[i][e], v.r, mr);
+        u[i][e] = w[i][e] * df[e];
+        s1 += u[i][e];
+        s2 = __builtin_fmaf(u[i][e], xh[i][e], s2);
+        dga[i][e] = __builtin_fmaf(df[e], xh[i][e], dga[i][e]);
+        dba[i][e] += df[e];
+      }
+    }
+    s1 = wave_sum(s1);
+    s2 = wave_sum(s2);
+    if constexpr (WPR > 1) {
+      if ((threadIdx.x & 63) == 0) sums[buf][threadIdx.x >> 6] = make_float2(s1, s2);
+      __syncthreads();
+      s1 = s2 = 0.0f;
+#pragma unroll
+      for (int k = 0; k < WPR; ++k) {
+        const float2 t = sums[buf][grp * WPR + k];
+        s1 += t.x;
+        s2 += t.y;
+      }
+      buf ^= 1;
+    }
+    const float c1 = -s1 * inv_h * v.r, c2 = -s2 * inv_h * v.r;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = col + i * LANES;
+      if (row < T && c < nch) {
+        float o[8];
+        unpack8(v.res[i], o);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          o[e] = r * (w[e] * df[e] - c1 - (xf[e] - m) * r * c2);
-        if (rr) {
-          float rf[8];
-          unpack8(rr[c], rf);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += rf[e];
-        }
-        dxr[c] = pack8(o);
+          o[e] = __builtin_fmaf(u[i][e], v.r, __builtin_fmaf(xh[i][e], c2, c1)) + o[e];
+        reinterpret_cast<uint4*>(dx + row * h)[c] = pack8(o);
       }
     }
+    v = next;
   }
-  float* pg = part + (long)blockIdx.x * 2 * h;
+  float* out = part + (long)blockIdx.x * 2 * h;
 #pragma unroll
-  for (int i = 0; i < MAXCH; ++i)
+  for (int i = 0; i < CH; ++i)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
+      float a[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) red[wave][lane * 8 + e] = k ? dba[i][e] : dga[i][e];
-      __syncthreads();
-      for (int j = threadIdx.x; j < 512; j += 64 * kBwdWaves) {
-        if (i * 512 + j < h) {
-          float s = 0.0f;
-#pragma unroll
-          for (int w = 0; w < kBwdWaves; ++w) s += red[w][j];
-          pg[k * h + i * 512 + j] = s;
+      for (int e = 0; e < 8; ++e) a[e] = k ? dba[i][e] : dga[i][e];
+      if constexpr (RG == 1) {
+        const int c = col + i * LANES;
+        if (c < nch) {
+          float4* p = reinterpret_cast<float4*>(out + k * h + c * 8);
+          p[0] = make_float4(a[0], a[1], a[2], a[3]);
+          p[1] = make_float4(a[4], a[5], a[6], a[7]);
         }
+      } else {
+        float4* p = reinterpret_cast<float4*>(&red[grp][col * 8]);
+        p[0] = make_float4(a[0], a[1], a[2], a[3]);
+        p[1] = make_float4(a[4], a[5], a[6], a[7]);
+        __syncthreads();
+        for (int j = threadIdx.x; j < LANES * 8; j += 64 * NW) {
+          if (i * LANES * 8 + j < h) {
+            float s = 0.0f;
+#pragma unroll
+            for (int q = 0; q < RG; ++q) s += red[q][j];
+            out[k * h + i * LANES * 8 + j] = s;
+          }
+        }
+        __syncthreads();
       }
-      __syncthreads();
     }
 }
 
 // dg[c] (and db[c], grid.y 1) = or += the sum over the workgroups' partial rows:
-// 64 columns per workgroup, 16 stripes of 16-byte loads, stripe sums added in order.
+// 64 columns per workgroup, 64 stripes of 16-byte loads, stripe sums added in order.
 template <bool ACC>
-__global__ __launch_bounds__(256) void layernorm_grad_sum_k(const float* __restrict__ part,
-                                                            int nblk, float* __restrict__ dg,
-                                                            float* __restrict__ db, int h) {
-  __shared__ float4 red[16][16];
+__global__ __launch_bounds__(1024) void layernorm_grad_sum_k(const float* __restrict__ part,
+                                                             int nblk, float* __restrict__ dg,
+                                                             float* __restrict__ db, int h) {
+  __shared__ float4 red[64][16];
+  __shared__ float quarter[4][64];
   const int cg = threadIdx.x & 15, stripe = threadIdx.x >> 4;
   const int col = blockIdx.x * 64 + cg * 4;
   const float* src = part + (long)blockIdx.y * h;
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   if (col < h) {
 #pragma unroll 8
-    for (int b = stripe; b < nblk; b += 16) {
+    for (int b = stripe; b < nblk; b += 64) {
       const float4 v = *reinterpret_cast<const float4*>(src + (long)b * 2 * h + col);
       s.x += v.x;
       s.y += v.y;
@@ -188,12 +238,19 @@ __global__ __launch_bounds__(256) void layernorm_grad_sum_k(const float* __restr
   }
   red[stripe][cg] = s;
   __syncthreads();
-  const int c = blockIdx.x * 64 + threadIdx.x;
-  if (threadIdx.x < 64 && c < h) {
-    const float* rf = reinterpret_cast<const float*>(red);
+  if (threadIdx.x < 256) {
+    const int c = threadIdx.x & 63, q = threadIdx.x >> 6;
+    const float* rf = reinterpret_cast<const float*>(&red[q * 16][0]);
     float t = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) t += rf[w * 64 + threadIdx.x];
+    for (int w = 0; w < 16; ++w) t += rf[w * 64 + c];
+    quarter[q][c] = t;
+  }
+  __syncthreads();
+  const int c = blockIdx.x * 64 + threadIdx.x;
+  if (threadIdx.x < 64 && c < h) {
+    const float t = (quarter[0][threadIdx.x] + quarter[1][threadIdx.x]) +
+                    (quarter[2][threadIdx.x] + quarter[3][threadIdx.x]);
     float* out = blockIdx.y ? db : dg;
     out[c] = ACC ? out[c] + t : t;
   }
@@ -217,8 +274,18 @@ hipError_t layernorm_fwd(const uint16_t* x, const uint16_t* g, const uint16_t* b
   return hipGetLastError();
 }
 
+namespace {
+// Eight waves a workgroup and one workgroup a CU: enough loads in flight for the
+// HBM's rate, and no more partial rows to write and add than CUs (16384 x 4096 with
+// resid: 192 workgroups 114 us, 256 103, 512 108; 999 x 2056: 256 12.5 us, 500 19).
+constexpr int kBwdWaves = 8, kBwdMaxBlocks = 256;
+// Waves of a row, two chunks of 512 columns each.
+int row_waves(int h) { return h <= 1024 ? 1 : h <= 2048 ? 2 : h <= 4096 ? 4 : 8; }
+}  // namespace
+
 int layernorm_bwd_blocks(int T, int h) {
-  const long need = ((long)T + kBwdWaves - 1) / kBwdWaves;
+  const int groups = kBwdWaves / row_waves(h);
+  const long need = ((long)T + groups - 1) / groups;
   return need < kBwdMaxBlocks ? (int)need : kBwdMaxBlocks;
 }
 
@@ -229,23 +296,22 @@ hipError_t layernorm_bwd(const uint16_t* x, const uint16_t* g, const float* mean
   const int nblk = T > 0 ? layernorm_bwd_blocks(T, h) : 0;
   if (nblk > 0) {
     const dim3 grid(nblk), block(64 * kBwdWaves);
-    const int ch = (h / 8 + 63) / 64;
-#define FORGE_LNB(N)                                                                       \
-  hipLaunchKernelGGL(layernorm_bwd_k<N>, grid, block, 0, s, x, g, mean, rstd, dy, resid, dx, \
-                     part, T, h)
-    if (ch <= 1) FORGE_LNB(1);
-    else if (ch <= 2) FORGE_LNB(2);
-    else if (ch <= 4) FORGE_LNB(4);
-    else if (ch <= 8) FORGE_LNB(8);
-    else if (ch <= 16) FORGE_LNB(16);
+#define FORGE_LNB(CH, WPR)                                                                     \
+  hipLaunchKernelGGL((layernorm_bwd_k<CH, WPR, kBwdWaves>), grid, block, 0, s, x, g, mean, rstd, \
+                     dy, resid, dx, part, T, h)
+    if (h <= 512) FORGE_LNB(1, 1);
+    else if (h <= 1024) FORGE_LNB(2, 1);
+    else if (h <= 2048) FORGE_LNB(2, 2);
+    else if (h <= 4096) FORGE_LNB(2, 4);
+    else if (h <= 8192) FORGE_LNB(2, 8);
     else return hipErrorInvalidValue;
 #undef FORGE_LNB
   }
   const dim3 sgrid((h + 63) / 64, db ? 2 : 1);
   if (accumulate)
-    hipLaunchKernelGGL(layernorm_grad_sum_k<true>, sgrid, dim3(256), 0, s, part, nblk, dg, db, h);
+    hipLaunchKernelGGL(layernorm_grad_sum_k<true>, sgrid, dim3(1024), 0, s, part, nblk, dg, db, h);
   else
-    hipLaunchKernelGGL(layernorm_grad_sum_k<false>, sgrid, dim3(256), 0, s, part, nblk, dg, db, h);
+    hipLaunchKernelGGL(layernorm_grad_sum_k<false>, sgrid, dim3(1024), 0, s, part, nblk, dg, db, h);
   return hipGetLastError();
 }
 
