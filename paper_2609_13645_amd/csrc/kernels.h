@@ -151,6 +151,7 @@ struct RopeFreqs {
 };
 struct RopeAxes {
   uint32_t axis[kRopeMaxPairs / 16];  // the axis of pair i: bits 2 (i % 16) of word i / 16
+  int at(int i) const { return axis[i / 16] >> 2 * (i % 16) & 3; }
 };
 hipError_t rope_axes_table(const RopeFreqs& f, int rows, int d, float* cos_t, float* sin_t,
                            hipStream_t s);
