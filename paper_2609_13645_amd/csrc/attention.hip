@@ -25,6 +25,7 @@
 // in the log2 domain (scale * log2 e folded into one multiply); the causal
 // mask is evaluated only on tiles that straddle the diagonal, and waves whose
 // rows are fully masked skip their MFMAs.
+#include <algorithm>
 #include <type_traits>
 #include <utility>
 
@@ -163,6 +164,12 @@ __device__ __forceinline__ int row_len(const AttnWindowArgs& a, int b) {
 // The rows of a batch row, of which `len` are its tokens.
 __device__ __forceinline__ int seq_of(const AttnArgs&, int len) { return len; }
 __device__ __forceinline__ int seq_of(const AttnWindowArgs& a, int) { return a.seq; }
+// Block id of the dispatcher's round robin over 8 XCDs -> position in an order of n
+// of which each XCD takes one contiguous part.
+__device__ __forceinline__ int xcd_order(int id, int n) {
+  const int x = id % 8;
+  return x * (n / 8) + min(x, n % 8) + id / 8;
+}
 struct WindowTiles {
   int sinks, skip, count;   // sink tiles before the window, tiles between, tiles in all
   // queries [q0, end) with key tiles of 64
@@ -304,8 +311,17 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
   const int id = (int)blockIdx.x;
   const int level = id / W, r = id % W;
   const int L = (W % 8 == 0) ? (r % 8) * (W / 8) + r / 8 : r;
-  const int qt = nqt - 1 - level;
-  const int n = L % a.n_heads, b = L / a.n_heads;
+  int qt = nqt - 1 - level, n = L % a.n_heads, b = L / a.n_heads;
+  if constexpr (WIN) {
+    // WIN: blocks are about alike but for the first; each XCD takes neighbouring
+    // query tiles of one kv head (its query heads side by side), whose windows overlap
+    const int grp = a.n_heads / a.n_kv_heads;
+    const int i = xcd_order(id, nqt * W);
+    const int t = i / grp / a.batch;
+    b = i / grp % a.batch;
+    qt = nqt - 1 - t % nqt;
+    n = t / nqt * grp + i % grp;
+  }
   const int m = n / (a.n_heads / a.n_kv_heads);
   const int E = WIN ? row_len(a, b) : S;   // end of the batch row's tokens
   const long rb = (long)b * S;
@@ -407,7 +423,21 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
   // max, the lazy rescale; returns -running max (log2 units)
   auto softmax_head = [&](f32x16_t (&s)[2], int j) __attribute__((always_inline)) {
     const int k0 = tile_of(j) * BKV;
-    if (k0 + BKV - 1 > q0w) {
+    if constexpr (WIN) {
+      // (and of one that the window's far edge crosses: the keys a query sees are a
+      // range, one subtraction and one comparison each, and the sinks)
+      if (k0 + BKV - 1 > q0w || (k0 <= q0w + 31 - a.window && k0 + BKV - 1 >= a.sinks)) {
+        const int lo = q - a.window + 1 - k0 - hh * 4;
+        const int sink = min(a.sinks, q + 1) - k0 - hh * 4;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = kb * 32 + (i >> 2) * 8 + (i & 3);
+            if ((unsigned)(key - lo) >= (unsigned)a.window && key >= sink) s[kb][i] = -INFINITY;
+          }
+      }
+    } else if (k0 + BKV - 1 > q0w) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -415,19 +445,6 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
           const int key = k0 + kb * 32 + (i >> 2) * 8 + hh * 4 + (i & 3);
           if (key > q) s[kb][i] = -INFINITY;
         }
-    }
-    if constexpr (WIN) {
-      // the same of a tile that the window's far edge crosses
-      if (k0 <= q0w + 31 - a.window && k0 + BKV - 1 >= a.sinks) {
-        const int far = q - a.window - k0 - hh * 4, sink = a.sinks - k0 - hh * 4;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = kb * 32 + (i >> 2) * 8 + (i & 3);
-            if (key <= far && key >= sink) s[kb][i] = -INFINITY;
-          }
-      }
     }
     // two running-max chains over the lane's 32 scores (the compiler forms
     // v_max3 without quieting every operand first)
@@ -713,6 +730,56 @@ struct KvBlock {
     z = r / a.n_kv_heads / a.batch;
   }
 };
+__device__ __forceinline__ KvBlock kv_block(const AttnArgs& a, int splits) {
+  return KvBlock(a, splits);
+}
+// WIN: first, where the slabs behind the sink tiles' own windows are cut into
+// chunks, a block for each chunk (a sink tile sees every later query: one block
+// for all of them would run long after the others); then the key tiles' splits.
+// Either in an order that gives each XCD neighbouring tiles of one kv head, whose
+// windows overlap. A sink tile's blocks leave their sums in slots of their own:
+// the splits, then the chunks.
+struct KvWindowBlock {
+  int kt, b, m, z, step;   // pairs z, z + step, .. (times four waves)
+  int slot;                // of the sink partials, -1: not there
+  int j0, ns, len;         // slabs of the block; tokens of the batch row
+  __device__ __forceinline__ KvWindowBlock(const AttnWindowArgs& a, int splits) {
+    const DsWindow L(a);
+    const int nkt = (a.seq + 63) / 64, bm = a.batch * a.n_kv_heads;
+    const int far = L.nst * a.sink_chunks * bm;
+    int id = (int)blockIdx.x, chunk = -1, r;
+    if (id < far) {
+      id = xcd_order(id, far);
+      r = id / a.batch;
+      chunk = r % a.sink_chunks;
+      kt = r / a.sink_chunks % L.nst;
+      m = r / a.sink_chunks / L.nst;
+      z = 0;
+      step = 1;
+    } else {
+      id = xcd_order(id - far, nkt * splits * bm);
+      r = id / a.batch;
+      z = r % splits;
+      kt = r / splits % nkt;
+      m = r / splits / nkt;
+      step = splits;
+    }
+    b = id % a.batch;
+    len = row_len(a, b);
+    slot = a.sink_chunks > 0 && kt < L.nst ? (chunk < 0 ? z : splits + chunk) : -1;
+    const int end = (len + 31) / 32;
+    j0 = 2 * kt;
+    int last = kt < L.nst && a.sink_chunks == 0 ? end : j0 + L.nwin;
+    if (chunk >= 0) {
+      j0 = last + chunk * a.chunk_slabs;
+      last = j0 + a.chunk_slabs;
+    }
+    ns = max(0, min(last, end) - j0);
+  }
+};
+__device__ __forceinline__ KvWindowBlock kv_block(const AttnWindowArgs& a, int splits) {
+  return KvWindowBlock(a, splits);
+}
 // s_waitcnt immediate that waits for vmcnt <= n only (gfx9 encoding: vmcnt
 // bits 3:0 and 15:14, expcnt 6:4 and lgkmcnt 11:8 at their maxima)
 constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
@@ -725,6 +792,20 @@ __device__ __forceinline__ float* kv_part(const AttnArgs& a, float* part, const 
   if (!part) return nullptr;
   const long T = (long)a.batch * a.seq;
   return part + ((k.z * T + row) * a.n_kv_heads + k.m) * D;
+}
+
+// WIN: the same, or the rows of the block's slot of a sink tile's partial sums
+// [slots][batch][sink rows][n_kv * D].
+template <int D>
+__device__ __forceinline__ float* kv_part(const AttnWindowArgs& a, float* part, float* sink_part,
+                                          const KvWindowBlock& k) {
+  const long width = (long)a.n_kv_heads * D;
+  if (k.slot >= 0) {
+    const int rows = (a.sinks + 63) / 64 * 64;
+    return sink_part + (((long)k.slot * a.batch + k.b) * rows + k.kt * 64) * width + k.m * D;
+  }
+  if (!part) return nullptr;
+  return part + (((long)k.z * a.batch + k.b) * a.seq + k.kt * 64) * width + k.m * D;
 }
 
 // One DMA instruction: 16 bytes per lane from a buffer of `bytes` bytes (zeros
@@ -863,16 +944,18 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   const int grp = a.n_heads / a.n_kv_heads;
   // block order: key tile slowest, so the low key tiles (the most work)
   // are dispatched first
-  const KvBlock kb_(a, splits);
+  const auto kb_ = kv_block(a, splits);
   const int kt = kb_.kt, m = kb_.m, b = kb_.b;
   const int k0 = kt * BK;
-  if constexpr (WIN) S = row_len(a, b);
-  const int j0 = k0 / BQ;                      // first slab holding a query >= k0
-  // slabs per query head (WIN: those that see the keys, none without tokens)
-  int ns = (S + BQ - 1) / BQ - j0;
   if constexpr (WIN) {
-    const DsWindow L(a);
-    ns = max(0, kt < L.nst ? ns : min(ns, L.nwin));
+    S = kb_.len;
+    splits = kb_.step;
+  }
+  int j0 = k0 / BQ;                            // first slab holding a query >= k0
+  int ns = (S + BQ - 1) / BQ - j0;             // slabs per query head
+  if constexpr (WIN) {
+    j0 = kb_.j0;
+    ns = kb_.ns;
   }
   const int total = grp * ns;
   const int lane = threadIdx.x & 63;
@@ -1175,8 +1258,24 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
         // causal mask and sequence tail (diagonal and last slabs only), once S
         // is complete: -inf scores, so exp2 gives 0
         if constexpr (i == KK && kb == 0) {
-          // (WIN: and where the window's far edge crosses the block)
-          if (q0 < k0 + BK - 1 || q0 + BQ > S) {
+          if constexpr (WIN) {
+            // (and where the window's far edge crosses the block: the queries that see
+            // a key are a range, one subtraction and one comparison each)
+            if (q0 < k0 + BK - 1 || q0 + BQ > S ||
+                (k0 <= q0 + BQ - 1 - a.window && k0 + BK - 1 >= a.sinks)) {
+#pragma unroll
+              for (int mb = 0; mb < 2; ++mb) {
+                const int key = k0 + mb * 32 + l32;
+                const int end = key < a.sinks ? S : min(S, key + a.window);
+                const int lo = key - q0 - hh * 4, n = max(0, end - key);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const int q = (e >> 2) * 8 + (e & 3);
+                  if ((unsigned)(q - lo) >= (unsigned)n) sc[mb][e] = -INFINITY;
+                }
+              }
+            }
+          } else if (q0 < k0 + BK - 1 || q0 + BQ > S) {
 #pragma unroll
             for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
@@ -1184,17 +1283,6 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
                 const int q = q0 + (e >> 2) * 8 + hh * 4 + (e & 3);
                 if (k0 + mb * 32 + l32 > q || q >= S) sc[mb][e] = -INFINITY;
               }
-          }
-          if constexpr (WIN) {
-            if (k0 <= q0 + BQ - 1 - a.window && k0 + BK - 1 >= a.sinks) {
-#pragma unroll
-              for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const int q = q0 + (e >> 2) * 8 + hh * 4 + (e & 3), key = k0 + mb * 32 + l32;
-                  if (key <= q - a.window && key >= a.sinks) sc[mb][e] = -INFINITY;
-                }
-            }
           }
         }
         under(fa::ic<2 * i + kb>{});
@@ -1218,24 +1306,36 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
     cur ^= 1;
   }
   if (dsblk) store_ds();
+  float *tv, *tk;
+  if constexpr (WIN) {
+    tv = kv_part<D>(a, pv, a.sink_pv, kb_);
+    tk = kv_part<D>(a, pk, a.sink_pk, kb_);
+  } else {
+    tv = kv_part<D>(a, pv, kb_, rb + k0);
+    tk = kv_part<D>(a, pk, kb_, rb + k0);
+  }
   kv_reduce_store<D>(acc, sm, sm + 2 * P::RED, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D,
-                     ld_d, kv_part<D>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D, seq_of(a, S) - k0);
+                     ld_d, tv, (long)a.n_kv_heads * D, seq_of(a, S) - k0);
   kv_reduce_store<D>(acck, sm, sm + 2 * P::RED, wave, lane, a.scale,
-                     dk + (rb + k0) * ld_d + (long)m * D, ld_d,
-                     kv_part<D>(a, pk, kb_, rb + k0), (long)a.n_kv_heads * D, seq_of(a, S) - k0);
+                     dk + (rb + k0) * ld_d + (long)m * D, ld_d, tk, (long)a.n_kv_heads * D,
+                     seq_of(a, S) - k0);
 }
 
 // dK and dV from the splits' partial sums, added in split order; eight columns
 // per thread, grid.y 0: dK (times scale), 1: dV.
+// (WIN: but for the first `skip` of every `seq` rows, those of sink tiles.)
+template <bool WIN>
 __global__ __launch_bounds__(256) void attn_bwd_kv_sum_k(const float* __restrict__ pk,
                                                          const float* __restrict__ pv, int splits,
                                                          long rows, int width, float scale,
                                                          bf16_t* __restrict__ dk,
-                                                         bf16_t* __restrict__ dv, long ld_d) {
+                                                         bf16_t* __restrict__ dv, long ld_d,
+                                                         int seq, int skip) {
   const int cpr = width / 8;
   const long q = (long)blockIdx.x * 256 + threadIdx.x;
   if (q >= rows * cpr) return;
   const long r = q / cpr;
+  if (WIN && r % seq < skip) return;
   const int c = (int)(q % cpr) * 8;
   const bool v = blockIdx.y != 0;
   const float* src = (v ? pv : pk) + r * width + c;
@@ -1251,6 +1351,48 @@ __global__ __launch_bounds__(256) void attn_bwd_kv_sum_k(const float* __restrict
   const float f[8] = {x[0] * sc, x[1] * sc, x[2] * sc, x[3] * sc,
                       y[0] * sc, y[1] * sc, y[2] * sc, y[3] * sc};
   *reinterpret_cast<uint4*>((v ? dv : dk) + r * ld_d + c) = pack8(f);
+}
+
+// WIN: dK and dV of the sink tiles' rows, the sums of their slots (splits, then
+// chunks). A workgroup takes 128 columns of a row: 16 lanes of eight columns, 16
+// stripes of slots, whose sums are added in order.
+__global__ __launch_bounds__(256) void attn_window_sink_sum_k(AttnWindowArgs a, int slots,
+                                                              int width, bf16_t* __restrict__ dk,
+                                                              bf16_t* __restrict__ dv, long ld_d) {
+  __shared__ float red[16][16][8];
+  const int cg = threadIdx.x & 15, stripe = threadIdx.x >> 4;
+  const int rows = (a.sinks + 63) / 64 * 64, mine = min(rows, a.seq);
+  const int pieces = (width + 127) / 128;
+  const int piece = (int)blockIdx.x % pieces, row = (int)blockIdx.x / pieces % mine;
+  const int b = (int)blockIdx.x / pieces / mine, col = piece * 128 + cg * 8;
+  const bool v = blockIdx.y != 0;
+  f32x4_t x = {}, y = {};
+  if (col < width) {
+    const float* src = (v ? a.sink_pv : a.sink_pk) + ((long)b * rows + row) * width + col;
+#pragma unroll 4
+    for (int z = stripe; z < slots; z += 16) {
+      const float* p = src + (long)z * a.batch * rows * width;
+      x += *reinterpret_cast<const f32x4_t*>(p);
+      y += *reinterpret_cast<const f32x4_t*>(p + 4);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    red[stripe][cg][e] = x[e];
+    red[stripe][cg][4 + e] = y[e];
+  }
+  __syncthreads();
+  if (stripe == 0 && col < width) {
+    const float sc = v ? 1.0f : a.scale;
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      f[e] = 0.0f;
+      for (int k = 0; k < 16; ++k) f[e] += red[k][cg][e];
+      f[e] *= sc;
+    }
+    *reinterpret_cast<uint4*>((v ? dv : dk) + ((long)b * a.seq + row) * ld_d + col) = pack8(f);
+  }
 }
 
 // 4. dQ: block of 256 queries (32 per wave, eight waves) of one (batch,
@@ -1286,10 +1428,19 @@ __global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(Args a, const bf16_t* __
   // head within its group, batch, and query tile, largest first
   const int grp = a.n_heads / a.n_kv_heads;
   const int id = (int)blockIdx.x;
-  const int m = id % a.n_kv_heads;
-  const int n = m * grp + id / a.n_kv_heads % grp;
-  const int b = id / a.n_kv_heads / grp % a.batch;
-  const int qt = nqt - 1 - id / (a.n_kv_heads * grp * a.batch);
+  int m = id % a.n_kv_heads;
+  int n = m * grp + id / a.n_kv_heads % grp;
+  int b = id / a.n_kv_heads / grp % a.batch;
+  int qt = nqt - 1 - id / (a.n_kv_heads * grp * a.batch);
+  if constexpr (WIN) {
+    // WIN: as in the forward
+    const int i = xcd_order(id, nqt * a.n_heads * a.batch);
+    const int t = i / grp / a.batch;
+    b = i / grp % a.batch;
+    qt = nqt - 1 - t % nqt;
+    m = t / nqt;
+    n = m * grp + i % grp;
+  }
   const long rb = (long)b * S;
   const int E = WIN ? row_len(a, b) : S;   // end of the batch row's tokens
   const auto L = ds_layout(a);
@@ -1511,31 +1662,134 @@ size_t attn_bwd_part_bytes(const AttnArgs& a) {
   return z > 1 ? (size_t)2 * z * a.batch * a.seq * a.n_kv_heads * a.d * 4 : 0;
 }
 
-static int kv_splits(const AttnWindowArgs&) { return 1; }
-size_t attn_window_bwd_part_bytes(const AttnWindowArgs&) { return 0; }
+// The same estimate for a sliding window, over the splits of a key tile's pairs and
+// the chunks of what the sink tiles see behind their own windows (0 chunks: the sink
+// tiles' own blocks take it).
+struct WindowPlan {
+  int splits, chunks, slabs;   // slabs of a chunk
+  size_t part, sink;           // floats of partial sums (dK or dV): of the splits, of the sinks
+};
+static WindowPlan window_plan(const AttnWindowArgs& a) {
+  constexpr double kCUs = 256.0, kLaunchUs = 2.0, kPartBytesPerUs = 3.6e6;
+  const double kPairUs = a.d == 128 ? 1.02 : 0.66, kBlockUs = a.d == 128 ? 3.2 : 6.4;
+  const DsWindow L(a);
+  const long grp = a.n_heads / a.n_kv_heads, bm = (long)a.batch * a.n_kv_heads;
+  const long nkt = (a.seq + 63) / 64, pairs = grp * L.nwin, far = L.nst > 0 ? L.ns - L.nwin : 0;
+  const double width = (double)a.n_kv_heads * a.d;
+  const auto block_us = [&](long n) { return kBlockUs + kPairUs * (double)((n + 3) / 4); };
+  WindowPlan best{};
+  double cost = 0.0;
+  for (int z = 1; z <= 16; ++z) {
+    if (z > 1 && (z * 8 > pairs || (z - 1) * nkt * bm >= 512)) break;
+    for (const int c : {0, 1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (c > 0 && far < c) break;
+      const double tile = block_us((pairs + z - 1) / z);
+      double longest = tile, all = tile * (double)(nkt * z), extra = 0.0;
+      if (c == 0 && far > 0) {
+        longest = block_us((grp * L.ns + z - 1) / z);
+        all += (longest - tile) * (double)(L.nst * z);
+      } else if (c > 0) {
+        const double chunk = block_us(grp * ((far + c - 1) / c));
+        longest = std::max(longest, chunk);
+        all += chunk * (double)(L.nst * c);
+        extra += kLaunchUs + 2.0 * (z + c) * a.batch * L.nst * 64 * width * 8.0 / kPartBytesPerUs;
+      }
+      if (z > 1) extra += kLaunchUs + (z + 1.0) * a.batch * a.seq * width * 8.0 / kPartBytesPerUs;
+      const double t = std::max(longest, all * (double)bm / kCUs) + extra;
+      if ((z == 1 && c == 0) || t < cost) {
+        cost = t;
+        best.splits = z;
+        best.chunks = c;
+      }
+    }
+  }
+  if (best.chunks > 0) {
+    best.slabs = (int)((far + best.chunks - 1) / best.chunks);
+    best.sink = (size_t)(best.splits + best.chunks) * a.batch * L.nst * 64 * a.n_kv_heads * a.d;
+  }
+  if (best.splits > 1)
+    best.part = (size_t)best.splits * a.batch * a.seq * a.n_kv_heads * a.d;
+  return best;
+}
+size_t attn_window_bwd_part_bytes(const AttnWindowArgs& a) {
+  const WindowPlan p = window_plan(a);
+  return 2 * (p.part + p.sink) * 4;
+}
 
 namespace {
+// How the kv pass divides its pairs, and where its partial sums lie in `part`.
+template <int D>
+struct KvLaunch {
+  int splits, blocks;
+  float *pk = nullptr, *pv = nullptr;
+  KvLaunch(AttnArgs& a, float* part) {
+    splits = kv_splits(a);
+    blocks = (a.seq + 63) / 64 * a.n_kv_heads * a.batch * splits;
+    if (splits > 1) {
+      pk = part;
+      pv = part + (long)splits * a.batch * a.seq * a.n_kv_heads * D;
+    }
+  }
+  KvLaunch(AttnWindowArgs& a, float* part) {
+    const WindowPlan p = window_plan(a);
+    splits = p.splits;
+    const int nst = (a.sinks + 63) / 64, bm = a.n_kv_heads * a.batch;
+    blocks = ((a.seq + 63) / 64 * splits + nst * p.chunks) * bm;
+    if (p.part) {
+      pk = part;
+      pv = part + p.part;
+    }
+    a.sink_chunks = p.chunks;
+    a.chunk_slabs = p.slabs;
+    a.sink_pk = part + 2 * p.part;
+    a.sink_pv = a.sink_pk + p.sink;
+  }
+};
+
+// dK and dV from the partial sums of the splits and, of sink tiles, the chunks.
+template <int D>
+void kv_sums(const AttnArgs& a, const KvLaunch<D>& k, uint16_t* dk, uint16_t* dv, long ld_d,
+             hipStream_t s) {
+  if (k.splits <= 1) return;
+  const long T = (long)a.batch * a.seq;
+  const int width = a.n_kv_heads * D;
+  const dim3 grid((unsigned)((T * (width / 8) + 255) / 256), 2);
+  hipLaunchKernelGGL(attn_bwd_kv_sum_k<false>, grid, dim3(256), 0, s, k.pk, k.pv, k.splits, T,
+                     width, a.scale, dk, dv, ld_d, a.seq, 0);
+}
+template <int D>
+void kv_sums(const AttnWindowArgs& a, const KvLaunch<D>& k, uint16_t* dk, uint16_t* dv, long ld_d,
+             hipStream_t s) {
+  const long T = (long)a.batch * a.seq;
+  const int width = a.n_kv_heads * D;
+  const int rows = a.sink_chunks > 0 ? (a.sinks + 63) / 64 * 64 : 0;
+  if (k.splits > 1) {
+    const dim3 grid((unsigned)((T * (width / 8) + 255) / 256), 2);
+    hipLaunchKernelGGL(attn_bwd_kv_sum_k<true>, grid, dim3(256), 0, s, k.pk, k.pv, k.splits, T,
+                       width, a.scale, dk, dv, ld_d, a.seq, rows);
+  }
+  if (rows > 0) {
+    const dim3 grid((unsigned)(std::min(rows, a.seq) * a.batch * ((width + 127) / 128)), 2);
+    hipLaunchKernelGGL(attn_window_sink_sum_k, grid, dim3(256), 0, s, a, k.splits + a.sink_chunks,
+                       width, dk, dv, ld_d);
+  }
+}
+
 template <int D, typename Args>
-hipError_t attn_bwd_d(const Args& a, const uint16_t* o, const uint16_t* dout, const float* lse,
+hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const float* lse,
                       float* delta, uint16_t* ds, float* part, uint16_t* dq, uint16_t* dk,
                       uint16_t* dv, long ld_d, hipStream_t s) {
-  const long T = (long)a.batch * a.seq, rows = T * a.n_heads;
-  const int z = kv_splits(a), width = a.n_kv_heads * D;
-  float* pk = z > 1 ? part : nullptr;
-  float* pv = z > 1 ? part + (long)z * T * width : nullptr;
+  const long rows = (long)a.batch * a.seq * a.n_heads;
+  const KvLaunch<D> k(a, part);
   const dim3 block(256);
   const dim3 pgrid((unsigned)((rows + 2048 / D - 1) / (2048 / D)));
-  const dim3 kgrid((unsigned)((long)((a.seq + 63) / 64) * a.n_kv_heads * a.batch * z));
+  const dim3 kgrid((unsigned)k.blocks);
   const dim3 qgrid((unsigned)((a.seq + 255) / 256 * a.n_heads * a.batch));
   hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
                      a.seq);
-  hipLaunchKernelGGL((attn_bwd_kv_k<D, Args>), kgrid, block, 0, s, a, dout, delta, ds, dv, dk, ld_d, pv, pk,
-                     z);
-  if (z > 1) {
-    const dim3 sgrid((unsigned)((T * (width / 8) + 255) / 256), 2);
-    hipLaunchKernelGGL(attn_bwd_kv_sum_k, sgrid, block, 0, s, pk, pv, z, T, width, a.scale, dk, dv,
-                       ld_d);
-  }
+  hipLaunchKernelGGL((attn_bwd_kv_k<D, Args>), kgrid, block, 0, s, a, dout, delta, ds, dv, dk, ld_d,
+                     k.pv, k.pk, k.splits);
+  kv_sums<D>(a, k, dk, dv, ld_d, s);
   hipLaunchKernelGGL((attn_bwd_dq_k<D, Args>), qgrid, dim3(512), 0, s, a, ds, dq, ld_d);
   return hipGetLastError();
 }
