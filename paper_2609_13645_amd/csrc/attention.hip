@@ -743,6 +743,7 @@ struct KvWindowBlock {
   int kt, b, m, z, step;   // pairs z, z + step, .. (times four waves)
   int slot;                // of the sink partials, -1: not there
   int j0, ns, len;         // slabs of the block; tokens of the batch row
+  int turn;                // the first slab walked is j0 + turn - 1 (0: j0 + ns - 1)
   __device__ __forceinline__ KvWindowBlock(const AttnWindowArgs& a, int splits) {
     const DsWindow L(a);
     const int nkt = (a.seq + 63) / 64, bm = a.batch * a.n_kv_heads;
@@ -775,6 +776,8 @@ struct KvWindowBlock {
       last = j0 + a.chunk_slabs;
     }
     ns = max(0, min(last, end) - j0);
+    turn = a.go_round ? (L.nwin - j0 % L.nwin) % L.nwin : 0;
+    if (turn >= ns) turn = 0;
   }
 };
 __device__ __forceinline__ KvWindowBlock kv_block(const AttnWindowArgs& a, int splits) {
@@ -1021,7 +1024,10 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   // block of the kv group walks the slabs from the sequence end, head-minor,
   // so the blocks running at once read the same Q / dO slabs (one XCD's L2
   // serves them; block ids cycle through the kv heads, which the dispatcher
-  // spreads over the XCDs).
+  // spreads over the XCDs). WIN: the windows of neighbouring key tiles begin and
+  // end two slabs apart; with go_round each block begins at the slab of its window
+  // that has a given remainder modulo nwin and goes round, so that here too those
+  // running at once read the same slabs.
   // (walked without a division or a product: head, slab and the addresses of
   // their rows advance by the step's)
   struct Pair {
@@ -1036,7 +1042,9 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   const long q_wrap = q_adv - (long)grp * D * 2 - (long)BQ * qrb;
   const long o_wrap = o_adv - (long)grp * D * 2 - (long)BQ * orb;
   auto pair_at = [&](int p) __attribute__((always_inline)) {
-    const int n = m * grp + p % grp, q0 = (j0 + ns - 1 - p / grp) * BQ;
+    const int n = m * grp + p % grp;
+    int q0 = (j0 + ns - 1 - p / grp) * BQ;
+    if constexpr (WIN) q0 += (kb_.turn > p / grp ? kb_.turn - ns : kb_.turn) * BQ;
     return Pair{n, q0,
                 reinterpret_cast<const char*>(a.q + (rb + q0) * a.ld_qkv + (long)n * D),
                 reinterpret_cast<const char*>(dout + (rb + q0) * ldo + (long)n * D)};
@@ -1049,6 +1057,16 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
     w.o += wrap ? o_wrap : o_adv;
     w.n -= wrap ? grp : 0;
     w.q0 -= wrap ? BQ : 0;
+    if constexpr (WIN) {
+      if (__builtin_expect(w.q0 < j0 * BQ, 0)) {
+        // (once in a block: a branch, which the comment keeps the compiler from
+        // turning into selects in every pair)
+        asm volatile("; round");
+        w.q0 += ns * BQ;
+        w.q += (long)ns * BQ * qrb;
+        w.o += (long)ns * BQ * orb;
+      }
+    }
     return w;
   };
   // DMA instruction I of a pair into a buffer: the Q slab, the dO slab, then
@@ -1744,6 +1762,14 @@ struct KvLaunch {
       pk = part;
       pv = part + p.part;
     }
+    // The Q and dO that an XCD's 32 blocks read at about the same time when each goes
+    // from its own window's end: beyond its L2 of 4 MB they go round instead (16384
+    // tokens, 32 / 2 heads of 128, window 512, 21 MB: backward 663 -> 560 us; 4 x 4096,
+    // 32 / 8, window 1024, 13 MB: 980 -> 940), below it costs 2 % (1 x 4096, 32 / 8,
+    // window 512, 5 MB: 179 -> 183)
+    const long batch = std::min(a.batch, 32), tiles = (32 + batch - 1) / batch;
+    const long slabs = batch * (2 * tiles + DsWindow(a).nwin);
+    a.go_round = slabs * (a.n_heads / a.n_kv_heads) * 128 * D > 6L << 20;
     a.sink_chunks = p.chunks;
     a.chunk_slabs = p.slabs;
     a.sink_pk = part + 2 * p.part;

@@ -180,8 +180,9 @@ struct AttnWindowArgs : AttnArgs {
   int window, sinks;
   const int32_t* lens;
   // set by the backward: chunks of the sink tiles' slabs behind their own windows (0:
-  // none), slabs of each, and the sink tiles' partial sums
-  int sink_chunks = 0, chunk_slabs = 0;
+  // none), slabs of each, and the sink tiles' partial sums; whether a key tile's slabs
+  // are walked round
+  int sink_chunks = 0, chunk_slabs = 0, go_round = 0;
   float *sink_pk = nullptr, *sink_pv = nullptr;
 };
 // o [T, n_heads*d] bf16; lse [batch, n_heads, seq] fp32 (natural log).

@@ -35,6 +35,10 @@ CASES = [
     (4, 96, 2, 1, 64, 7, 1, (96, 95, 33, 0)),
     (1, 2050, 2, 1, 128, 513, 16, None),
     (1, 2050, 2, 1, 64, 100, 3, (1987,)),
+    # many heads to a kv head: the key tiles' queries are walked round their window
+    (1, 700, 8, 1, 128, 100, 3, None),
+    (2, 450, 16, 1, 64, 90, 70, (450, 391)),
+    (1, 1300, 16, 2, 128, 400, 0, None),
 ]
 
 
