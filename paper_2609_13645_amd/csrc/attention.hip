@@ -1704,7 +1704,8 @@ static WindowPlan window_plan(const AttnWindowArgs& a) {
   for (int z = 1; z <= 16; ++z) {
     if (z > 1 && (z * 8 > pairs || (z - 1) * nkt * bm >= 512)) break;
     for (const int c : {0, 1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      if (c > 0 && far < c) break;
+      // (the sums of the sink tiles' rows are one launch)
+      if (c > 0 && (far < c || bm * L.nst * 64 * a.d >= 1 << 29)) break;
       const double tile = block_us((pairs + z - 1) / z);
       double longest = tile, all = tile * (double)(nkt * z), extra = 0.0;
       if (c == 0 && far > 0) {

@@ -9,6 +9,8 @@
 // lane keeps its columns' shares of dg and db in registers over all rows of its
 // workgroup; the workgroups' sums are added by a second kernel in a fixed order
 // (no atomics, so the gradients repeat bit for bit).
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(1024) void layernorm_grad_sum_k(const float* __rest
 
 hipError_t layernorm_fwd(const uint16_t* x, const uint16_t* g, const uint16_t* b, uint16_t* y,
                          float* mean, float* rstd, int T, int h, float eps, hipStream_t s) {
-  const dim3 grid((unsigned)(((long)T + 3) / 4)), block(256);
+  const dim3 grid((T + 3) / 4), block(256);
   const int ch = (h / 8 + 63) / 64;
 #define FORGE_LNF(N) \
   hipLaunchKernelGGL(layernorm_fwd_k<N>, grid, block, 0, s, x, g, b, y, mean, rstd, T, h, eps)
@@ -285,8 +287,7 @@ int row_waves(int h) { return h <= 1024 ? 1 : h <= 2048 ? 2 : h <= 4096 ? 4 : 8;
 
 int layernorm_bwd_blocks(int T, int h) {
   const int groups = kBwdWaves / row_waves(h);
-  const long need = ((long)T + groups - 1) / groups;
-  return need < kBwdMaxBlocks ? (int)need : kBwdMaxBlocks;
+  return std::min((T + groups - 1) / groups, kBwdMaxBlocks);
 }
 
 hipError_t layernorm_bwd(const uint16_t* x, const uint16_t* g, const float* mean,
