@@ -789,7 +789,7 @@ constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) |
 
 // The block's rows of its split's partial sums [splits][T][n_kv * D] (NULL
 // when the pairs are not split).
-template <int D>
+template <int D, bool V>
 __device__ __forceinline__ float* kv_part(const AttnArgs& a, float* part, const KvBlock& k,
                                           long row) {
   if (!part) return nullptr;
@@ -798,17 +798,18 @@ __device__ __forceinline__ float* kv_part(const AttnArgs& a, float* part, const 
 }
 
 // WIN: the same, or the rows of the block's slot of a sink tile's partial sums
-// [slots][batch][sink rows][n_kv * D].
-template <int D>
-__device__ __forceinline__ float* kv_part(const AttnWindowArgs& a, float* part, float* sink_part,
-                                          const KvWindowBlock& k) {
+// [slots][batch][sink rows][n_kv * D] of dV (V) or dK.
+template <int D, bool V>
+__device__ __forceinline__ float* kv_part(const AttnWindowArgs& a, float* part,
+                                          const KvWindowBlock& k, long row) {
   const long width = (long)a.n_kv_heads * D;
   if (k.slot >= 0) {
     const int rows = (a.sinks + 63) / 64 * 64;
-    return sink_part + (((long)k.slot * a.batch + k.b) * rows + k.kt * 64) * width + k.m * D;
+    return (V ? a.sink_pv : a.sink_pk) +
+           (((long)k.slot * a.batch + k.b) * rows + k.kt * 64) * width + k.m * D;
   }
   if (!part) return nullptr;
-  return part + (((long)k.z * a.batch + k.b) * a.seq + k.kt * 64) * width + k.m * D;
+  return part + ((long)k.z * a.batch * a.seq + row) * width + k.m * D;
 }
 
 // One DMA instruction: 16 bytes per lane from a buffer of `bytes` bytes (zeros
@@ -1324,18 +1325,12 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
     cur ^= 1;
   }
   if (dsblk) store_ds();
-  float *tv, *tk;
-  if constexpr (WIN) {
-    tv = kv_part<D>(a, pv, a.sink_pv, kb_);
-    tk = kv_part<D>(a, pk, a.sink_pk, kb_);
-  } else {
-    tv = kv_part<D>(a, pv, kb_, rb + k0);
-    tk = kv_part<D>(a, pk, kb_, rb + k0);
-  }
   kv_reduce_store<D>(acc, sm, sm + 2 * P::RED, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D,
-                     ld_d, tv, (long)a.n_kv_heads * D, seq_of(a, S) - k0);
+                     ld_d, kv_part<D, true>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D,
+                     seq_of(a, S) - k0);
   kv_reduce_store<D>(acck, sm, sm + 2 * P::RED, wave, lane, a.scale,
-                     dk + (rb + k0) * ld_d + (long)m * D, ld_d, tk, (long)a.n_kv_heads * D,
+                     dk + (rb + k0) * ld_d + (long)m * D, ld_d,
+                     kv_part<D, false>(a, pk, kb_, rb + k0), (long)a.n_kv_heads * D,
                      seq_of(a, S) - k0);
 }
 
