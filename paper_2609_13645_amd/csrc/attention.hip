@@ -1408,7 +1408,7 @@ __global__ __launch_bounds__(256) void attn_window_sink_sum_k(AttnWindowArgs a, 
   }
 }
 
-// 4. dQ: block of 256 queries (32 per wave, eight waves) of one (batch,
+// 4. dQ: block of 256 queries (32 per wave, eight waves; WIN: or 128, four) of one (batch,
 // head), 64-key tiles up to the diagonal: dQ^T += K^T dS^T, both operands
 // transposed reads from LDS: K^T from the natural K tile [64 keys][D], dS^T
 // from the tile's eight dS blocks (wave w's 32 queries are block w), whose
@@ -1418,19 +1418,19 @@ __global__ __launch_bounds__(256) void attn_window_sink_sum_k(AttnWindowArgs a, 
 // oldest stage's DMA. A wave whose queries all precede a tile skips it;
 // blocks of a tile that do not exist (queries before the keys) are fetched
 // as zeros.
-template <int D>
+template <int D, int WAVES>
 struct DqPlan {
-  static constexpr int BQ = 256, BKV = 64, NW = 8, NST = 3;
+  static constexpr int NW = WAVES, BQ = 32 * NW, BKV = 64, NST = 3;
   static constexpr int NAT = BKV * D / 8;      // K tile chunks
   static constexpr int NDS = BKV * BQ / 8;     // dS tile chunks (eight 4 KB blocks)
   static constexpr int STAGE = NAT + NDS;
   static constexpr int MEM = DmaPlan<D, NW>::PER + NDS / 64 / NW;   // DMA per wave per tile
 };
 
-template <int D, typename Args>
-__global__ __launch_bounds__(512, 1) void attn_bwd_dq_k(Args a, const bf16_t* __restrict__ ds,
+template <int D, typename Args, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 1) void attn_bwd_dq_k(Args a, const bf16_t* __restrict__ ds,
                                                        bf16_t* __restrict__ dq, long ld_d) {
-  using Q = DqPlan<D>;
+  using Q = DqPlan<D, WAVES>;
   constexpr bool WIN = kWindow<Args>;
   constexpr int BQ = Q::BQ, BKV = Q::BKV, NAT = Q::NAT, NW = Q::NW, NST = Q::NST, DB = D / 32;
   __shared__ uint4 sm[NST * Q::STAGE];
@@ -1811,13 +1811,26 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
   const dim3 block(256);
   const dim3 pgrid((unsigned)((rows + 2048 / D - 1) / (2048 / D)));
   const dim3 kgrid((unsigned)k.blocks);
-  const dim3 qgrid((unsigned)((a.seq + 255) / 256 * a.n_heads * a.batch));
   hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
                      a.seq);
   hipLaunchKernelGGL((attn_bwd_kv_k<D, Args>), kgrid, block, 0, s, a, dout, delta, ds, dv, dk, ld_d,
                      k.pv, k.pk, k.splits);
   kv_sums<D>(a, k, dk, dv, ld_d, s);
-  hipLaunchKernelGGL((attn_bwd_dq_k<D, Args>), qgrid, dim3(512), 0, s, a, ds, dq, ld_d);
+  const auto dq_pass = [&](auto waves) {
+    constexpr int W = decltype(waves)::value;
+    const dim3 grid((unsigned)((a.seq + 32 * W - 1) / (32 * W) * a.n_heads * a.batch));
+    hipLaunchKernelGGL((attn_bwd_dq_k<D, Args, W>), grid, dim3(64 * W), 0, s, a, ds, dq, ld_d);
+  };
+  if constexpr (kWindow<Args>) {
+    // blocks of 128 queries where those of 256 are fewer than CUs (1 x 2048 tokens, 8
+    // heads of 128, window 256: backward 46.0 us, 40.3 with them; 2 x 2000, 16 heads,
+    // window 512, 256 blocks: 113 and 116)
+    if ((long)((a.seq + 255) / 256) * a.n_heads * a.batch < 256) {
+      dq_pass(std::integral_constant<int, 4>{});
+      return hipGetLastError();
+    }
+  }
+  dq_pass(std::integral_constant<int, 8>{});
   return hipGetLastError();
 }
 }  // namespace

@@ -39,6 +39,9 @@ CASES = [
     (1, 700, 8, 1, 128, 100, 3, None),
     (2, 450, 16, 1, 64, 90, 70, (450, 391)),
     (1, 1300, 16, 2, 128, 400, 0, None),
+    # as many blocks of 256 queries as CUs, and more
+    (2, 530, 48, 4, 64, 150, 66, (530, 301)),
+    (1, 420, 128, 16, 128, 90, 2, None),
 ]
 
 
