@@ -276,8 +276,7 @@ forge_status forge_rope_apply(forge_bf16* qkv, int64_t ld, const float* rope_cos
  * mean[t] = mean_j x[t,j], rstd[t] = 1 / sqrt(mean_j (x[t,j] - mean[t])^2 +
  * eps) in fp32, y[t,j] = bf16((x[t,j] - mean[t]) * rstd[t] * g[j] + b[j]).
  * x, y [T, h] bf16 (y must not overlap x), g [h] bf16, b [h] bf16 or NULL (no
- * bias), mean, rstd [T] fp32. 8 <= h <= 8192, h % 8 == 0; T < 2^26 (else
- * UNSUPPORTED).
+ * bias), mean, rstd [T] fp32. 8 <= h <= 8192, h % 8 == 0.
  */
 forge_status forge_layernorm_fwd(const forge_bf16* x, const forge_bf16* g, const forge_bf16* b,
                                  forge_bf16* y, float* mean, float* rstd, int32_t tokens,
@@ -726,7 +725,7 @@ forge_status forge_attention_bwd(const forge_attn_cfg* cfg, const forge_bf16* qk
  * the last `window` tokens, the query's own among them, and the row's first
  * `sinks` tokens. Rules: those of forge_attn_cfg; window >= 1, sinks >= 0
  * (values beyond seq are as seq; window >= seq is causal attention); seq <=
- * 2^23, batch * n_heads * seq < 2^28, batch * n_heads * ceil(seq / 128) < 2^23,
+ * 2^23, batch * n_heads * seq <= 2^27, batch * n_heads * ceil(seq / 128) < 2^23,
  * (n_heads + 2 n_kv_heads) * head_dim <= 2^22 (else UNSUPPORTED).
  */
 typedef struct {

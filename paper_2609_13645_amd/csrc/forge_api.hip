@@ -937,18 +937,10 @@ forge_status forge_rope_apply(forge_bf16* qkv, int64_t ld, const float* rope_cos
   return ok();
 }
 
-namespace {
-forge_status check_layernorm(int32_t tokens, int32_t hidden) {
-  if (forge_status s = check_rows(tokens, hidden)) return s;
-  FORGE_CHECK(tokens < 1 << 26, FORGE_ERR_UNSUPPORTED, "tokens must be < 2^26 (got %d)", tokens);
-  return ok();
-}
-}  // namespace
-
 forge_status forge_layernorm_fwd(const forge_bf16* x, const forge_bf16* g, const forge_bf16* b,
                                  forge_bf16* y, float* mean, float* rstd, int32_t tokens,
                                  int32_t hidden, float eps, forge_stream stream) {
-  if (forge_status s = check_layernorm(tokens, hidden)) return s;
+  if (forge_status s = check_rows(tokens, hidden)) return s;
   FORGE_CHECK(eps >= 0.0f && std::isfinite(eps), FORGE_ERR_INVALID_ARG, "eps must be >= 0");
   if (tokens == 0) return ok();
   FORGE_PTR(x);
@@ -965,7 +957,7 @@ forge_status forge_layernorm_fwd(const forge_bf16* x, const forge_bf16* g, const
 }
 
 forge_status forge_layernorm_bwd_workspace_bytes(int32_t tokens, int32_t hidden, size_t* bytes) {
-  if (forge_status s = check_layernorm(tokens, hidden)) return s;
+  if (forge_status s = check_rows(tokens, hidden)) return s;
   FORGE_CHECK(bytes != nullptr, FORGE_ERR_INVALID_ARG, "bytes is NULL");
   *bytes = (size_t)forge::layernorm_bwd_blocks(tokens, hidden) * 2 * hidden * 4;
   return ok();
@@ -976,7 +968,7 @@ forge_status forge_layernorm_bwd(const forge_bf16* x, const forge_bf16* g, const
                                  const forge_bf16* resid, forge_bf16* dx, float* dg, float* db,
                                  int32_t accumulate, int32_t tokens, int32_t hidden,
                                  void* workspace, forge_stream stream) {
-  if (forge_status s = check_layernorm(tokens, hidden)) return s;
+  if (forge_status s = check_rows(tokens, hidden)) return s;
   FORGE_PTR(dg);
   if (db) FORGE_PTR(db);
   FORGE_CHECK(!overlap(dg, (size_t)hidden * 4, db, (size_t)hidden * 4), FORGE_ERR_INVALID_ARG,
@@ -1923,9 +1915,9 @@ forge_status check_attn_window(const forge_attn_window_cfg* c) {
   FORGE_CHECK(c->seq <= 1 << 23, FORGE_ERR_UNSUPPORTED, "seq > 2^23 (got %d)", c->seq);
   FORGE_CHECK((int64_t)c->n_heads + 2 * (int64_t)c->n_kv_heads <= (1 << 22) / c->head_dim,
               FORGE_ERR_UNSUPPORTED, "a row of qkv exceeds 2^22 elements");
-  FORGE_CHECK((int64_t)c->batch * c->seq < (1 << 28) &&
-                  (int64_t)c->batch * c->seq * c->n_heads < (1 << 28),
-              FORGE_ERR_UNSUPPORTED, "batch * n_heads * seq exceeds 2^28");
+  FORGE_CHECK((int64_t)c->batch * c->seq <= (1 << 27) &&
+                  (int64_t)c->batch * c->seq * c->n_heads <= (1 << 27),
+              FORGE_ERR_UNSUPPORTED, "batch * n_heads * seq exceeds 2^27");
   // (threads of a launch: 512 to every 128 queries at most)
   FORGE_CHECK((int64_t)c->batch * ((c->seq + 127) / 128) * c->n_heads < (1 << 23),
               FORGE_ERR_UNSUPPORTED, "batch * n_heads * ceil(seq / 128) exceeds 2^23");

@@ -31,9 +31,6 @@ __global__ __launch_bounds__(256) void layernorm_fwd_k(const bf16_t* __restrict_
   constexpr int RG = 4 / WPR, LANES = 64 * WPR;
   __shared__ float part[2][4];
   const int grp = threadIdx.x / LANES, col = threadIdx.x % LANES, wave = threadIdx.x >> 6;
-  const long row = (long)blockIdx.x * RG + grp;
-  const int nch = row < T ? h / 8 : 0;   // (no chunks past the last row)
-  const uint4* xr = reinterpret_cast<const uint4*>(x + row * h);
   // sum over the row's waves, in order
   const auto row_sum = [&](float v, int k) {
     v = wave_sum(v);
@@ -46,6 +43,10 @@ __global__ __launch_bounds__(256) void layernorm_fwd_k(const bf16_t* __restrict_
     }
     return v;
   };
+  // (grid.y: more rows than one dimension of a launch has threads for)
+  const long row = ((long)blockIdx.y * gridDim.x + blockIdx.x) * RG + grp;
+  const int nch = row < T ? h / 8 : 0;   // (no chunks past the last row)
+  const uint4* xr = reinterpret_cast<const uint4*>(x + row * h);
   float f[CH][8];
   float s = 0.0f;
 #pragma unroll
@@ -277,9 +278,13 @@ __global__ __launch_bounds__(1024) void layernorm_grad_sum_k(const float* __rest
 
 hipError_t layernorm_fwd(const uint16_t* x, const uint16_t* g, const uint16_t* b, uint16_t* y,
                          float* mean, float* rstd, int T, int h, float eps, hipStream_t s) {
-#define FORGE_LNF(CH, WPR)                                                                  \
-  hipLaunchKernelGGL((layernorm_fwd_k<CH, WPR>), dim3((T + 4 / WPR - 1) / (4 / WPR)), dim3(256), \
-                     0, s, x, g, b, y, mean, rstd, T, h, eps)
+  const auto grid = [&](int rows) {
+    const long n = ((long)T + rows - 1) / rows, most = 1L << 23;
+    return dim3((unsigned)std::min(n, most), (unsigned)((n + most - 1) / most));
+  };
+#define FORGE_LNF(CH, WPR)                                                              \
+  hipLaunchKernelGGL((layernorm_fwd_k<CH, WPR>), grid(4 / WPR), dim3(256), 0, s, x, g, b, y, \
+                     mean, rstd, T, h, eps)
   if (h <= 512) FORGE_LNF(1, 1);
   else if (h <= 1024) FORGE_LNF(2, 1);
   else if (h <= 2048) FORGE_LNF(2, 2);
@@ -301,7 +306,7 @@ int row_waves(int h) { return h <= 1024 ? 1 : h <= 2048 ? 2 : h <= 4096 ? 4 : 8;
 
 int layernorm_bwd_blocks(int T, int h) {
   const int groups = kBwdWaves / row_waves(h);
-  return std::min((T + groups - 1) / groups, kBwdMaxBlocks);
+  return (int)std::min(((long)T + groups - 1) / groups, (long)kBwdMaxBlocks);
 }
 
 hipError_t layernorm_bwd(const uint16_t* x, const uint16_t* g, const float* mean,

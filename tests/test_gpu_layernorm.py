@@ -150,3 +150,25 @@ def test_layernorm_bwd_repeats_bit_for_bit_and_without_rows():
     _lib.forge_layernorm_bwd(None, None, None, None, None, None, None, dg, db, False, 0, h, None)
     torch.cuda.synchronize()
     assert not dg.any() and not db.any()
+
+
+def test_layernorm_of_more_rows_than_a_launch_holds():
+    """2^25 + 3 rows of 8: the forward's workgroups take several turns."""
+    import torch
+    from paper_2609_13645_amd import _lib
+    T, h = (1 << 25) + 3, 8
+    banner(f"layernorm fwd T={T} h={h}")
+    x = torch.randn((T, h), device="cuda").to(torch.bfloat16)
+    g, b = (torch.randn(h, device="cuda").to(torch.bfloat16) for _ in range(2))
+    y, mean, rstd = _fwd(x, g, b, T, h)
+    for at in (0, (1 << 24) - 100, T - 1000):
+        rows = slice(at, at + 1000)
+        xr = x[rows].double()
+        m = xr.mean(1, keepdim=True)
+        rs = ((xr - m).square().mean(1, keepdim=True) + EPS).rsqrt()
+        ref = (xr - m) * rs * g.double() + b.double()
+        terms = (xr.abs() + m.abs()) * rs * g.double().abs() + b.double().abs()
+        off = (y[rows].double() - ref).abs()
+        assert bool((off <= HALF * ref.abs() + SUM * terms).all()), at
+        assert bool(((rstd[rows].double() - rs[:, 0]).abs() <= SUM * rs[:, 0]).all()), at
+    assert bool(torch.isfinite(mean).all()) and bool(torch.isfinite(y).all())
