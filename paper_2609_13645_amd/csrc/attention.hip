@@ -674,7 +674,14 @@ __global__ __launch_bounds__(256) void attn_bwd_prep_k(const bf16_t* __restrict_
                                                        float* __restrict__ delta, long rows,
                                                        int n_heads, int S) {
   constexpr int TPR = D / 8;
-  const long r = (long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  long r = (long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if constexpr (D == 64) {
+    // a workgroup takes one head of 32 tokens, whose statistics are neighbours (32
+    // heads of a token: 8192 tokens 16.5 us, now 12.9; 16 tokens of head dim 128 are
+    // no faster than 16 heads)
+    const unsigned n = blockIdx.x % (unsigned)n_heads, t = blockIdx.x / (unsigned)n_heads;
+    r = ((long)t * (256 / TPR) + threadIdx.x / TPR) * n_heads + n;
+  }
   const int c = threadIdx.x % TPR;
   float s = 0.0f;
   if (r < rows) {
@@ -932,7 +939,7 @@ __device__ __forceinline__ f32x16_t rows16(const bf16x8_t (&r)[4]) {
   return x;
 }
 
-template <int D, typename Args>
+template <int D, typename Args, bool CACHED>
 __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
                                                        const bf16_t* __restrict__ dout,
                                                        const float* __restrict__ delta,
@@ -1123,12 +1130,14 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   // instruction; nontemporal, since it is read back only after the pass (as
   // ordinary stores, the dirty lines the memory-side cache holds at the end
   // are written back while the next pass reads dS: 7 % on that pass)
+  // (CACHED: ordinary, where all of dS fits that cache)
   auto store_ds = [&]() __attribute__((always_inline)) {
     static_for<4>([&](auto J) __attribute__((always_inline)) {
       constexpr int j = J;
-      __builtin_nontemporal_store(
-          dsp[j], reinterpret_cast<u32x4_t*>(dsblk + (j / 2) * 1024 + (j % 2) * 512 +
-                                             (pc0 ^ ((j % 2) * 32))));
+      u32x4_t* piece = reinterpret_cast<u32x4_t*>(dsblk + (j / 2) * 1024 + (j % 2) * 512 +
+                                                  (pc0 ^ ((j % 2) * 32)));
+      if constexpr (CACHED) *piece = dsp[j];
+      else __builtin_nontemporal_store(dsp[j], piece);
     });
   };
   auto pair = [&](const uint4* base, const Pair& w, uint4* next, const Pair& wn)
@@ -1813,12 +1822,25 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
   const long rows = (long)a.batch * a.seq * a.n_heads;
   const KvLaunch<D> k(a, part);
   const dim3 block(256);
-  const dim3 pgrid((unsigned)((rows + 2048 / D - 1) / (2048 / D)));
+  const long T = (long)a.batch * a.seq;
+  const dim3 pgrid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
   const dim3 kgrid((unsigned)k.blocks);
   hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
                      a.seq);
-  hipLaunchKernelGGL((attn_bwd_kv_k<D, Args>), kgrid, block, 0, s, a, dout, delta, ds, dv, dk, ld_d,
-                     k.pv, k.pk, k.splits);
+  bool cached = false;
+  if constexpr (kWindow<Args>) {
+    // Where the memory-side cache of 256 MB holds dS until the dQ pass reads it, ordinary
+    // stores: 15 shapes timed both ways, up to 230 MB 1 to 7 % of the backward (3 x 3000
+    // tokens, 24 / 8 heads of 64, window 400, 198 MB: 167 us nontemporal, 156), from 256
+    // MB between 5 % gained and 19 % lost (4096 tokens, 32 / 8 of 64, 1 GB: 284, 338)
+    cached = attn_window_bwd_ds_bytes(a) <= 240u << 20;
+    if (cached)
+      hipLaunchKernelGGL((attn_bwd_kv_k<D, Args, true>), kgrid, block, 0, s, a, dout, delta, ds,
+                         dv, dk, ld_d, k.pv, k.pk, k.splits);
+  }
+  if (!cached)
+    hipLaunchKernelGGL((attn_bwd_kv_k<D, Args, false>), kgrid, block, 0, s, a, dout, delta, ds, dv,
+                       dk, ld_d, k.pv, k.pk, k.splits);
   kv_sums<D>(a, k, dk, dv, ld_d, s);
   const auto dq_pass = [&](auto waves) {
     constexpr int W = decltype(waves)::value;

@@ -42,6 +42,9 @@ CASES = [
     # as many blocks of 256 queries as CUs, and more
     (2, 530, 48, 4, 64, 150, 66, (530, 301)),
     (1, 420, 128, 16, 128, 90, 2, None),
+    # a score gradient beyond the memory-side cache: stored past it
+    (1, 3500, 20, 4, 64, 2000, 2, None),
+    (1, 3500, 20, 2, 128, 1990, 0, (3333,)),
 ]
 
 
