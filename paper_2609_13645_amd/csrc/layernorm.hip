@@ -98,8 +98,9 @@ __global__ __launch_bounds__(256) void layernorm_fwd_k(const bf16_t* __restrict_
 // groups take rows grid-strided and end with their sums in part [gridDim.x][2][h].
 // Bound by HBM: 16384 x 4096, residual included, 103 us for 537 MB (5.2 TB/s; with a
 // wave per row, whose 8 chunks a lane left one row's loads in flight, 233 us).
-// Narrow rows come near the vector units: 12 operations an element, as few as xh by
-// one fma and dx by two leave.
+// Narrow rows come near the vector units, 13 operations an element (x r - m r as one
+// fma, a 13th less, is no faster at any of 11 shapes and off by 2^-24 |m| r where x - m
+// is exact: rows of one value, whose r is eps^(-1/2)).
 template <int CH, int WPR, int NW>
 __global__ __launch_bounds__(64 * NW) void layernorm_bwd_k(
     const bf16_t* __restrict__ x, const bf16_t* __restrict__ g, const float* __restrict__ mean,
@@ -152,9 +153,7 @@ __global__ __launch_bounds__(64 * NW) void layernorm_bwd_k(
   // (every wave of a workgroup makes the same number of turns: the barriers)
   for (long base = (long)blockIdx.x * RG; base < T; base += step, row += step) {
     const Row next = load(row + step);
-    // xh as one fma each: m r is off by 2^-24 |m| r, as x - m is by m's rounding
     float xh[CH][8], u[CH][8], s1 = 0.0f, s2 = 0.0f;
-    const float mr = -v.m * v.r;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       float df[8];
@@ -162,7 +161,7 @@ __global__ __launch_bounds__(64 * NW) void layernorm_bwd_k(
       unpack8(v.dy[i], df);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        xh[i][e] = __builtin_fmaf(xh[i][e], v.r, mr);
+        xh[i][e] = (xh[i][e] - v.m) * v.r;
         u[i][e] = w[i][e] * df[e];
         s1 += u[i][e];
         s2 = __builtin_fmaf(u[i][e], xh[i][e], s2);

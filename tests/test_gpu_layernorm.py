@@ -124,6 +124,31 @@ def test_layernorm_bwd(T, h, bias, resid, acc):
         assert bool(torch.all(db == 0.25)) if acc else bool(torch.isnan(db).all())
 
 
+@pytest.mark.parametrize("h", [256, 2056, 8192])
+def test_layernorm_bwd_of_rows_of_one_value(h):
+    """x equals its mean: xh is 0 exactly, however large rstd, so dg is 0 and dx that of
+    the centred u."""
+    import torch
+    from paper_2609_13645_amd import _lib
+    banner(f"layernorm bwd rows of one value h={h}")
+    T = 77
+    d, r = _inputs(T, h, h)
+    value = torch.linspace(-700, 900, T, device="cuda").to(torch.bfloat16)
+    x = value[:, None].expand(T, h).contiguous()
+    m, rs = value.float(), torch.full((T,), EPS ** -0.5, device="cuda")
+    ws = torch.empty(_lib.forge_layernorm_bwd_workspace_bytes(T, h), dtype=torch.uint8,
+                     device="cuda")
+    dx = torch.full_like(x, float("nan"))
+    dg, db = (torch.full((h,), float("nan"), device="cuda") for _ in range(2))
+    _lib.forge_layernorm_bwd(x, d["g"], m, rs, d["dy"], None, dx, dg, db, False, T, h, ws)
+    torch.cuda.synchronize()
+    assert not dg.any()
+    u, scale = r["dy"] * r["g"], float(rs[0])
+    ref = scale * (u - u.mean(1, keepdims=True))
+    terms = scale * (np.abs(u) + np.abs(u).mean(1, keepdims=True))
+    _within(dx, ref, HALF * np.abs(ref) + SUM * terms, "dx")
+
+
 def test_layernorm_bwd_repeats_bit_for_bit_and_without_rows():
     import torch
     from paper_2609_13645_amd import _lib
