@@ -289,11 +289,13 @@ __device__ __forceinline__ float sum_xor32(float v) {
 }
 }  // namespace fa
 
-template <int D, typename Args>
-__global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict__ o,
-                                                         float* __restrict__ lse) {
+// NW waves of 32 queries; KG groups of them share the block's key tiles (group g takes
+// tiles g, g + KG, ..) and add up their softmaxes at the end.
+template <int D, typename Args, int NW, int KG>
+__global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k(
+    Args a, bf16_t* __restrict__ o, float* __restrict__ lse) {
   constexpr bool WIN = kWindow<Args>;
-  constexpr int BQ = 128, BKV = 64, NAT = BKV * D / 8, KK = D / 16, DB = D / 32;
+  constexpr int BQ = 32 * NW, BKV = 64, NAT = BKV * D / 8, KK = D / 16, DB = D / 32;
   constexpr int TILE_B = NAT * 16;       // bytes of one K or V tile
   constexpr int HALF_B = TILE_B / 2;     // rows 32..63 of a tile
   constexpr int ROW16_B = 16 * D * 2;    // 16 rows of a tile
@@ -302,7 +304,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
   // K slots 0, 1 then V slots 0, 1: tile t's K in K slot t & 1, its V in V
   // slot t & 1. K runs one tile ahead of V (S of tile j + 1 is formed while
   // tile j's softmax and P V run), so each slot pair is a double buffer.
-  __shared__ uint4 smem[4 * NAT];
+  __shared__ uint4 smem_[KG * 4 * NAT];   // (of each group)
   const int S = a.seq;
   const int nqt = (S + BQ - 1) / BQ;
   // Block order: the query tiles with the most keys (the last ones) first,
@@ -333,7 +335,12 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
   const bf16_t* Kg = a.k + rb * a.ld_qkv + (long)m * D;
   const bf16_t* Vg = a.v + rb * a.ld_qkv + (long)m * D;
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = 0;
+  if constexpr (KG > 1) {
+    kg = wave / NW;
+    wave %= NW;
+  }
+  uint4* smem = smem_ + kg * 4 * NAT;
   const int hh = lane >> 5, l32 = lane & 31;
   const int q0w = qt * BQ + wave * 32;
   const int q = q0w + l32;
@@ -351,13 +358,15 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
   const int q_last = min(qt * BQ + BQ, E) - 1;
   const WindowTiles win(a, qt * BQ, q_last + 1);
   const int nkt = WIN ? win.count : q_last / BKV + 1;
-  const auto tile_of = [&](int j) __attribute__((always_inline)) { return WIN ? win(j) : j; };
+  const auto at = [&](int j) __attribute__((always_inline)) { return KG > 1 ? j * KG + kg : j; };
+  const auto tile_of = [&](int j) __attribute__((always_inline)) { return WIN ? win(at(j)) : j; };
   // the wave's last key tile (its queries end at q0w + 31)
   const int lw = min(q0w + 31, E - 1) / BKV;
   // whether the wave's queries see a key of tile j
   const auto sees = [&](int j) __attribute__((always_inline)) {
     const int k0 = tile_of(j) * BKV;
-    return k0 <= lw * BKV && (k0 < a.sinks || k0 + BKV - 1 > q0w - a.window);
+    return (KG == 1 || at(j) < nkt) && k0 <= lw * BKV &&
+           (k0 < a.sinks || k0 + BKV - 1 > q0w - a.window);
   };
 
   // per-lane byte addresses in K slot 0 / V slot 0: K row fragment of slice
@@ -378,16 +387,16 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
     }
   }
 
-  uint32_t doff[DmaPlan<D, 4>::PER];
-  dma_offsets<D, 4>(a.ld_qkv, wave, lane, doff);
+  uint32_t doff[DmaPlan<D, NW>::PER];
+  dma_offsets<D, NW>(a.ld_qkv, wave, lane, doff);
   auto dma_k = [&](int j) __attribute__((always_inline)) {
-    dma_tile_at<D, 4>(Kg, a.ld_qkv, tile_of(j) * BKV, E, smem + (j & 1) * NAT, wave, doff);
+    dma_tile_at<D, NW>(Kg, a.ld_qkv, tile_of(j) * BKV, E, smem + (j & 1) * NAT, wave, doff);
   };
   auto dma_v = [&](int j) __attribute__((always_inline)) {
-    dma_tile_at<D, 4>(Vg, a.ld_qkv, tile_of(j) * BKV, E, smem + (2 + (j & 1)) * NAT, wave, doff);
+    dma_tile_at<D, NW>(Vg, a.ld_qkv, tile_of(j) * BKV, E, smem + (2 + (j & 1)) * NAT, wave, doff);
   };
 
-  // S^T of a tile (K slot KS) into sc: K fragments KW steps ahead, each MFMA
+  // S^T of a tile (K slot KG) into sc: K fragments KW steps ahead, each MFMA
   // pair waiting for its own two reads; after MFMA step kk, the hook runs
   // (the softmax work of the previous tile, interleaved with these MFMAs)
   auto scores = [&](auto KS, f32x16_t (&sc)[2], auto&& hook) __attribute__((always_inline)) {
@@ -526,9 +535,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
       __attribute__((always_inline)) {
     constexpr int P = decltype(PAR)::value;   // j & 1
     fa::sync_block();
-    if (j + 2 < nkt) dma_k(j + 2);
-    if (j + 1 < nkt) dma_v(j + 1);
-    const bool next = WIN ? j + 1 < nkt && sees(j + 1) : j < lw;
+    if (at(j + 2) < nkt) dma_k(j + 2);
+    if (at(j + 1) < nkt) dma_v(j + 1);
+    const bool next = WIN ? at(j + 1) < nkt && sees(j + 1) : j < lw;
     // no query of this wave sees a key of the tile: all are before it (WIN: or
     // past its window; the last such tile runs all the same, its scores hidden
     // whatever they hold, since the next one's are due now: as a branch of its
@@ -557,7 +566,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
   const long orow_ld = (long)(a.n_heads * D);
   if (WIN && qt * BQ >= E) {
     // no tokens: zeros
-    if (q < S) {
+    if (q < S && kg == 0) {
       bf16_t* orow = o + (rb + q) * orow_ld + (long)n * D;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
@@ -568,20 +577,63 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(Args a, bf16_t* __restrict_
     }
     return;
   }
-  dma_k(0);
-  dma_v(0);
-  if (nkt > 1) dma_k(1);
+  if (KG == 1 || kg < nkt) {
+    dma_k(0);
+    dma_v(0);
+  }
+  if (at(1) < nkt) dma_k(1);
   fa::sync_block();
   scores(fa::ic<0>{}, sa, no_hook);
   if constexpr (WIN) {
     zero(sb[0]);
     zero(sb[1]);
   }
-  for (int j = 0; j < nkt; j += 2) {
+  const int steps = (nkt + KG - 1) / KG;   // (the same for every group: the barriers)
+  for (int j = 0; j < steps; j += 2) {
     iteration(fa::ic<0>{}, sa, sb, j);
-    if (j + 1 < nkt) iteration(fa::ic<1>{}, sb, sa, j + 1);
+    if (j + 1 < steps) iteration(fa::ic<1>{}, sb, sa, j + 1);
   }
   lrow = fa::sum_xor32(lrow);
+  if constexpr (KG > 1) {
+    // the groups' rows to the first: o = sum_g o_g 2^(m_g - m), l likewise, m = max_g m_g
+    __shared__ float2 ml[KG][NW * 64];
+    const int t = wave * 64 + lane;
+    __syncthreads();   // the last tiles are read
+    ml[kg][t] = make_float2(mrow, lrow);
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < DB * 4; ++i)
+        smem[i * (NW * 64) + t] = __builtin_bit_cast(
+            uint4, make_float4(oacc[i / 4][i % 4 * 4], oacc[i / 4][i % 4 * 4 + 1],
+                               oacc[i / 4][i % 4 * 4 + 2], oacc[i / 4][i % 4 * 4 + 3]));
+    }
+    __syncthreads();
+    if (kg > 0) return;
+    float m_all = mrow;
+#pragma unroll
+    for (int k = 1; k < KG; ++k) m_all = fmaxf(m_all, ml[k][t].x);
+    const float own = fast_exp2(mrow - m_all);
+    lrow *= own;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) oacc[db][e] *= own;
+#pragma unroll
+    for (int k = 1; k < KG; ++k) {
+      const float2 other = ml[k][t];
+      const float f = fast_exp2(other.x - m_all);
+      lrow = __builtin_fmaf(other.y, f, lrow);
+#pragma unroll
+      for (int i = 0; i < DB * 4; ++i) {
+        const float4 v = __builtin_bit_cast(float4, smem_[k * 4 * NAT + i * (NW * 64) + t]);
+        oacc[i / 4][i % 4 * 4] = __builtin_fmaf(v.x, f, oacc[i / 4][i % 4 * 4]);
+        oacc[i / 4][i % 4 * 4 + 1] = __builtin_fmaf(v.y, f, oacc[i / 4][i % 4 * 4 + 1]);
+        oacc[i / 4][i % 4 * 4 + 2] = __builtin_fmaf(v.z, f, oacc[i / 4][i % 4 * 4 + 2]);
+        oacc[i / 4][i % 4 * 4 + 3] = __builtin_fmaf(v.w, f, oacc[i / 4][i % 4 * 4 + 3]);
+      }
+    }
+    mrow = m_all;
+  }
   if (q < S) {
     // (WIN: rows past the tokens' end get zeros and -inf)
     const bool none = WIN && q >= E;
@@ -1621,21 +1673,30 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_bwd_dq_k(Args a, const bf1
 }  // namespace
 
 namespace {
-template <typename Args>
-hipError_t attn_fwd_any(const Args& a, uint16_t* o, float* lse, hipStream_t s) {
-  const dim3 grid((unsigned)((a.seq + 127) / 128 * a.n_heads * a.batch)), block(256);
-  if (a.d == 128) hipLaunchKernelGGL((attn_fwd_k<128, Args>), grid, block, 0, s, a, o, lse);
-  else if (a.d == 64) hipLaunchKernelGGL((attn_fwd_k<64, Args>), grid, block, 0, s, a, o, lse);
+template <int NW, int KG, typename Args>
+hipError_t attn_fwd_waves(const Args& a, uint16_t* o, float* lse, hipStream_t s) {
+  constexpr int BQ = 32 * NW;
+  const dim3 grid((unsigned)((a.seq + BQ - 1) / BQ * a.n_heads * a.batch)), block(64 * NW * KG);
+  if (a.d == 128) hipLaunchKernelGGL((attn_fwd_k<128, Args, NW, KG>), grid, block, 0, s, a, o, lse);
+  else if (a.d == 64) hipLaunchKernelGGL((attn_fwd_k<64, Args, NW, KG>), grid, block, 0, s, a, o, lse);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
 }  // namespace
 
 hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s) {
-  return attn_fwd_any(a, o, lse, s);
+  return attn_fwd_waves<4, 1>(a, o, lse, s);
 }
 hipError_t attn_window_fwd(const AttnWindowArgs& a, uint16_t* o, float* lse, hipStream_t s) {
-  return attn_fwd_any(a, o, lse, s);
+  // Blocks of 64 queries, their key tiles in two groups, where all of them run at once (by
+  // their LDS one on a CU for head dim 128, two for 64). 50 shapes timed both ways: 3 x 333
+  // tokens, 12 heads of 64, window 128 10.2 us as blocks of 128 queries, so 6.9; all keys:
+  // 4096 tokens, 2 heads of 64 64.5, 35.4; 2048, 7 of 128 43.3, 27.8. Where some wait for a
+  // CU they lose (2048, 9 of 128, window 500 19.3, 24.6), and where all keys are one tile
+  // (64, 8 of 64 4.6, 5.1).
+  const long blocks = (long)((a.seq + 63) / 64) * a.n_heads * a.batch;
+  if (a.seq > 64 && blocks <= 256 * (a.d == 64 ? 2 : 1)) return attn_fwd_waves<2, 2>(a, o, lse, s);
+  return attn_fwd_waves<4, 1>(a, o, lse, s);
 }
 
 size_t attn_bwd_ds_bytes(const AttnArgs& a) {

@@ -42,6 +42,15 @@ CASES = [
     # as many blocks of 256 queries as CUs, and more
     (2, 530, 48, 4, 64, 150, 66, (530, 301)),
     (1, 420, 128, 16, 128, 90, 2, None),
+    # more blocks of 64 queries than run at once: the forward's blocks of 128
+    (3, 200, 48, 12, 64, 37, 3, (200, 129, 0)),
+    (2, 333, 24, 6, 128, 100, 70, (333, 65)),
+    (1, 129, 180, 12, 64, 5, 0, None),
+    (5, 65, 30, 2, 128, 3, 1, (65, 64, 1, 33, 65)),
+    (2, 700, 24, 4, 64, 33, 130, (700, 513)),
+    # one tile of keys
+    (2, 64, 4, 2, 64, 20, 3, (64, 0)),
+    (3, 50, 6, 2, 128, 50, 0, (50, 33, 1)),
     # a score gradient beyond the memory-side cache: stored past it
     (1, 3500, 20, 4, 64, 2000, 2, None),
     (1, 3500, 20, 2, 128, 1990, 0, (3333,)),
