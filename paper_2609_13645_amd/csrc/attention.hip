@@ -1400,24 +1400,9 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
 }
 
 // dK and dV from the splits' partial sums, added in split order; eight columns
-// per thread, grid.y 0: dK (times scale), 1: dV.
-// (WIN: but for the first `skip` of every `seq` rows, those of sink tiles.)
-template <bool WIN>
-__global__ __launch_bounds__(256) void attn_bwd_kv_sum_k(const float* __restrict__ pk,
-                                                         const float* __restrict__ pv, int splits,
-                                                         long rows, int width, float scale,
-                                                         bf16_t* __restrict__ dk,
-                                                         bf16_t* __restrict__ dv, long ld_d,
-                                                         int seq, int skip) {
-  const int cpr = width / 8;
-  const long q = (long)blockIdx.x * 256 + threadIdx.x;
-  if (q >= rows * cpr) return;
-  const long r = q / cpr;
-  if (WIN && r % seq < skip) return;
-  const int c = (int)(q % cpr) * 8;
-  const bool v = blockIdx.y != 0;
-  const float* src = (v ? pv : pk) + r * width + c;
-  const long stride = rows * width;
+// per thread.
+__device__ __forceinline__ void split_sum(const float* src, int splits, long stride, float scale,
+                                          bf16_t* out) {
   f32x4_t x = *reinterpret_cast<const f32x4_t*>(src);
   f32x4_t y = *reinterpret_cast<const f32x4_t*>(src + 4);
 #pragma unroll 4
@@ -1425,43 +1410,67 @@ __global__ __launch_bounds__(256) void attn_bwd_kv_sum_k(const float* __restrict
     x += *reinterpret_cast<const f32x4_t*>(src + z * stride);
     y += *reinterpret_cast<const f32x4_t*>(src + z * stride + 4);
   }
-  const float sc = v ? 1.0f : scale;
-  const float f[8] = {x[0] * sc, x[1] * sc, x[2] * sc, x[3] * sc,
-                      y[0] * sc, y[1] * sc, y[2] * sc, y[3] * sc};
-  *reinterpret_cast<uint4*>((v ? dv : dk) + r * ld_d + c) = pack8(f);
+  const float f[8] = {x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale,
+                      y[0] * scale, y[1] * scale, y[2] * scale, y[3] * scale};
+  *reinterpret_cast<uint4*>(out) = pack8(f);
+}
+// (grid.y 0: dK, times scale; 1: dV)
+__global__ __launch_bounds__(256) void attn_bwd_kv_sum_k(const float* __restrict__ pk,
+                                                         const float* __restrict__ pv, int splits,
+                                                         long rows, int width, float scale,
+                                                         bf16_t* __restrict__ dk,
+                                                         bf16_t* __restrict__ dv, long ld_d) {
+  const int cpr = width / 8;
+  const long q = (long)blockIdx.x * 256 + threadIdx.x;
+  if (q >= rows * cpr) return;
+  const long r = q / cpr;
+  const int c = (int)(q % cpr) * 8;
+  const bool v = blockIdx.y != 0;
+  split_sum((v ? pv : pk) + r * width + c, splits, rows * width, v ? 1.0f : scale,
+            (v ? dv : dk) + r * ld_d + c);
 }
 
-// WIN: dK and dV of the sink tiles' rows, the sums of their slots (splits, then
-// chunks). A workgroup takes 128 columns of a row: 16 lanes of eight columns, 16
-// stripes of slots, whose sums are added in order.
-__global__ __launch_bounds__(256) void attn_window_sink_sum_k(AttnWindowArgs a, int slots,
-                                                              int width, bf16_t* __restrict__ dk,
-                                                              bf16_t* __restrict__ dv, long ld_d) {
-  __shared__ float red[16][16][8];
-  const int cg = threadIdx.x & 15, stripe = threadIdx.x >> 4;
-  const int rows = (a.sinks + 63) / 64 * 64, mine = min(rows, a.seq);
-  const int pieces = (width + 127) / 128;
-  const int piece = (int)blockIdx.x % pieces, row = (int)blockIdx.x / pieces % mine;
-  const int b = (int)blockIdx.x / pieces / mine, col = piece * 128 + cg * 8;
-  const bool v = blockIdx.y != 0;
-  f32x4_t x = {}, y = {};
-  if (col < width) {
+// WIN: all sums of partials, in units of 256 threads (t, with 8 KB of LDS): the rows
+// whose pairs are split, but for those of sink tiles kept in slots (a.part_units; dK,
+// then dV), then the sink tiles' rows, the sums of their slots (splits, then chunks): a
+// unit takes 128 columns of a row, 16 lanes of eight columns, 16 stripes of slots, whose
+// sums are added in order.
+__device__ __forceinline__ void window_sums(const AttnWindowArgs& a, int unit, int t, float* lds,
+                                            long ld_d) {
+  float(*red)[16][8] = reinterpret_cast<float(*)[16][8]>(lds);
+  const int width = a.n_kv_heads * a.d, rows = (a.sinks + 63) / 64 * 64, mine = min(rows, a.seq);
+  const int pieces = (width + 127) / 128, cg = t & 15, stripe = t >> 4;
+  const int u = unit - a.part_units;
+  const int half = u < 0 ? a.part_units / 2 : (a.sum_units - a.part_units) / 2;
+  const bool v = (u < 0 ? unit : u) >= half;
+  const float sc = v ? 1.0f : a.scale;
+  bf16_t* out = v ? a.dv : a.dk;
+  const int i = (u < 0 ? unit : u) - (v ? half : 0);
+  const int b = i / pieces / max(1, mine), row = i / pieces % max(1, mine);
+  const int col = i % pieces * 128 + cg * 8;
+  const bool sink = u >= 0 && col < width;
+  if (u < 0) {
+    const long T = (long)a.batch * a.seq, q = (long)i * 256 + t, r = q / (width / 8);
+    const int c = (int)(q % (width / 8)) * 8;
+    if (r < T && r % a.seq >= (a.sink_chunks > 0 ? rows : 0))
+      split_sum((v ? a.pv : a.pk) + r * width + c, a.splits, T * width, sc, out + r * ld_d + c);
+  } else if (sink) {
+    f32x4_t x = {}, y = {};
     const float* src = (v ? a.sink_pv : a.sink_pk) + ((long)b * rows + row) * width + col;
 #pragma unroll 4
-    for (int z = stripe; z < slots; z += 16) {
+    for (int z = stripe; z < a.splits + a.sink_chunks; z += 16) {
       const float* p = src + (long)z * a.batch * rows * width;
       x += *reinterpret_cast<const f32x4_t*>(p);
       y += *reinterpret_cast<const f32x4_t*>(p + 4);
     }
-  }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    red[stripe][cg][e] = x[e];
-    red[stripe][cg][4 + e] = y[e];
+    for (int e = 0; e < 4; ++e) {
+      red[stripe][cg][e] = x[e];
+      red[stripe][cg][4 + e] = y[e];
+    }
   }
   __syncthreads();
-  if (stripe == 0 && col < width) {
-    const float sc = v ? 1.0f : a.scale;
+  if (sink && stripe == 0) {
     float f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -1469,8 +1478,12 @@ __global__ __launch_bounds__(256) void attn_window_sink_sum_k(AttnWindowArgs a, 
       for (int k = 0; k < 16; ++k) f[e] += red[k][cg][e];
       f[e] *= sc;
     }
-    *reinterpret_cast<uint4*>((v ? dv : dk) + ((long)b * a.seq + row) * ld_d + col) = pack8(f);
+    *reinterpret_cast<uint4*>(out + ((long)b * a.seq + row) * ld_d + col) = pack8(f);
   }
+}
+__global__ __launch_bounds__(256) void attn_window_sum_k(AttnWindowArgs a, long ld_d) {
+  __shared__ float red[2048];
+  window_sums(a, (int)blockIdx.x, (int)threadIdx.x, red, ld_d);
 }
 
 // 4. dQ: block of 256 queries (32 per wave, eight waves; WIN: or 128, four) of one (batch,
@@ -1511,8 +1524,15 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_bwd_dq_k(Args a, const bf1
   int b = id / a.n_kv_heads / grp % a.batch;
   int qt = nqt - 1 - id / (a.n_kv_heads * grp * a.batch);
   if constexpr (WIN) {
-    // WIN: as in the forward
-    const int i = xcd_order(id, nqt * a.n_heads * a.batch);
+    // WIN: the last blocks are the sums, where the kv pass left few; else as in the forward
+    const int blocks = nqt * a.n_heads * a.batch;
+    if (id >= blocks) {
+      const int t = (int)threadIdx.x;
+      window_sums(a, (id - blocks) * (WAVES / 4) + (t >> 8), t & 255,
+                  reinterpret_cast<float*>(sm) + (t >> 8) * 2048, ld_d);
+      return;
+    }
+    const int i = xcd_order(id, blocks);
     const int t = i / grp / a.batch;
     b = i / grp % a.batch;
     qt = nqt - 1 - t % nqt;
@@ -1752,16 +1772,17 @@ size_t attn_bwd_part_bytes(const AttnArgs& a) {
 // The like estimate for a sliding window, over the splits of a key tile's pairs and
 // the chunks of what the sink tiles see behind their own windows (0 chunks: the sink
 // tiles' own blocks take it): the longest block, or an even share of all of them and
-// a quarter of the longest behind it, plus the sums' launches and partials. Fitted
+// a quarter of the longest behind it, plus the sums' start and partials. Fitted
 // to 34 shapes timed with up to 8 splits x 13 chunks: the pick is on average 0.6 %
 // slower than the fastest, one split and no chunk 68 % (1 x 8192 tokens, 16 / 2 heads
-// of 128, window 256, 4 sinks: 918 us, with 64 chunks 136).
+// of 128, window 256, 4 sinks: 918 us, with 64 chunks 136); the sums' terms to 31, most
+// of them small (3 us and 1.5 MB a us, a launch of their own: up to 12 % slower).
 struct WindowPlan {
   int splits, chunks, slabs;   // slabs of a chunk
   size_t part, sink;           // floats of partial sums (dK or dV): of the splits, of the sinks
 };
 static WindowPlan window_plan(const AttnWindowArgs& a) {
-  constexpr double kCUs = 256.0, kLaunchUs = 3.0, kPartBytesPerUs = 1.5e6;
+  constexpr double kCUs = 256.0, kSumUs = 1.0, kPartBytesPerUs = 3.0e6;
   const double kPairUs = a.d == 128 ? 3.0 : 1.5, kBlockUs = a.d == 128 ? 1.5 : 4.5;
   const DsWindow L(a);
   const long grp = a.n_heads / a.n_kv_heads, bm = (long)a.batch * a.n_kv_heads;
@@ -1771,9 +1792,9 @@ static WindowPlan window_plan(const AttnWindowArgs& a) {
   WindowPlan best{};
   double cost = 0.0;
   for (int z = 1; z <= 16; ++z) {
-    if (z > 1 && (z * 8 > pairs || (z - 1) * nkt * bm >= 512)) break;
+    if (z > 1 && (z * 4 > pairs || (z - 1) * nkt * bm >= 512)) break;
     for (const int c : {0, 1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      // (the sums of the sink tiles' rows are one launch)
+      // (the units of the sums are counted in 32 bits)
       if (c > 0 && (far < c || bm * L.nst * 64 * a.d >= 1 << 29)) break;
       const double tile = block_us((pairs + z - 1) / z);
       double longest = tile, all = tile * (double)(nkt * z), extra = 0.0;
@@ -1784,9 +1805,9 @@ static WindowPlan window_plan(const AttnWindowArgs& a) {
         const double chunk = block_us(grp * ((far + c - 1) / c));
         longest = std::max(longest, chunk);
         all += chunk * (double)(L.nst * c);
-        extra += kLaunchUs + 2.0 * (z + c) * a.batch * L.nst * 64 * width * 8.0 / kPartBytesPerUs;
+        extra += kSumUs + 2.0 * (z + c) * a.batch * L.nst * 64 * width * 8.0 / kPartBytesPerUs;
       }
-      if (z > 1) extra += kLaunchUs + (z + 1.0) * a.batch * a.seq * width * 8.0 / kPartBytesPerUs;
+      if (z > 1) extra += kSumUs + (z + 1.0) * a.batch * a.seq * width * 8.0 / kPartBytesPerUs;
       const double share = all * (double)bm / kCUs;
       const double t = (share > longest ? share + 0.25 * longest : longest) + extra;
       if ((z == 1 && c == 0) || t < cost) {
@@ -1844,37 +1865,15 @@ struct KvLaunch {
     a.chunk_slabs = p.slabs;
     a.sink_pk = part + 2 * p.part;
     a.sink_pv = a.sink_pk + p.sink;
+    a.pk = pk;
+    a.pv = pv;
+    a.splits = splits;
+    const long width = a.n_kv_heads * D, rows = a.sink_chunks > 0 ? std::min(nst * 64, a.seq) : 0;
+    a.part_units =
+        splits > 1 ? (int)(((long)a.batch * a.seq * (width / 8) + 255) / 256 * 2) : 0;
+    a.sum_units = a.part_units + (int)(rows * a.batch * ((width + 127) / 128) * 2);
   }
 };
-
-// dK and dV from the partial sums of the splits and, of sink tiles, the chunks.
-template <int D>
-void kv_sums(const AttnArgs& a, const KvLaunch<D>& k, uint16_t* dk, uint16_t* dv, long ld_d,
-             hipStream_t s) {
-  if (k.splits <= 1) return;
-  const long T = (long)a.batch * a.seq;
-  const int width = a.n_kv_heads * D;
-  const dim3 grid((unsigned)((T * (width / 8) + 255) / 256), 2);
-  hipLaunchKernelGGL(attn_bwd_kv_sum_k<false>, grid, dim3(256), 0, s, k.pk, k.pv, k.splits, T,
-                     width, a.scale, dk, dv, ld_d, a.seq, 0);
-}
-template <int D>
-void kv_sums(const AttnWindowArgs& a, const KvLaunch<D>& k, uint16_t* dk, uint16_t* dv, long ld_d,
-             hipStream_t s) {
-  const long T = (long)a.batch * a.seq;
-  const int width = a.n_kv_heads * D;
-  const int rows = a.sink_chunks > 0 ? (a.sinks + 63) / 64 * 64 : 0;
-  if (k.splits > 1) {
-    const dim3 grid((unsigned)((T * (width / 8) + 255) / 256), 2);
-    hipLaunchKernelGGL(attn_bwd_kv_sum_k<true>, grid, dim3(256), 0, s, k.pk, k.pv, k.splits, T,
-                       width, a.scale, dk, dv, ld_d, a.seq, rows);
-  }
-  if (rows > 0) {
-    const dim3 grid((unsigned)(std::min(rows, a.seq) * a.batch * ((width + 127) / 128)), 2);
-    hipLaunchKernelGGL(attn_window_sink_sum_k, grid, dim3(256), 0, s, a, k.splits + a.sink_chunks,
-                       width, dk, dv, ld_d);
-  }
-}
 
 template <int D, typename Args>
 hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const float* lse,
@@ -1902,10 +1901,25 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
   if (!cached)
     hipLaunchKernelGGL((attn_bwd_kv_k<D, Args, false>), kgrid, block, 0, s, a, dout, delta, ds, dv,
                        dk, ld_d, k.pv, k.pk, k.splits);
-  kv_sums<D>(a, k, dk, dv, ld_d, s);
+  int tail = 0;   // units of the sums in the dQ pass (even: dK and dV)
+  if constexpr (kWindow<Args>) {
+    a.dk = dk;
+    a.dv = dv;
+    // Few sums (up to three for a CU) run in the dQ pass, a launch less: 257 tokens, 4 / 2
+    // heads of 64, window 64 18.3 -> 15.8 us, 2 x 500, 8 / 2 of 128, window 100 28.3 -> 25.5;
+    // more take it longer than a launch (4096, 8 / 8 of 128, 16 sinks, 1024: 66.8, 69.8)
+    if (a.sum_units <= 768) tail = a.sum_units;
+    else hipLaunchKernelGGL(attn_window_sum_k, dim3((unsigned)a.sum_units), block, 0, s, a, ld_d);
+  } else if (k.splits > 1) {
+    const int width = a.n_kv_heads * D;
+    const dim3 grid((unsigned)((T * (width / 8) + 255) / 256), 2);
+    hipLaunchKernelGGL(attn_bwd_kv_sum_k, grid, block, 0, s, k.pk, k.pv, k.splits, T, width,
+                       a.scale, dk, dv, ld_d);
+  }
   const auto dq_pass = [&](auto waves) {
     constexpr int W = decltype(waves)::value;
-    const dim3 grid((unsigned)((a.seq + 32 * W - 1) / (32 * W) * a.n_heads * a.batch));
+    const dim3 grid((unsigned)((a.seq + 32 * W - 1) / (32 * W) * a.n_heads * a.batch +
+                               tail / (W / 4)));
     hipLaunchKernelGGL((attn_bwd_dq_k<D, Args, W>), grid, dim3(64 * W), 0, s, a, ds, dq, ld_d);
   };
   if constexpr (kWindow<Args>) {

@@ -184,6 +184,11 @@ struct AttnWindowArgs : AttnArgs {
   // are walked round
   int sink_chunks = 0, chunk_slabs = 0, go_round = 0;
   float *sink_pk = nullptr, *sink_pv = nullptr;
+  // the other key tiles' splits and their partial sums; units of the sums, of the splits'
+  // and in all; where the sums go
+  float *pk = nullptr, *pv = nullptr;
+  int splits = 1, part_units = 0, sum_units = 0;
+  uint16_t *dk = nullptr, *dv = nullptr;
 };
 // o [T, n_heads*d] bf16; lse [batch, n_heads, seq] fp32 (natural log).
 hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s);
