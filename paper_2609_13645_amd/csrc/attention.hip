@@ -1486,8 +1486,8 @@ __global__ __launch_bounds__(256) void attn_window_sum_k(AttnWindowArgs a, long 
   window_sums(a, (int)blockIdx.x, (int)threadIdx.x, red, ld_d);
 }
 
-// 4. dQ: block of 256 queries (32 per wave, eight waves; WIN: or 128, four) of one (batch,
-// head), 64-key tiles up to the diagonal: dQ^T += K^T dS^T, both operands
+// 4. dQ: block of 256 queries (32 per wave, eight waves; WIN: or 128, four, or 64, two and
+// KG groups of them that share the key tiles) of one (batch, head), 64-key tiles up to the diagonal: dQ^T += K^T dS^T, both operands
 // transposed reads from LDS: K^T from the natural K tile [64 keys][D], dS^T
 // from the tile's eight dS blocks (wave w's 32 queries are block w), whose
 // accumulator order holds four consecutive queries of one key in 8 bytes,
@@ -1505,13 +1505,13 @@ struct DqPlan {
   static constexpr int MEM = DmaPlan<D, NW>::PER + NDS / 64 / NW;   // DMA per wave per tile
 };
 
-template <int D, typename Args, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 1) void attn_bwd_dq_k(Args a, const bf16_t* __restrict__ ds,
-                                                       bf16_t* __restrict__ dq, long ld_d) {
+template <int D, typename Args, int WAVES, int KG>
+__global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
+    Args a, const bf16_t* __restrict__ ds, bf16_t* __restrict__ dq, long ld_d) {
   using Q = DqPlan<D, WAVES>;
   constexpr bool WIN = kWindow<Args>;
   constexpr int BQ = Q::BQ, BKV = Q::BKV, NAT = Q::NAT, NW = Q::NW, NST = Q::NST, DB = D / 32;
-  __shared__ uint4 sm[NST * Q::STAGE];
+  __shared__ uint4 sm_[KG * NST * Q::STAGE];   // (of each group of waves)
   const int S = a.seq;
   const int nqt = (S + BQ - 1) / BQ;
   // block id: kv head fastest (the dispatcher spreads consecutive ids over
@@ -1528,8 +1528,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_bwd_dq_k(Args a, const bf1
     const int blocks = nqt * a.n_heads * a.batch;
     if (id >= blocks) {
       const int t = (int)threadIdx.x;
-      window_sums(a, (id - blocks) * (WAVES / 4) + (t >> 8), t & 255,
-                  reinterpret_cast<float*>(sm) + (t >> 8) * 2048, ld_d);
+      window_sums(a, (id - blocks) * (WAVES * KG / 4) + (t >> 8), t & 255,
+                  reinterpret_cast<float*>(sm_) + (t >> 8) * 2048, ld_d);
       return;
     }
     const int i = xcd_order(id, blocks);
@@ -1545,7 +1545,12 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_bwd_dq_k(Args a, const bf1
   const bf16_t* Kg = a.k + rb * a.ld_qkv + (long)m * D;
   const bf16_t* dsh = ds + ((long)b * a.n_heads + n) * L.head;
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = 0;
+  if constexpr (KG > 1) {
+    kg = wave / NW;
+    wave %= NW;
+  }
+  uint4* sm = sm_ + kg * NST * Q::STAGE;
   const int hh = lane >> 5, l32 = lane & 31;
   const int qb0 = qt * BQ;
   const int q0w = qb0 + wave * 32;
@@ -1556,7 +1561,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_bwd_dq_k(Args a, const bf1
   const int q_last = min(qb0 + BQ, E) - 1;
   const WindowTiles win(a, qb0, q_last + 1);
   const int nkt = !WIN ? q_last / BKV + 1 : qb0 < E ? win.count : 0;
-  const auto tile_of = [&](int j) __attribute__((always_inline)) { return WIN ? win(j) : j; };
+  const auto at = [&](int j) __attribute__((always_inline)) { return KG > 1 ? j * KG + kg : j; };
+  const auto tile_of = [&](int j) __attribute__((always_inline)) { return WIN ? win(at(j)) : j; };
   uint32_t koff[DmaPlan<D, NW>::PER];
   dma_offsets<D, NW>(a.ld_qkv, wave, lane, koff);
   // dS: instruction t of wave w copies KB c = NW t + w of the tile, the
@@ -1658,17 +1664,43 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_bwd_dq_k(Args a, const bf1
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
   };
+  const int steps = (nkt + KG - 1) / KG;   // (the same for every group: the barriers)
   if (!WIN || nkt > 0) {
-    dma(tile_of(0), 0);
-    if (nkt > 1) dma(tile_of(1), 1);
-    sync(nkt > 1);
+    if (KG == 1 || kg < nkt) dma(tile_of(0), 0);
+    if (at(1) < nkt) dma(tile_of(1), 1);
+    sync(at(1) < nkt);
   }
   int st = 0;
-  for (int j = 0; j < nkt; ++j) {
-    if (j + 2 < nkt) dma(tile_of(j + 2), st == 0 ? 2 : st - 1);
-    tile(tile_of(j), st);
-    if (j + 1 < nkt) sync(j + 2 < nkt);
+  for (int j = 0; j < steps; ++j) {
+    if (at(j + 2) < nkt) dma(tile_of(j + 2), st == 0 ? 2 : st - 1);
+    if (KG == 1 || at(j) < nkt) tile(tile_of(j), st);
+    if (j + 1 < steps) sync(at(j + 2) < nkt);
     st = st == NST - 1 ? 0 : st + 1;
+  }
+  if constexpr (KG > 1) {
+    // the groups' sums to the first, in order
+    const int t = wave * 64 + lane;
+    __syncthreads();   // the last tiles are read
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < DB * 4; ++i)
+        sm[i * (NW * 64) + t] = __builtin_bit_cast(
+            uint4, make_float4(dqa[i / 4][i % 4 * 4], dqa[i / 4][i % 4 * 4 + 1],
+                               dqa[i / 4][i % 4 * 4 + 2], dqa[i / 4][i % 4 * 4 + 3]));
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int g = 1; g < KG; ++g)
+#pragma unroll
+      for (int i = 0; i < DB * 4; ++i) {
+        const float4 v =
+            __builtin_bit_cast(float4, sm_[g * NST * Q::STAGE + i * (NW * 64) + t]);
+        dqa[i / 4][i % 4 * 4] += v.x;
+        dqa[i / 4][i % 4 * 4 + 1] += v.y;
+        dqa[i / 4][i % 4 * 4 + 2] += v.z;
+        dqa[i / 4][i % 4 * 4 + 3] += v.w;
+      }
   }
   if (q < S) {
     // (WIN: rows past the tokens' end have no dS and no tiles of their own, but
@@ -1916,22 +1948,34 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
     hipLaunchKernelGGL(attn_bwd_kv_sum_k, grid, block, 0, s, k.pk, k.pv, k.splits, T, width,
                        a.scale, dk, dv, ld_d);
   }
-  const auto dq_pass = [&](auto waves) {
-    constexpr int W = decltype(waves)::value;
+  const auto dq_pass = [&](auto waves, auto groups) {
+    constexpr int W = decltype(waves)::value, G = decltype(groups)::value;
     const dim3 grid((unsigned)((a.seq + 32 * W - 1) / (32 * W) * a.n_heads * a.batch +
-                               tail / (W / 4)));
-    hipLaunchKernelGGL((attn_bwd_dq_k<D, Args, W>), grid, dim3(64 * W), 0, s, a, ds, dq, ld_d);
+                               tail / (W * G / 4)));
+    hipLaunchKernelGGL((attn_bwd_dq_k<D, Args, W, G>), grid, dim3(64 * W * G), 0, s, a, ds, dq,
+                       ld_d);
   };
+  using std::integral_constant;
   if constexpr (kWindow<Args>) {
+    // blocks of 64 queries, their key tiles in two groups, where they and the sums run at
+    // once (2048 tokens, 3 heads of 128, window 200 28.0 -> 26.3 us for the whole backward,
+    // 1500 46.3 -> 38.6; 8 heads, 256 blocks and 256 units of sums, window 200 30.8, 32.3), or
+    // the blocks alone do and have many tiles (window 600 39.6, 39.0, 1500 61.8, 57.6)
+    const long blocks = (long)((a.seq + 63) / 64) * a.n_heads * a.batch;
+    const int tiles = std::min((a.seq + 63) / 64, (a.window + 126) / 64 + (a.sinks + 63) / 64);
+    if (a.seq > 64 && blocks <= 256 && (blocks + tail <= 256 || tiles >= 12)) {
+      dq_pass(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+      return hipGetLastError();
+    }
     // blocks of 128 queries where those of 256 are fewer than CUs (1 x 2048 tokens, 8
     // heads of 128, window 256: backward 46.0 us, 40.3 with them; 2 x 2000, 16 heads,
     // window 512, 256 blocks: 113 and 116)
     if ((long)((a.seq + 255) / 256) * a.n_heads * a.batch < 256) {
-      dq_pass(std::integral_constant<int, 4>{});
+      dq_pass(integral_constant<int, 4>{}, integral_constant<int, 1>{});
       return hipGetLastError();
     }
   }
-  dq_pass(std::integral_constant<int, 8>{});
+  dq_pass(integral_constant<int, 8>{}, integral_constant<int, 1>{});
   return hipGetLastError();
 }
 }  // namespace
