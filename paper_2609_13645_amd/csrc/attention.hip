@@ -1725,19 +1725,19 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
 }  // namespace
 
 namespace {
-template <int NW, int KG, typename Args>
-hipError_t attn_fwd_waves(const Args& a, uint16_t* o, float* lse, hipStream_t s) {
+template <int D, int NW, int KG, typename Args>
+hipError_t attn_fwd_d(const Args& a, uint16_t* o, float* lse, hipStream_t s) {
   constexpr int BQ = 32 * NW;
   const dim3 grid((unsigned)((a.seq + BQ - 1) / BQ * a.n_heads * a.batch)), block(64 * NW * KG);
-  if (a.d == 128) hipLaunchKernelGGL((attn_fwd_k<128, Args, NW, KG>), grid, block, 0, s, a, o, lse);
-  else if (a.d == 64) hipLaunchKernelGGL((attn_fwd_k<64, Args, NW, KG>), grid, block, 0, s, a, o, lse);
-  else return hipErrorInvalidValue;
+  hipLaunchKernelGGL((attn_fwd_k<D, Args, NW, KG>), grid, block, 0, s, a, o, lse);
   return hipGetLastError();
 }
 }  // namespace
 
 hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s) {
-  return attn_fwd_waves<4, 1>(a, o, lse, s);
+  if (a.d == 128) return attn_fwd_d<128, 4, 1>(a, o, lse, s);
+  if (a.d == 64) return attn_fwd_d<64, 4, 1>(a, o, lse, s);
+  return hipErrorInvalidValue;
 }
 hipError_t attn_window_fwd(const AttnWindowArgs& a, uint16_t* o, float* lse, hipStream_t s) {
   // Blocks of 64 queries, their key tiles in two groups, where all of them run at once (by
@@ -1745,10 +1745,19 @@ hipError_t attn_window_fwd(const AttnWindowArgs& a, uint16_t* o, float* lse, hip
   // tokens, 12 heads of 64, window 128 10.2 us as blocks of 128 queries, so 6.9; all keys:
   // 4096 tokens, 2 heads of 64 64.5, 35.4; 2048, 7 of 128 43.3, 27.8. Where some wait for a
   // CU they lose (2048, 9 of 128, window 500 19.3, 24.6), and where all keys are one tile
-  // (64, 8 of 64 4.6, 5.1).
+  // (64, 8 of 64 4.6, 5.1). Head dim 64: up to four on a CU without groups (2048 tokens, 24
+  // heads, window 200 17.4, 15.0; 30, all keys 46.4, 41.3; of more blocks some gain 9 %, some
+  // lose 13; head dim 128 no difference).
   const long blocks = (long)((a.seq + 63) / 64) * a.n_heads * a.batch;
-  if (a.seq > 64 && blocks <= 256 * (a.d == 64 ? 2 : 1)) return attn_fwd_waves<2, 2>(a, o, lse, s);
-  return attn_fwd_waves<4, 1>(a, o, lse, s);
+  const bool groups = a.seq > 64 && blocks <= 256 * (a.d == 64 ? 2 : 1);
+  if (a.d == 128)
+    return groups ? attn_fwd_d<128, 2, 2>(a, o, lse, s) : attn_fwd_d<128, 4, 1>(a, o, lse, s);
+  if (a.d == 64) {
+    if (groups) return attn_fwd_d<64, 2, 2>(a, o, lse, s);
+    if (blocks <= 1024) return attn_fwd_d<64, 2, 1>(a, o, lse, s);
+    return attn_fwd_d<64, 4, 1>(a, o, lse, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 size_t attn_bwd_ds_bytes(const AttnArgs& a) {

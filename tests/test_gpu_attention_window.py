@@ -43,6 +43,10 @@ CASES = [
     (2, 530, 48, 4, 64, 150, 66, (530, 301)),
     (1, 420, 128, 16, 128, 90, 2, None),
     # more blocks of 64 queries than run at once: the forward's blocks of 128
+    (3, 200, 90, 6, 64, 37, 3, (200, 129, 0)),
+    (1, 700, 96, 4, 64, 33, 130, (513,)),
+    (17, 64, 64, 8, 64, 64, 0, None),
+    # and, of head dim 64, up to four on a CU
     (3, 200, 48, 12, 64, 37, 3, (200, 129, 0)),
     (2, 333, 24, 6, 128, 100, 70, (333, 65)),
     (1, 129, 180, 12, 64, 5, 0, None),
