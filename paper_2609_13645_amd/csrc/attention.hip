@@ -1725,6 +1725,10 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
 }  // namespace
 
 namespace {
+// Key tiles that a block of `queries` (a multiple of 64) has at most.
+int most_tiles(const AttnWindowArgs& a, int queries) {
+  return std::min((a.seq + 63) / 64, (a.window + queries + 62) / 64 + (a.sinks + 63) / 64);
+}
 template <int D, int NW, int KG, typename Args>
 hipError_t attn_fwd_d(const Args& a, uint16_t* o, float* lse, hipStream_t s) {
   constexpr int BQ = 32 * NW;
@@ -1747,11 +1751,17 @@ hipError_t attn_window_fwd(const AttnWindowArgs& a, uint16_t* o, float* lse, hip
   // CU they lose (2048, 9 of 128, window 500 19.3, 24.6), and where all keys are one tile
   // (64, 8 of 64 4.6, 5.1). Head dim 64: up to four on a CU without groups (2048 tokens, 24
   // heads, window 200 17.4, 15.0; 30, all keys 46.4, 41.3; of more blocks some gain 9 %, some
-  // lose 13; head dim 128 no difference).
+  // lose 13; head dim 128 no difference). Head dim 128: two groups also in blocks of 128,
+  // one on a CU, with enough tiles to share (8192, 4 heads, all keys 160.8, 130.7; 2048, 9
+  // heads, window 500 20.9, 19.9, window 200 even, window 50 11.8, 12.7).
   const long blocks = (long)((a.seq + 63) / 64) * a.n_heads * a.batch;
   const bool groups = a.seq > 64 && blocks <= 256 * (a.d == 64 ? 2 : 1);
-  if (a.d == 128)
-    return groups ? attn_fwd_d<128, 2, 2>(a, o, lse, s) : attn_fwd_d<128, 4, 1>(a, o, lse, s);
+  if (a.d == 128) {
+    if (groups) return attn_fwd_d<128, 2, 2>(a, o, lse, s);
+    if ((long)((a.seq + 127) / 128) * a.n_heads * a.batch <= 256 && most_tiles(a, 128) >= 8)
+      return attn_fwd_d<128, 4, 2>(a, o, lse, s);
+    return attn_fwd_d<128, 4, 1>(a, o, lse, s);
+  }
   if (a.d == 64) {
     if (groups) return attn_fwd_d<64, 2, 2>(a, o, lse, s);
     if (blocks <= 1024) return attn_fwd_d<64, 2, 1>(a, o, lse, s);
@@ -1971,8 +1981,7 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
     // 1500 46.3 -> 38.6; 8 heads, 256 blocks and 256 units of sums, window 200 30.8, 32.3), or
     // the blocks alone do and have many tiles (window 600 39.6, 39.0, 1500 61.8, 57.6)
     const long blocks = (long)((a.seq + 63) / 64) * a.n_heads * a.batch;
-    const int tiles = std::min((a.seq + 63) / 64, (a.window + 126) / 64 + (a.sinks + 63) / 64);
-    if (a.seq > 64 && blocks <= 256 && (blocks + tail <= 256 || tiles >= 12)) {
+    if (a.seq > 64 && blocks <= 256 && (blocks + tail <= 256 || most_tiles(a, 64) >= 12)) {
       dq_pass(integral_constant<int, 2>{}, integral_constant<int, 2>{});
       return hipGetLastError();
     }

@@ -52,6 +52,9 @@ CASES = [
     (1, 129, 180, 12, 64, 5, 0, None),
     (5, 65, 30, 2, 128, 3, 1, (65, 64, 1, 33, 65)),
     (2, 700, 24, 4, 64, 33, 130, (700, 513)),
+    # as many blocks of 128 queries as run at once, with many key tiles
+    (3, 600, 10, 2, 128, 450, 70, (600, 333, 0)),
+    (1, 1100, 20, 4, 128, 1100, 0, None),
     # many key tiles and many sums beside few blocks of 64 queries
     (1, 1500, 8, 2, 64, 1000, 0, (1437,)),
     (1, 1100, 6, 3, 128, 1100, 0, None),
