@@ -1987,8 +1987,10 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
     }
     // blocks of 128 queries where those of 256 are fewer than CUs (1 x 2048 tokens, 8
     // heads of 128, window 256: backward 46.0 us, 40.3 with them; 2 x 2000, 16 heads,
-    // window 512, 256 blocks: 113 and 116)
-    if ((long)((a.seq + 255) / 256) * a.n_heads * a.batch < 256) {
+    // window 512, 256 blocks: 113 and 116), and head dim 64, two of whose blocks a CU then
+    // holds, with narrow windows (4 x 2047, 32 heads, window 100 109.7, 104.3; 4096, 24 heads,
+    // 1024 119.4, 115.9; 8192, 16 heads, 2048 267.5, 270.6; head dim 128 2 % the other way)
+    if ((long)((a.seq + 255) / 256) * a.n_heads * a.batch < 256 || (D == 64 && a.window <= 1024)) {
       dq_pass(integral_constant<int, 4>{}, integral_constant<int, 1>{});
       return hipGetLastError();
     }
