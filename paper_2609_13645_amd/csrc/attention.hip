@@ -1744,27 +1744,32 @@ hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 hipError_t attn_window_fwd(const AttnWindowArgs& a, uint16_t* o, float* lse, hipStream_t s) {
+  const long blocks = (long)((a.seq + 63) / 64) * a.n_heads * a.batch;   // of 64 queries
   // Blocks of 64 queries, their key tiles in two groups, where all of them run at once (by
   // their LDS one on a CU for head dim 128, two for 64). 50 shapes timed both ways: 3 x 333
   // tokens, 12 heads of 64, window 128 10.2 us as blocks of 128 queries, so 6.9; all keys:
   // 4096 tokens, 2 heads of 64 64.5, 35.4; 2048, 7 of 128 43.3, 27.8. Where some wait for a
   // CU they lose (2048, 9 of 128, window 500 19.3, 24.6), and where all keys are one tile
-  // (64, 8 of 64 4.6, 5.1). Head dim 64: up to four on a CU without groups (2048 tokens, 24
-  // heads, window 200 17.4, 15.0; 30, all keys 46.4, 41.3; of more blocks some gain 9 %, some
-  // lose 13; head dim 128 no difference). Head dim 128: two groups also in blocks of 128,
-  // one on a CU, with enough tiles to share (8192, 4 heads, all keys 160.8, 130.7; 2048, 9
-  // heads, window 500 20.9, 19.9, window 200 even, window 50 11.8, 12.7).
-  const long blocks = (long)((a.seq + 63) / 64) * a.n_heads * a.batch;
+  // (64, 8 of 64 4.6, 5.1).
   const bool groups = a.seq > 64 && blocks <= 256 * (a.d == 64 ? 2 : 1);
   if (a.d == 128) {
     if (groups) return attn_fwd_d<128, 2, 2>(a, o, lse, s);
+    // Two groups also in blocks of 128, one on a CU, with enough tiles to share (8192 tokens,
+    // 4 heads, all keys 160.8 us, 130.7; 2048, 9 heads, window 500 20.9, 19.9, window 200
+    // even, window 50 11.8, 12.7).
     if ((long)((a.seq + 127) / 128) * a.n_heads * a.batch <= 256 && most_tiles(a, 128) >= 8)
       return attn_fwd_d<128, 4, 2>(a, o, lse, s);
     return attn_fwd_d<128, 4, 1>(a, o, lse, s);
   }
   if (a.d == 64) {
     if (groups) return attn_fwd_d<64, 2, 2>(a, o, lse, s);
-    if (blocks <= 1024) return attn_fwd_d<64, 2, 1>(a, o, lse, s);
+    // Blocks of 64 without groups up to four on a CU (2048 tokens, 24 heads, window 200 17.4
+    // us, 15.0; 30, all keys 46.4, 41.3), and from four rounds of those on while the window
+    // is narrow, whose far edge costs a block of 128 more (16384, 32 heads, window 512 148.0,
+    // 137.1; 8192, 12 heads, 512 31.6, 33.4; 16384, 32 heads, 8192 1012, 1055). Head dim 128:
+    // no difference up to two on a CU, slower beyond.
+    if (blocks <= 1024 || (blocks >= 4096 && a.window <= 768))
+      return attn_fwd_d<64, 2, 1>(a, o, lse, s);
     return attn_fwd_d<64, 4, 1>(a, o, lse, s);
   }
   return hipErrorInvalidValue;

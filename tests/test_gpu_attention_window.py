@@ -42,11 +42,13 @@ CASES = [
     # as many blocks of 256 queries as CUs, and more
     (2, 530, 48, 4, 64, 150, 66, (530, 301)),
     (1, 420, 128, 16, 128, 90, 2, None),
-    # more blocks of 64 queries than run at once: the forward's blocks of 128
+    # more blocks of 64 queries than run at once: the forward's blocks of 128, and the
+    # last one's many rounds of 64
     (3, 200, 90, 6, 64, 37, 3, (200, 129, 0)),
     (1, 700, 96, 4, 64, 33, 130, (513,)),
     (17, 64, 64, 8, 64, 64, 0, None),
-    # and, of head dim 64, up to four on a CU
+    (9, 450, 60, 6, 64, 120, 2, (450, 449, 0, 64, 65, 63, 300, 128, 129)),
+    # up to four of them on a CU (head dim 64)
     (3, 200, 48, 12, 64, 37, 3, (200, 129, 0)),
     (2, 333, 24, 6, 128, 100, 70, (333, 65)),
     (1, 129, 180, 12, 64, 5, 0, None),
