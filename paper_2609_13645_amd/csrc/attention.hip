@@ -659,6 +659,7 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
 // atomics, so every output is deterministic:
 //  1. attn_bwd_prep_k: per query, -delta = -rowsum(dO * O) and
 //     -LSE log2(e) (the exponent offset of P = exp(S - LSE) in base 2).
+//     (WIN: small sizes leave it to 2, template argument STATS.)
 //  2. attn_bwd_kv_k, key-owned (64 keys of a kv head per block):
 //     S = Q K^T, P, dP = dO V^T, dS = P (dP - delta); dV = sum P^T dO and
 //     dK = scale * sum dS^T Q over the GQA group; dS goes to a scratch buffer
@@ -991,7 +992,7 @@ __device__ __forceinline__ f32x16_t rows16(const bf16x8_t (&r)[4]) {
   return x;
 }
 
-template <int D, typename Args, bool CACHED>
+template <int D, typename Args, bool CACHED, bool STATS>
 __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
                                                        const bf16_t* __restrict__ dout,
                                                        const float* __restrict__ delta,
@@ -1134,7 +1135,8 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
     return w;
   };
   // DMA instruction I of a pair into a buffer: the Q slab, the dO slab, then
-  // (lanes 0-31) -LSE log2(e) and (lanes 32-63) -delta of the slab's queries
+  // (lanes 0-31) -LSE log2(e) and (lanes 32-63) -delta of the slab's queries (STATS:
+  // formed below instead)
   // (z: a zero the compiler cannot see through; the offsets of all instructions,
   // hoisted out of the loop, would not fit the registers)
   auto dma = [&](auto I, const Pair& w, uint32_t z, uint4* base) __attribute__((always_inline)) {
@@ -1147,7 +1149,7 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
       constexpr int j = i - P::PER;
       dma_16(w.o, rows * orb, base + SLAB + j * 64,
              orow + (c0 ^ fsw<D>(j * P::RPI) * 16) + (j * P::RPI * orb + z));
-    } else {
+    } else if constexpr (!STATS) {
       const long li = ((long)b * a.n_heads + w.n) * seq_of(a, S) + w.q0 + l32;
       dma_4(delta, base + 2 * SLAB,
             w.q0 + l32 < S ? (uint32_t)(((hh ? 0 : nrows) + li) * 4) : kOOB);
@@ -1380,6 +1382,36 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   uint4* mine = sm + wave * 2 * B::WBUF;
   int cur = 0;
   Pair w = pair_at(min(p0, total - 1));
+  if constexpr (STATS) {
+    // the statistics of the wave's one or two pairs, each for its buffer: two lanes to a
+    // query, half of the row of dO and O each
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int p = p0 + i * step;
+      if (p >= total) break;
+      const Pair u = pair_at(p);
+      const bool in = u.q0 + l32 < S;
+      const bf16_t* x = reinterpret_cast<const bf16_t*>(u.o) + l32 * ldo + hh * (D / 2);
+      const bf16_t* y = a.o + (x - dout);
+      float dot = 0.0f;
+      if (in) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          float f[8], g[8];
+          unpack8(*reinterpret_cast<const uint4*>(x + k * 8), f);
+          unpack8(*reinterpret_cast<const uint4*>(y + k * 8), g);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(f[e], g[e], dot);
+        }
+      }
+      dot = fa::sum_xor32(dot);
+      float v = -dot;
+      if (hh == 0)
+        v = in ? -kLog2e * a.lse[((long)b * a.n_heads + u.n) * a.seq + u.q0 + l32] : 0.0f;
+      reinterpret_cast<float*>(mine + i * B::WBUF + 2 * SLAB)[lane] = v;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the pairs' reads are inline asm)
+  }
   if (!WIN || total > 0)
     static_for<B::DMA>([&](auto I) __attribute__((always_inline)) { dma(I, w, 0, mine); });
   for (int p = p0; p < total; p += step) {
@@ -1890,7 +1922,7 @@ namespace {
 // How the kv pass divides its pairs, and where its partial sums lie in `part`.
 template <int D>
 struct KvLaunch {
-  int splits, blocks;
+  int splits, blocks, wave_pairs = 0;
   float *pk = nullptr, *pv = nullptr;
   KvLaunch(AttnArgs& a, float* part) {
     splits = kv_splits(a);
@@ -1927,6 +1959,12 @@ struct KvLaunch {
     const long width = a.n_kv_heads * D, rows = a.sink_chunks > 0 ? std::min(nst * 64, a.seq) : 0;
     a.part_units =
         splits > 1 ? (int)(((long)a.batch * a.seq * (width / 8) + 255) / 256 * 2) : 0;
+    // pairs of a wave at most, of key tiles, sink tiles and their chunks
+    const DsWindow L(a);
+    const int grp = a.n_heads / a.n_kv_heads;
+    const auto of_wave = [&](int slabs, int z) { return (grp * slabs + 4 * z - 1) / (4 * z); };
+    wave_pairs = std::max(of_wave(nst > 0 && p.chunks == 0 ? L.ns : L.nwin, splits),
+                          of_wave(p.slabs, 1));
     a.sum_units = a.part_units + (int)(rows * a.batch * ((width + 127) / 128) * 2);
   }
 };
@@ -1941,22 +1979,41 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
   const long T = (long)a.batch * a.seq;
   const dim3 pgrid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
   const dim3 kgrid((unsigned)k.blocks);
-  hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
-                     a.seq);
-  bool cached = false;
+  const auto prep = [&] {
+    hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows,
+                       a.n_heads, a.seq);
+  };
+  const auto kv_pass = [&](auto cached, auto stats) {
+    hipLaunchKernelGGL((attn_bwd_kv_k<D, Args, decltype(cached)::value, decltype(stats)::value>),
+                       kgrid, block, 0, s, a, dout, delta, ds, dv, dk, ld_d, k.pv, k.pk, k.splits);
+  };
+  using std::false_type;
+  using std::true_type;
   if constexpr (kWindow<Args>) {
     // Where the memory-side cache of 256 MB holds dS until the dQ pass reads it, ordinary
     // stores: 15 shapes timed both ways, up to 230 MB 1 to 7 % of the backward (3 x 3000
     // tokens, 24 / 8 heads of 64, window 400, 198 MB: 167 us nontemporal, 156), from 256
     // MB between 5 % gained and 19 % lost (4096 tokens, 32 / 8 of 64, 1 GB: 284, 338)
-    cached = attn_window_bwd_ds_bytes(a) <= 240u << 20;
-    if (cached)
-      hipLaunchKernelGGL((attn_bwd_kv_k<D, Args, true>), kgrid, block, 0, s, a, dout, delta, ds,
-                         dv, dk, ld_d, k.pv, k.pk, k.splits);
+    const bool cached = attn_window_bwd_ds_bytes(a) <= 240u << 20;
+    a.o = o;
+    a.lse = lse;
+    // One launch less where each wave of the kv pass has no more pairs than buffers, and
+    // forms their statistics itself (every key tile those of all queries it sees): 257 tokens,
+    // 4 / 2 heads of 64, window 64 14.0 us, 13.0; 1000, 4 / 1 of 64, all keys 23.6, 21.6; 4 x
+    // 15, 8 / 1 of 128 15.5, 14.0. More blocks than CUs do it one after another (4096 tokens,
+    // 16 heads of 128, window 60 68.6, 69.9)
+    const bool stats = cached && k.wave_pairs <= 2 && k.blocks <= 256;
+    if (stats) {
+      kv_pass(true_type{}, true_type{});
+    } else {
+      prep();
+      if (cached) kv_pass(true_type{}, false_type{});
+      else kv_pass(false_type{}, false_type{});
+    }
+  } else {
+    prep();
+    kv_pass(false_type{}, false_type{});
   }
-  if (!cached)
-    hipLaunchKernelGGL((attn_bwd_kv_k<D, Args, false>), kgrid, block, 0, s, a, dout, delta, ds, dv,
-                       dk, ld_d, k.pv, k.pk, k.splits);
   int tail = 0;   // units of the sums in the dQ pass (even: dK and dV)
   if constexpr (kWindow<Args>) {
     a.dk = dk;

@@ -189,6 +189,9 @@ struct AttnWindowArgs : AttnArgs {
   float *pk = nullptr, *pv = nullptr;
   int splits = 1, part_units = 0, sum_units = 0;
   uint16_t *dk = nullptr, *dv = nullptr;
+  // the forward's outputs
+  const uint16_t* o = nullptr;
+  const float* lse = nullptr;
 };
 // o [T, n_heads*d] bf16; lse [batch, n_heads, seq] fp32 (natural log).
 hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s);
