@@ -203,6 +203,27 @@ def test_window_of_the_whole_row_is_causal_attention(S, nh, nkv, d):
         assert float((lse2 - lse).abs().max()) <= 1e-5
 
 
+def test_the_end_of_a_row_of_over_4_gb():
+    """The last rows depend on the last ones alone: those of the oracle over these."""
+    import torch
+    S, nh, nkv, d, W, n = (1 << 22) + 100, 2, 1, 128, 70, 600
+    banner(f"window attention S={S} nh={nh} nkv={nkv} d={d} W={W}")
+    qkv = torch.randn((S, (nh + 2 * nkv) * d), dtype=torch.bfloat16, device="cuda")
+    do = torch.randn((S, nh * d), dtype=torch.bfloat16, device="cuda")
+    o, lse, dqkv = (t[..., -n:, :] if t.dim() == 2 else t[..., -n:]
+                    for t in _call(1, S, nh, nkv, d, W, 0, None, qkv, do))
+    x, g = host_f64(qkv[-n:]), host_f64(do[-n:])
+    q, k, v = _split(x, nh, nkv, d)
+    r = branch.window_attention(q, k, v, g.reshape(n, nh, d), 1, n, W, 0, None)
+    got = dict(zip(("dq", "dk", "dv"), _split(host_f64(dqkv), nh, nkv, d)),
+               o=host_f64(o).reshape(n, nh, d))
+    assert np.allclose(host_f64(lse)[..., W:], r["lse"][..., W:], rtol=0, atol=1e-5)
+    for name, y in got.items():
+        slack = 1e-5 * np.max(np.abs(g)) * np.max(np.abs(x)) ** 2
+        off, bound = np.abs(y - r[name])[W:], (1.02 * r["err_" + name] + slack)[W:]
+        assert np.all(off <= bound), f"{name}: {float(np.max(off / bound)):.2f} of its bound"
+
+
 def test_lens_outside_the_row_are_clamped():
     import torch
     banner("window attention clamped lens")
