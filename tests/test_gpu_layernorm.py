@@ -19,7 +19,9 @@ pytestmark = pytest.mark.gpu
 HALF, SUM = 2.0 ** -8, 2.0 ** -16
 EPS = 1e-5
 SIZES = [(1, 8), (1, 8192), (37, 24), (300, 520), (64, 512), (999, 2056), (130, 1000), (5, 4104),
-         (2050, 1024), (700, 4096), (9000, 264), (3, 6160)]
+         (2050, 1024), (700, 4096), (9000, 264), (3, 6160),
+         # backward: the most rows of one workgroup, and one more
+         (24, 520), (12, 1032), (6, 2056), (3, 8192), (25, 72)]
 
 
 def _bits(rng, shape, std=1.0, mean=0.0):
