@@ -1518,8 +1518,9 @@ __global__ __launch_bounds__(256) void attn_window_sum_k(AttnWindowArgs a, long 
   window_sums(a, (int)blockIdx.x, (int)threadIdx.x, red, ld_d);
 }
 
-// 4. dQ: block of 256 queries (32 per wave, eight waves; WIN: or 128, four, or 64, two and
-// KG groups of them that share the key tiles) of one (batch, head), 64-key tiles up to the diagonal: dQ^T += K^T dS^T, both operands
+// 4. dQ: block of 256 queries (32 per wave, eight waves; WIN: or 128, four, or 64,
+// two and KG groups of them that share the key tiles) of one (batch, head), 64-key
+// tiles up to the diagonal: dQ^T += K^T dS^T, both operands
 // transposed reads from LDS: K^T from the natural K tile [64 keys][D], dS^T
 // from the tile's eight dS blocks (wave w's 32 queries are block w), whose
 // accumulator order holds four consecutive queries of one key in 8 bytes,
