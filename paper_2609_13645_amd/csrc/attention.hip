@@ -891,12 +891,13 @@ __device__ __forceinline__ void dma_4(const float* base, uint4* lds, uint32_t of
 // keys) summed in wave order through sm0 / sm1, times scale, stored as bf16
 // rows out[key][D] (key-major, row stride ld) for the first nkeys keys; with
 // part (a block that holds one split of the pairs) as fp32 rows part[key][D]
-// (row stride ldp), unscaled.
+// (row stride ldp), unscaled. Keys from ntok on are padding and get zeros: their
+// sums are of 0 * dO and 0 * Q, NaN where a token's row of these is not finite.
 template <int D>
 __device__ __forceinline__ void kv_reduce_store(const f32x16_t (&acc)[D / 32][2], uint4* sm0,
                                                 uint4* sm1, int wave, int lane, float scale,
                                                 bf16_t* out, long ld, float* part, long ldp,
-                                                int nkeys) {
+                                                int nkeys, int ntok) {
   using P = KvPlan<D>;
   constexpr int DB = D / 32;
   const int hh = lane >> 5, l32 = lane & 31;
@@ -918,6 +919,7 @@ __device__ __forceinline__ void kv_reduce_store(const f32x16_t (&acc)[D / 32][2]
   const int key = threadIdx.x >> 2;
   const int piece = threadIdx.x & 3;
   if (key < nkeys) {
+    const uint32_t keep = key < ntok ? ~0u : 0u;   // (a mask: as a choice, a branch for each)
     const float* w0 = reinterpret_cast<const float*>(sm0);
     const float* w1 = reinterpret_cast<const float*>(sm0 + P::RED);
     const float* w2 = reinterpret_cast<const float*>(sm1);
@@ -927,7 +929,10 @@ __device__ __forceinline__ void kv_reduce_store(const f32x16_t (&acc)[D / 32][2]
       const int o = key * (D + 4) + j * 32 + piece * 8;
       float f[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) f[u] = ((w0[o + u] + w1[o + u]) + w2[o + u]) + w3[o + u];
+      for (int u = 0; u < 8; ++u) {
+        f[u] = ((w0[o + u] + w1[o + u]) + w2[o + u]) + w3[o + u];
+        f[u] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, f[u]) & keep);
+      }
       if (part) {
         float4* prow = reinterpret_cast<float4*>(part + (long)key * ldp + piece * 8 + j * 32);
         prow[0] = make_float4(f[0], f[1], f[2], f[3]);
@@ -1424,11 +1429,11 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   if (dsblk) store_ds();
   kv_reduce_store<D>(acc, sm, sm + 2 * P::RED, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D,
                      ld_d, kv_part<D, true>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D,
-                     seq_of(a, S) - k0);
+                     seq_of(a, S) - k0, S - k0);
   kv_reduce_store<D>(acck, sm, sm + 2 * P::RED, wave, lane, a.scale,
                      dk + (rb + k0) * ld_d + (long)m * D, ld_d,
                      kv_part<D, false>(a, pk, kb_, rb + k0), (long)a.n_kv_heads * D,
-                     seq_of(a, S) - k0);
+                     seq_of(a, S) - k0, S - k0);
 }
 
 // dK and dV from the splits' partial sums, added in split order; eight columns

@@ -271,3 +271,44 @@ def test_results_repeat_bit_for_bit():
     for _ in range(2):
         again = _call(B, S, nh, nkv, d, 100, 70, (900, 640), qkv, do)
         assert all(torch.equal(a, b) for a, b in zip(again, first))
+
+
+@pytest.mark.parametrize("B,S,nh,nkv,d,W,sinks,lens", [
+    (3, 200, 4, 2, 64, 40, 3, (200, 90, 0)),
+    (3, 200, 4, 2, 128, 40, 3, (200, 90, 0)),
+    # sums of partials: of splits, of the chunks of what the sinks see
+    (2, 1000, 8, 2, 64, 300, 70, (333, 1000)),
+    (2, 1500, 8, 2, 128, 100, 70, (1409, 1500)),
+    (2, 700, 48, 4, 128, 64, 0, (65, 700)),
+])
+def test_infinities_stay_in_their_batch_row_and_kv_head(B, S, nh, nkv, d, W, sinks, lens):
+    """A token's NaN or infinity, in q, k, v or d_o of the first heads of batch row b, leaves
+    the other batch rows and kv heads as they are, bit for bit, and padding rows zeros."""
+    import torch
+    banner(f"window attention infinities B={B} S={S} nh={nh} nkv={nkv} d={d} W={W} sinks={sinks}")
+    hq, hkv, grp = nh * d, nkv * d, nh // nkv
+    b = 1 if lens[1] < S else 0
+    qkv = torch.randn((B * S, hq + 2 * hkv), device="cuda").to(torch.bfloat16)
+    do = torch.randn((B * S, hq), device="cuda").to(torch.bfloat16)
+    clean = _call(B, S, nh, nkv, d, W, sinks, lens, qkv, do)
+    pad = torch.from_numpy(_pad_rows(B, S, lens)).cuda()
+    # rows that share a tile of keys with the padding, and the row's first
+    at = [b * S, b * S + lens[b] - 1]
+    for what, col in (("q", 0), ("k", hq), ("v", hq + hkv), ("d_o", None)):
+        for value in (float("inf"), float("nan")):
+            x, g = qkv.clone(), do.clone()
+            if col is None:
+                g[at, :d] = value
+            else:
+                x[at, col:col + d] = value
+            o, lse, dqkv = _call(B, S, nh, nkv, d, W, sinks, lens, x, g)
+            assert not o[pad].any() and not dqkv[pad].any(), (what, value)
+            other = torch.arange(B * S, device="cuda") // S != b
+            assert torch.equal(o[other], clean[0][other]), (what, value)
+            assert torch.equal(dqkv[other], clean[2][other]), (what, value)
+            assert torch.equal(o[:, grp * d:], clean[0][:, grp * d:]), (what, value)
+            assert torch.equal(lse[:, grp:], clean[1][:, grp:]), (what, value)
+            for lo, hi in ((grp * d, hq), (hq + d, hq + hkv), (hq + hkv + d, hq + 2 * hkv)):
+                assert torch.equal(dqkv[:, lo:hi], clean[2][:, lo:hi]), (what, value)
+            # (the row itself does show it)
+            assert not torch.isfinite(dqkv[b * S:b * S + lens[b]]).all(), (what, value)
