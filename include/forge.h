@@ -739,7 +739,8 @@ typedef struct {
  * padded batch), clamped to [0, seq]; NULL: seq each. Padding rows of qkv are
  * not read and visible to no query; their rows of o are written as zeros and
  * their lse as -infinity. (Among the tokens of a row, a NaN or an infinity in
- * v may reach rows that do not see it, as 0 * NaN.) One token is a valid row.
+ * v may reach rows that do not see it, as 0 * NaN, in the query heads of its kv
+ * head; one in k reaches only rows that see it.) One token is a valid row.
  */
 forge_status forge_attention_window_fwd(const forge_attn_window_cfg* cfg, const forge_bf16* qkv,
                                         const int32_t* seq_lens, forge_bf16* o, float* lse,
@@ -756,7 +757,11 @@ forge_status forge_attention_window_bwd_workspace_bytes(const forge_attn_window_
  * Backward, as forge_attention_bwd over the visible pairs: from d_o [T, hq]
  * bf16 and the forward's qkv, seq_lens, o, lse, writes d_qkv [T, hq+2hkv] bf16
  * (=), which must not overlap qkv, o or d_o. Padding rows of d_o are not used,
- * those of d_qkv are written as zeros. No atomics: bitwise deterministic.
+ * those of d_qkv are written as zeros. (Among the tokens of a batch row, a NaN or
+ * an infinity in q, k, v, o, lse or d_o may reach, as 0 * NaN, the gradients of
+ * tokens that it does not see or that do not see it, within its kv head and the
+ * query heads of that; it reaches no other batch row, no other kv head's and no
+ * padding row.) No atomics: bitwise deterministic.
  */
 forge_status forge_attention_window_bwd(const forge_attn_window_cfg* cfg, const forge_bf16* qkv,
                                         const int32_t* seq_lens, const forge_bf16* o,

@@ -312,3 +312,32 @@ def test_infinities_stay_in_their_batch_row_and_kv_head(B, S, nh, nkv, d, W, sin
                 assert torch.equal(dqkv[:, lo:hi], clean[2][:, lo:hi]), (what, value)
             # (the row itself does show it)
             assert not torch.isfinite(dqkv[b * S:b * S + lens[b]]).all(), (what, value)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_backward_of_a_forward_result_that_is_not_finite(d):
+    """The same of o and lse as the backward takes them, in both forms of the row sums."""
+    import torch
+    from paper_2609_13645_amd import _lib
+    banner(f"window attention infinities of o and lse d={d}")
+    for B, S, nh, nkv, W, lens in ((2, 200, 4, 2, 40, (200, 90)), (2, 1000, 48, 4, 300, (650, 999))):
+        hq, hkv, grp = nh * d, nkv * d, nh // nkv
+        qkv = torch.randn((B * S, hq + 2 * hkv), device="cuda").to(torch.bfloat16)
+        do = torch.randn((B * S, hq), device="cuda").to(torch.bfloat16)
+        o, lse, clean = _call(B, S, nh, nkv, d, W, 3, lens, qkv, do)
+        cfg = _lib.AttnWindowCfg(B, S, nh, nkv, d, W, 3)
+        pad = torch.from_numpy(_pad_rows(B, S, lens)).cuda()
+        at = S + lens[1] - 1
+        for bad in (float("inf"), float("nan"), float("-inf")):
+            o2, lse2 = o.clone(), lse.clone()
+            o2[at - 5, :d] = bad
+            lse2[1, 0, lens[1] - 1] = bad
+            got = torch.full_like(qkv, float("nan"))
+            ws = torch.full((_lib.forge_attention_window_bwd_workspace_bytes(cfg) // 4,),
+                            float("nan"), device="cuda")
+            _lib.forge_attention_window_bwd(cfg, qkv, _dev(lens), o2, lse2, do, got, ws)
+            torch.cuda.synchronize()
+            assert not got[pad].any()
+            assert torch.equal(got[:S], clean[:S])
+            for lo, hi in ((grp * d, hq), (hq + d, hq + hkv), (hq + hkv + d, hq + 2 * hkv)):
+                assert torch.equal(got[:, lo:hi], clean[:, lo:hi])
