@@ -746,10 +746,11 @@ forge_status forge_attention_window_fwd(const forge_attn_window_cfg* cfg, const 
                                         const int32_t* seq_lens, forge_bf16* o, float* lse,
                                         forge_stream stream);
 
-/* Scratch bytes of forge_attention_window_bwd: per-query statistics and the
- * score gradient in bf16, of each head a band of about seq x (window + 64) and
- * seq for each of ceil(sinks / 64) * 64 keys, and where few blocks would share the
- * work partial sums of dK and dV. Host only. */
+/* Scratch bytes of forge_attention_window_bwd: per-query statistics; the score
+ * gradient in bf16, of each head a band of about seq x (window + 64) and all later
+ * queries of ceil(sinks / 64) * 64 keys, cut at the sequence's end (no more than
+ * that of forge_attention_bwd); and where few blocks would share the work partial
+ * sums of dK and dV. Host only. */
 forge_status forge_attention_window_bwd_workspace_bytes(const forge_attn_window_cfg* cfg,
                                                         size_t* bytes);
 

@@ -694,28 +694,22 @@ struct DsLayout {
   __host__ __device__ long block(int kt, int j) const { return tile(kt) + 2048L * (j - 2 * kt); }
 };
 
-// WIN: a sink tile (kt < nst) has a block for every slab of the sequence, the
-// others for the nwin slabs from 2 kt on that its keys' windows can reach.
-struct DsWindow {
-  int ns, nst, nwin;
-  long head;
-  __host__ __device__ explicit DsWindow(const AttnWindowArgs& a) {
-    ns = (a.seq + 31) / 32;
-    nst = (a.sinks + 63) / 64;
-    nwin = (62 + a.window) / 32 + 1;
-    if (nwin > ns) nwin = ns;
-    head = 2048L * ((long)nst * ns + (long)((a.seq + 63) / 64 - nst) * nwin);
-  }
-  // the tile's first block and the slab it belongs to
-  __host__ __device__ long tile(int kt) const {
-    return 2048L * (kt < nst ? (long)kt * ns : (long)nst * ns + (long)(kt - nst) * nwin);
-  }
-  __host__ __device__ int first(int kt) const { return kt < nst ? 0 : 2 * kt; }
-  __host__ __device__ long block(int kt, int j) const { return tile(kt) + 2048L * (j - first(kt)); }
-};
+// WIN: DsWindow (kernels.h), worked out on the host.
+static DsWindow ds_window(const AttnWindowArgs& a) {
+  DsWindow L;
+  L.ns = (a.seq + 31) / 32;
+  L.nst = (a.sinks + 63) / 64;
+  L.nwin = std::min((62 + a.window) / 32 + 1, L.ns);
+  L.cut = std::max((L.ns - L.nwin + 1) / 2, L.nst);
+  const auto half = [&](long kt) { return kt * (L.ns + 1 - kt); };
+  L.band = half(L.nst) - (long)L.nst * L.nwin;
+  L.tail = L.band + (long)L.cut * L.nwin - half(L.cut);
+  L.head = L.tile((a.seq + 63) / 64);
+  return L;
+}
 
 __device__ __forceinline__ DsLayout ds_layout(const AttnArgs& a) { return DsLayout(a.seq); }
-__device__ __forceinline__ DsWindow ds_layout(const AttnWindowArgs& a) { return DsWindow(a); }
+__device__ __forceinline__ const DsWindow& ds_layout(const AttnWindowArgs& a) { return a.ds; }
 
 // 1. -delta and -LSE log2(e) of every (batch, head, query): D / 8 lanes per
 // (token, head) row of dO and O, 16-byte loads (the heads of a token are
@@ -809,7 +803,7 @@ struct KvWindowBlock {
   int j0, ns, len;         // slabs of the block; tokens of the batch row
   int turn;                // the first slab walked is j0 + turn - 1 (0: j0 + ns - 1)
   __device__ __forceinline__ KvWindowBlock(const AttnWindowArgs& a, int splits) {
-    const DsWindow L(a);
+    const DsWindow& L = a.ds;
     const int nkt = (a.seq + 63) / 64, bm = a.batch * a.n_kv_heads;
     const int far = L.nst * a.sink_chunks * bm;
     int id = (int)blockIdx.x, chunk = -1, r;
@@ -1609,13 +1603,11 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
   auto dma = [&](int kt, int st) __attribute__((always_inline)) {
     uint4* stg = sm + st * Q::STAGE;
     dma_tile_at<D, NW>(Kg, a.ld_qkv, kt * BKV, E, stg, wave, koff);
-    // block of slab qb0 / 32 in the tile (>= -6), first block and blocks of it
-    int jb = qb0 / 32 - 2 * kt, lo = 0, nb = L.ns - 2 * kt;
+    // block of slab qb0 / 32 in the tile (>= -6) and blocks of it
+    const int jb = qb0 / 32 - 2 * kt;
+    int nb = L.ns - 2 * kt;
     if constexpr (WIN) {
-      const int first = L.first(kt);
-      jb = qb0 / 32 - first;
-      lo = 2 * kt - first;
-      nb = (E + 31) / 32 - first;
+      nb = (E + 31) / 32 - 2 * kt;
       if (kt >= L.nst) nb = min(nb, L.nwin);
     }
     const __amdgpu_buffer_rsrc_t r = rsrc_n(dsh + L.tile(kt), 4096L * nb);
@@ -1626,7 +1618,7 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
       // non-temporal (cache policy 2): dS is read once here; K stays in L2
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           r, (lds_ptr_t)(stg + NAT + c * 64), 16,
-          blk < lo ? kOOB : (uint32_t)((2048 * blk + ((c & 3) * 64 + lane) * 8) * 2), 0, 0, 2);
+          blk < 0 ? kOOB : (uint32_t)((2048 * blk + ((c & 3) * 64 + lane) * 8) * 2), 0, 0, 2);
     }
   };
   // per-lane offsets: K^T fragments of column block db; the wave's dS^T
@@ -1817,7 +1809,7 @@ size_t attn_bwd_ds_bytes(const AttnArgs& a) {
   return (size_t)a.batch * a.n_heads * DsLayout(a.seq).head * 2;
 }
 size_t attn_window_bwd_ds_bytes(const AttnWindowArgs& a) {
-  return (size_t)a.batch * a.n_heads * DsWindow(a).head * 2;
+  return (size_t)a.batch * a.n_heads * ds_window(a).head * 2;
 }
 
 // Splits of a key-owned block's pairs: the smallest estimate of the kv pass. One
@@ -1878,7 +1870,7 @@ struct WindowPlan {
 static WindowPlan window_plan(const AttnWindowArgs& a) {
   constexpr double kCUs = 256.0, kSumUs = 1.0, kPartBytesPerUs = 3.0e6;
   const double kPairUs = a.d == 128 ? 3.0 : 1.5, kBlockUs = a.d == 128 ? 1.5 : 4.5;
-  const DsWindow L(a);
+  const DsWindow L = ds_window(a);
   const long grp = a.n_heads / a.n_kv_heads, bm = (long)a.batch * a.n_kv_heads;
   const long nkt = (a.seq + 63) / 64, pairs = grp * L.nwin, far = L.nst > 0 ? L.ns - L.nwin : 0;
   const double width = (double)a.n_kv_heads * a.d;
@@ -1941,7 +1933,8 @@ struct KvLaunch {
   KvLaunch(AttnWindowArgs& a, float* part) {
     const WindowPlan p = window_plan(a);
     splits = p.splits;
-    const int nst = (a.sinks + 63) / 64, bm = a.n_kv_heads * a.batch;
+    const DsWindow L = a.ds = ds_window(a);
+    const int nst = L.nst, bm = a.n_kv_heads * a.batch;
     blocks = ((a.seq + 63) / 64 * splits + nst * p.chunks) * bm;
     if (p.part) {
       pk = part;
@@ -1953,7 +1946,7 @@ struct KvLaunch {
     // 32 / 8, window 1024, 13 MB: 980 -> 940), below it costs 2 % (1 x 4096, 32 / 8,
     // window 512, 5 MB: 179 -> 183)
     const long batch = std::min(a.batch, 32), tiles = (32 + batch - 1) / batch;
-    const long slabs = batch * (2 * tiles + DsWindow(a).nwin);
+    const long slabs = batch * (2 * tiles + L.nwin);
     a.go_round = slabs * (a.n_heads / a.n_kv_heads) * 128 * D > 6L << 20;
     a.sink_chunks = p.chunks;
     a.chunk_slabs = p.slabs;
@@ -1966,7 +1959,6 @@ struct KvLaunch {
     a.part_units =
         splits > 1 ? (int)(((long)a.batch * a.seq * (width / 8) + 255) / 256 * 2) : 0;
     // pairs of a wave at most, of key tiles, sink tiles and their chunks
-    const DsWindow L(a);
     const int grp = a.n_heads / a.n_kv_heads;
     const auto of_wave = [&](int slabs, int z) { return (grp * slabs + 4 * z - 1) / (4 * z); };
     wave_pairs = std::max(of_wave(nst > 0 && p.chunks == 0 ? L.ns : L.nwin, splits),

@@ -172,6 +172,20 @@ struct AttnArgs {
   static constexpr int window = 0, sinks = 0;
   static constexpr const int32_t* lens = nullptr;
 };
+// Where a sliding window's backward keeps dS, of each (batch, head): for every key tile
+// kt of 64 a block of 2048 elements for each slab of 32 queries from 2 kt on that is
+// stored, and no more: of a sink tile (kt < nst) all ns - 2 kt, of the others the nwin
+// slabs that its keys' windows can reach, from tile cut on fewer, as the sequence ends.
+struct DsWindow {
+  int ns = 0, nst = 0, nwin = 0, cut = 0;
+  long band = 0, tail = 0;   // added by tile() from tile nst and from tile cut on
+  long head = 0;             // elements of a (batch, head)
+  __host__ __device__ long tile(int kt) const {
+    const bool full = kt > nst && kt <= cut;
+    return 2048L * ((long)kt * (full ? nwin : ns + 1 - kt) + (kt <= nst ? 0 : full ? band : tail));
+  }
+  __host__ __device__ long block(int kt, int j) const { return tile(kt) + 2048L * (j - 2 * kt); }
+};
 // Sliding window: key j is visible to query i iff j <= i and (j > i - window or
 // j < sinks); 1 <= window <= seq, 0 <= sinks <= seq. lens (device int32 [batch],
 // may be NULL): tokens of each batch row, clamped to [0, seq]; the rows behind
@@ -179,9 +193,10 @@ struct AttnArgs {
 struct AttnWindowArgs : AttnArgs {
   int window, sinks;
   const int32_t* lens;
-  // set by the backward: chunks of the sink tiles' slabs behind their own windows (0:
-  // none), slabs of each, and the sink tiles' partial sums; whether a key tile's slabs
-  // are walked round
+  // set by the backward: where dS lies; chunks of the sink tiles' slabs behind their own
+  // windows (0: none), slabs of each, and the sink tiles' partial sums; whether a key
+  // tile's slabs are walked round
+  DsWindow ds;
   int sink_chunks = 0, chunk_slabs = 0, go_round = 0;
   float *sink_pk = nullptr, *sink_pv = nullptr;
   // the other key tiles' splits and their partial sums; units of the sums, of the splits'

@@ -201,3 +201,24 @@ def test_window_workspace_is_a_band():
     same = [_lib.forge_attention_window_bwd_workspace_bytes(acfg(window=n, sinks=s))
             for n, s in ((256, 256), ((1 << 31) - 1, (1 << 31) - 1))]
     assert same[0] == same[1]
+
+
+@pytest.mark.parametrize("seq,heads,window,sinks,blocks", [
+    # 4 KB blocks of 64 keys x 32 queries of each head: all that a causal tile has
+    (16384, 32, 16384, 0, 256 * 512 - 256 * 255), (16384, 32, 1, 16384, 256 * 512 - 256 * 255),
+    (16384, 32, 16384, 16384, 256 * 512 - 256 * 255), (3000, 20, 3000, 2, 47 * 94 - 47 * 46),
+    # a band that the sequence's end cuts, and the rest of the sinks' rows
+    (16384, 32, 8192, 16, 512 + sum(min(258, 512 - 2 * t) for t in range(1, 256))),
+    (2050, 64, 1500, 2, 65 + sum(min(49, 65 - 2 * t) for t in range(1, 33))),
+    (4128, 16, 100, 130, 129 + 127 + 125 + sum(min(6, 129 - 2 * t) for t in range(3, 65)))])
+def test_window_workspace_holds_the_stored_score_gradient_alone(seq, heads, window, sinks, blocks):
+    """... beside the statistics, 8 bytes a query and head, and partial sums of up to 192 MB."""
+    need = heads * (4096 * blocks + 8 * seq)
+    got = _lib.forge_attention_window_bwd_workspace_bytes(
+        _lib.AttnWindowCfg(1, seq, heads, heads // 4, 64, window, sinks))
+    whole = _lib.forge_attention_bwd_workspace_bytes(_lib.AttnCfg(1, seq, heads, heads // 4, 64))
+    assert need <= got <= need + (192 << 20)
+    if window >= seq:
+        # no sinks before any window, so no sums of theirs
+        assert got <= whole + (192 << 20)
+        assert seq < 16384 or got <= whole

@@ -341,3 +341,21 @@ def test_backward_of_a_forward_result_that_is_not_finite(d):
             assert torch.equal(got[:S], clean[:S])
             for lo, hi in ((grp * d, hq), (hq + d, hq + hkv), (hq + hkv + d, hq + 2 * hkv)):
                 assert torch.equal(got[:, lo:hi], clean[:, lo:hi])
+
+
+@pytest.mark.parametrize("B,S,nh,nkv,d,W,sinks,lens", [
+    # windows and sinks that reach the end of the sequence: before, at and behind the key
+    # tile from which it cuts them, with an odd number of 32 queries and an even one
+    (1, 700, 4, 1, 64, 400, 130, None),
+    (1, 161, 4, 2, 128, 90, 70, (150,)),
+    (2, 97, 2, 1, 64, 60, 1, None),
+    (1, 1100, 6, 3, 64, 700, 1100, (1037,)),
+    (1, 640, 4, 1, 128, 320, 64, None),
+    (2, 640, 4, 4, 64, 2, 321, (640, 577)),
+    (1, 450, 8, 2, 128, 449, 385, None),
+    # more of the score gradient than the memory-side cache holds
+    (1, 2050, 64, 4, 64, 1500, 2, None),
+    (1, 2050, 64, 4, 128, 2050, 0, (2011,)),
+])
+def test_parity_where_the_end_of_the_sequence_cuts_windows(B, S, nh, nkv, d, W, sinks, lens):
+    test_parity(B, S, nh, nkv, d, W, sinks, lens)
