@@ -1989,10 +1989,12 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
   using std::true_type;
   if constexpr (kWindow<Args>) {
     // Where the memory-side cache of 256 MB holds dS until the dQ pass reads it, ordinary
-    // stores: 15 shapes timed both ways, up to 230 MB 1 to 7 % of the backward (3 x 3000
-    // tokens, 24 / 8 heads of 64, window 400, 198 MB: 167 us nontemporal, 156), from 256
-    // MB between 5 % gained and 19 % lost (4096 tokens, 32 / 8 of 64, 1 GB: 284, 338)
-    const bool cached = attn_window_bwd_ds_bytes(a) <= 240u << 20;
+    // stores: 28 shapes timed both ways, up to 252 MB 1 to 10 % of the backward (3 x 3000
+    // tokens, 24 / 8 heads of 64, window 400, 184 MB: 157 us nontemporal, 147), from 260 to
+    // 310 MB between 6 % gained and 5 % lost, at 390 MB 1 to 7 % lost (4096 tokens, 24 / 8 of
+    // 64, all keys: 223, 238). MB of 2^20, of all batch rows at full length: their tokens are
+    // known on the device alone
+    const bool cached = attn_window_bwd_ds_bytes(a) <= 256u << 20;
     a.o = o;
     a.lse = lse;
     // One launch less where each wave of the kv pass has no more pairs than buffers, and
