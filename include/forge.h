@@ -338,10 +338,11 @@ forge_status forge_rope_axes_table(const forge_rope_axes_cfg* cfg, int32_t n_pos
  * Rotates the first n_rot heads of each row of x [T, ldx] bf16 (head r at
  * columns r*head_dim ..) into the same heads of y [T, ldy]; other columns of y
  * are left as they are. y may be x (in place, ldy == ldx), else the two must
- * not overlap. positions: device int32 [n_axes, T], axis a's position of every
- * token, clamped to [0, n_positions). inverse != 0 rotates back (the backward:
- * x the gradient). ldx, ldy % 8 == 0 and >= n_rot * head_dim; T * n_rot *
- * head_dim / 16 < 2^31; positions 4-byte aligned.
+ * not overlap, each taken from its first rotated element to its last (so other
+ * columns of x's own rows are refused too). positions: device int32 [n_axes, T],
+ * axis a's position of every token, clamped to [0, n_positions). inverse != 0
+ * rotates back (the backward: x the gradient). ldx, ldy % 8 == 0 and >= n_rot *
+ * head_dim; T * n_rot * head_dim / 16 < 2^31; positions 4-byte aligned.
  */
 forge_status forge_rope_axes_apply(const forge_rope_axes_cfg* cfg, const forge_bf16* x,
                                    int64_t ldx, forge_bf16* y, int64_t ldy, const float* rope_cos,

@@ -17,9 +17,10 @@
 namespace forge {
 namespace {
 
-// A row belongs to WPR waves with CH 16-byte chunks per lane. Bound by HBM: 16384 x
-// 4096 51 us for 268 MB (5.2 TB/s; with one wave to a row 60), 16384 x 2048 26.7 (28.9);
-// few rows by the latency of a row: 64 x 4096 3.5 us (6.0), 1 x 8192 4.1 (8.3).
+// A row belongs to WPR waves with CH 16-byte chunks per lane. Bound by memory:
+// 16384 x 4096 50 us for 268 MB (5.4 TB/s, above a large copy's 4.9: the memory-side
+// cache has a part; with one wave to a row 60), 16384 x 2048 26.7 (28.9); few rows by
+// the latency of a row: 64 x 4096 3.5 us (6.0), 1 x 8192 4.1 (8.3).
 template <int CH, int WPR>
 __global__ __launch_bounds__(256) void layernorm_fwd_k(const bf16_t* __restrict__ x,
                                                        const bf16_t* __restrict__ g,
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(256) void layernorm_fwd_k(const bf16_t* __restrict_
 // keeps few registers (the columns' shares of dg and db, the row and the next one,
 // whose loads are in flight while this one is reduced); a workgroup's NW / WPR row
 // groups take rows grid-strided and end with their sums in part [gridDim.x][2][h].
-// Bound by HBM: 16384 x 4096, residual included, 103 us for 537 MB (5.2 TB/s; with a
+// Bound by memory: 16384 x 4096, residual included, 102 us for 537 MB (5.3 TB/s; with a
 // wave per row, whose 8 chunks a lane left one row's loads in flight, 233 us).
 // Narrow rows come near the vector units, 13 operations an element (x r - m r as one
 // fma, a 13th less, is no faster at any of 11 shapes and off by 2^-24 |m| r where x - m
