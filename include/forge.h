@@ -351,6 +351,70 @@ forge_status forge_rope_axes_apply(const forge_rope_axes_cfg* cfg, const forge_b
                                    int32_t inverse, forge_stream stream);
 
 /*
+ * Rotary positions on a part of each head, with scaled frequencies: columns
+ * [rot_offset, rot_offset + rot_dim) of a head are turned, r = rot_dim / 2
+ * pairs of them, the others are passed through.
+ *   interleaved == 0: pair i is columns (i, i + r) of the part (halves);
+ *   interleaved != 0: columns (2i, 2i + 1).
+ * Pair i turns by w_i per position, from w = base^(-2i / rot_dim):
+ *   FORGE_ROPE_SCALE_NONE    w
+ *   FORGE_ROPE_SCALE_LINEAR  w / factor (positions interpolated)
+ *   FORGE_ROPE_SCALE_BASE    w with base factor^(rot_dim / (rot_dim - 2)) times
+ *                            as large: the slowest pair is that of LINEAR, the
+ *                            fastest as it was (rot_dim > 2)
+ *   FORGE_ROPE_SCALE_PARTS   w (g + (1 - g) / factor), g = (t - low_turns) /
+ *                            (high_turns - low_turns) cut to [0, 1], of the
+ *                            turns t = original_positions w / 2 pi that the pair
+ *                            makes in the context the model was trained on: fast
+ *                            pairs stay, slow ones are interpolated
+ * amplitude multiplies every cos and sin (the attention temperature that goes
+ * with a longer context; 1 for a plain rotation).
+ * Rules (else INVALID_ARG): head_dim a multiple of 8, 8 <= head_dim <= 512;
+ * rot_dim and rot_offset even, rot_dim >= 2, rot_offset >= 0, together at most
+ * head_dim; factor > 0; PARTS: 0 <= low_turns < high_turns,
+ * original_positions >= 1; amplitude finite and > 0. What a scaling does not
+ * use is ignored.
+ */
+#define FORGE_ROPE_SCALE_NONE 0
+#define FORGE_ROPE_SCALE_LINEAR 1
+#define FORGE_ROPE_SCALE_BASE 2
+#define FORGE_ROPE_SCALE_PARTS 3
+typedef struct {
+  int32_t head_dim, rot_dim, rot_offset, interleaved;
+  int32_t scaling, original_positions;
+  float factor, low_turns, high_turns, amplitude;
+} forge_rope_part_cfg;
+
+/*
+ * Tables [n_positions, rot_dim/2] fp32 of amplitude cos and amplitude sin of
+ * position p's angle p w_i, computed in fp64. pair_factors: host fp32
+ * [rot_dim/2], each > 0, or NULL: w_i is divided by pair i's, after the scaling.
+ * Fill once per configuration and base. n_positions * rot_dim / 2 < 2^31.
+ */
+forge_status forge_rope_part_table(const forge_rope_part_cfg* cfg, const float* pair_factors,
+                                   int32_t n_positions, float base, float* cos_out,
+                                   float* sin_out, forge_stream stream);
+
+/*
+ * Rotates the first n_rot heads of each row of x [T, ldx] bf16 (head r at
+ * columns r*head_dim ..) into the same heads of y [T, ldy], fp32 math, one
+ * rounding; the columns of these heads outside the part are copied, other
+ * columns of y left as they are. y may be x (in place, ldy == ldx), else the two
+ * must not overlap, each taken from its first rotated element to its last.
+ * positions: device int32 [T], clamped to [0, n_positions); NULL: a token's index
+ * modulo n_positions. backward != 0: the gradient's way back (the transposed
+ * matrix; with amplitude 1 the inverse rotation), x the gradient. ldx, ldy % 8
+ * == 0 and >= n_rot * head_dim; T * n_rot * head_dim < 2^31 (else UNSUPPORTED);
+ * positions 4-byte aligned. A token's other heads and other tokens are not
+ * touched by a NaN or an infinity in one head, nor are other pairs of it.
+ */
+forge_status forge_rope_part_apply(const forge_rope_part_cfg* cfg, const forge_bf16* x,
+                                   int64_t ldx, forge_bf16* y, int64_t ldy, const float* rope_cos,
+                                   const float* rope_sin, const int32_t* positions,
+                                   int32_t tokens, int32_t n_positions, int32_t n_rot,
+                                   int32_t backward, forge_stream stream);
+
+/*
  * SwiGLU (App. B): gu [T, 2f] bf16 holds the gate G (columns 0..f-1) and up
  * U (columns f..2f-1) of each row; a [T, f] bf16 = bf16(silu(G) * U) with
  * silu(z) = z / (1 + exp(-z)) in fp32. f % 8 == 0; a must not overlap gu.

@@ -104,6 +104,17 @@ class RopeAxesCfg(ctypes.Structure):
                 ("own_ladder", ctypes.c_int32)]
 
 
+# frequencies of rotary positions (forge_rope_part_cfg)
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+class RopePartCfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("head_dim", "rot_dim", "rot_offset", "interleaved", "scaling",
+                 "original_positions")] + [
+        (n, ctypes.c_float) for n in ("factor", "low_turns", "high_turns", "amplitude")]
+
+
 _lib = None
 
 
@@ -150,6 +161,10 @@ def load():
         "forge_rope_axes_table": (ctypes.c_int, [ctypes.POINTER(RopeAxesCfg), I32, F32, P, P,
                                                  P]),
         "forge_rope_axes_apply": (ctypes.c_int, [ctypes.POINTER(RopeAxesCfg), P, I64, P, I64, P,
+                                                 P, P, I32, I32, I32, I32, P]),
+        "forge_rope_part_table": (ctypes.c_int, [ctypes.POINTER(RopePartCfg),
+                                                 ctypes.POINTER(F32), I32, F32, P, P, P]),
+        "forge_rope_part_apply": (ctypes.c_int, [ctypes.POINTER(RopePartCfg), P, I64, P, I64, P,
                                                  P, P, I32, I32, I32, I32, P]),
         "forge_swiglu_fwd": (ctypes.c_int, [P, P, I32, I32, P]),
         "forge_swiglu_bwd": (ctypes.c_int, [P, P, P, I32, I32, P]),
@@ -279,6 +294,15 @@ def rope_axes_cfg(c: dict) -> RopeAxesCfg:
         raise ValueError(f"at most {ROPE_MAX_AXES} axes (got {len(pairs)})")
     return RopeAxesCfg(c["head_dim"], len(pairs), (ctypes.c_int32 * ROPE_MAX_AXES)(*pairs),
                        int(bool(c.get("interleaved", 0))), int(bool(c.get("own_ladder", 0))))
+
+
+def rope_part_cfg(c: dict) -> RopePartCfg:
+    """c: head_dim, and optionally rot_dim (all of the head), rot_offset, interleaved, scaling
+    (a name of ROPE_SCALINGS) with factor, low_turns, high_turns, original_positions, amplitude."""
+    return RopePartCfg(c["head_dim"], c.get("rot_dim", c["head_dim"]), c.get("rot_offset", 0),
+                       int(bool(c.get("interleaved", 0))), ROPE_SCALINGS[c.get("scaling", "none")],
+                       c.get("original_positions", 0), c.get("factor", 1.0),
+                       c.get("low_turns", 0.0), c.get("high_turns", 0.0), c.get("amplitude", 1.0))
 
 
 # ---------------------------------------------------------------- calls ----
@@ -413,6 +437,25 @@ def forge_rope_axes_apply(cfg: RopeAxesCfg, x, ldx, y, ldy, rope_cos, rope_sin, 
     _check(load().forge_rope_axes_apply(ctypes.byref(cfg), _ptr(x), int(ldx), _ptr(y), int(ldy),
                                         _ptr(rope_cos), _ptr(rope_sin), _ptr(positions), tokens,
                                         n_positions, n_rot, int(bool(inverse)), _stream(stream)))
+
+
+def forge_rope_part_table(cfg: RopePartCfg, pair_factors, n_positions, base, cos_out, sin_out,
+                          stream=None):
+    """pair_factors: rot_dim / 2 numbers, or None."""
+    if pair_factors is not None:
+        if len(pair_factors) != cfg.rot_dim // 2:
+            raise ValueError(f"{cfg.rot_dim // 2} pair factors are wanted "
+                             f"(got {len(pair_factors)})")
+        pair_factors = (ctypes.c_float * len(pair_factors))(*pair_factors)
+    _check(load().forge_rope_part_table(ctypes.byref(cfg), pair_factors, n_positions, float(base),
+                                        _ptr(cos_out), _ptr(sin_out), _stream(stream)))
+
+
+def forge_rope_part_apply(cfg: RopePartCfg, x, ldx, y, ldy, rope_cos, rope_sin, positions, tokens,
+                          n_positions, n_rot, backward=False, stream=None):
+    _check(load().forge_rope_part_apply(ctypes.byref(cfg), _ptr(x), int(ldx), _ptr(y), int(ldy),
+                                        _ptr(rope_cos), _ptr(rope_sin), _ptr(positions), tokens,
+                                        n_positions, n_rot, int(bool(backward)), _stream(stream)))
 
 
 def forge_swiglu_fwd(gu, a, tokens, ffn, stream=None):

@@ -1082,6 +1082,119 @@ forge_status forge_rope_axes_apply(const forge_rope_axes_cfg* cfg, const forge_b
   return ok();
 }
 
+namespace {
+forge_status check_rope_part(const forge_rope_part_cfg* c) {
+  FORGE_CHECK(c != nullptr, FORGE_ERR_INVALID_ARG, "cfg is NULL");
+  FORGE_CHECK(c->head_dim >= 8 && c->head_dim % 8 == 0 && c->head_dim / 2 <= forge::kRopeMaxPairs,
+              FORGE_ERR_INVALID_ARG, "head_dim must be a multiple of 8 in [8, %d] (got %d)",
+              2 * forge::kRopeMaxPairs, c->head_dim);
+  FORGE_CHECK(c->rot_dim >= 2 && c->rot_dim % 2 == 0 && c->rot_dim <= c->head_dim &&
+                  c->rot_offset >= 0 && c->rot_offset % 2 == 0 &&
+                  c->rot_offset <= c->head_dim - c->rot_dim,
+              FORGE_ERR_INVALID_ARG, "rot_dim %d at rot_offset %d: even, inside the head of %d",
+              c->rot_dim, c->rot_offset, c->head_dim);
+  FORGE_CHECK(std::isfinite(c->amplitude) && c->amplitude > 0.0f, FORGE_ERR_INVALID_ARG,
+              "amplitude must be > 0");
+  const int k = c->scaling;
+  FORGE_CHECK(k >= FORGE_ROPE_SCALE_NONE && k <= FORGE_ROPE_SCALE_PARTS, FORGE_ERR_INVALID_ARG,
+              "unknown scaling %d", k);
+  FORGE_CHECK(k == FORGE_ROPE_SCALE_NONE || (std::isfinite(c->factor) && c->factor > 0.0f),
+              FORGE_ERR_INVALID_ARG, "factor must be > 0");
+  FORGE_CHECK(k != FORGE_ROPE_SCALE_BASE || c->rot_dim > 2, FORGE_ERR_INVALID_ARG,
+              "a scaled base needs rot_dim > 2");
+  FORGE_CHECK(k != FORGE_ROPE_SCALE_PARTS ||
+                  (c->original_positions >= 1 && c->low_turns >= 0.0f &&
+                   c->low_turns < c->high_turns && std::isfinite(c->high_turns)),
+              FORGE_ERR_INVALID_ARG,
+              "scaling by parts needs original_positions >= 1 and 0 <= low_turns < high_turns");
+  return ok();
+}
+// The angle of pair i for one position.
+double rope_part_frequency(const forge_rope_part_cfg& c, double base, int i) {
+  constexpr double kTwoPi = 6.283185307179586;
+  const double r = c.rot_dim, f = c.factor, w = std::pow(base, -2.0 * i / r);
+  switch (c.scaling) {
+    case FORGE_ROPE_SCALE_LINEAR: return w / f;
+    case FORGE_ROPE_SCALE_BASE: return std::pow(base * std::pow(f, r / (r - 2.0)), -2.0 * i / r);
+    case FORGE_ROPE_SCALE_PARTS: {
+      const double turns = c.original_positions * w / kTwoPi, low = c.low_turns;
+      const double g = std::min(1.0, std::max(0.0, (turns - low) / ((double)c.high_turns - low)));
+      return w * (g + (1.0 - g) / f);
+    }
+    default: return w;
+  }
+}
+}  // namespace
+
+forge_status forge_rope_part_table(const forge_rope_part_cfg* cfg, const float* pair_factors,
+                                   int32_t n_positions, float base, float* cos_out,
+                                   float* sin_out, forge_stream stream) {
+  if (forge_status s = check_rope_part(cfg)) return s;
+  const int half = cfg->rot_dim / 2;
+  FORGE_CHECK(n_positions >= 1, FORGE_ERR_INVALID_ARG, "n_positions must be >= 1");
+  FORGE_CHECK((int64_t)n_positions * half < (1LL << 31), FORGE_ERR_UNSUPPORTED,
+              "a table exceeds 2^31 elements");
+  FORGE_CHECK(base > 0.0f && std::isfinite(base), FORGE_ERR_INVALID_ARG, "base must be > 0");
+  FORGE_PTR(cos_out);
+  FORGE_PTR(sin_out);
+  forge::RopeFreqs f{};
+  for (int i = 0; i < half; ++i) {
+    f.w[i] = rope_part_frequency(*cfg, base, i);
+    if (!pair_factors) continue;
+    FORGE_CHECK(std::isfinite(pair_factors[i]) && pair_factors[i] > 0.0f, FORGE_ERR_INVALID_ARG,
+                "pair_factors[%d] must be > 0", i);
+    f.w[i] /= pair_factors[i];
+  }
+  FORGE_HIP(forge::rope_part_table(f, cfg->amplitude, n_positions, half, cos_out, sin_out,
+                                   (hipStream_t)stream));
+  return ok();
+}
+
+forge_status forge_rope_part_apply(const forge_rope_part_cfg* cfg, const forge_bf16* x,
+                                   int64_t ldx, forge_bf16* y, int64_t ldy, const float* rope_cos,
+                                   const float* rope_sin, const int32_t* positions,
+                                   int32_t tokens, int32_t n_positions, int32_t n_rot,
+                                   int32_t backward, forge_stream stream) {
+  if (forge_status s = check_rope_part(cfg)) return s;
+  FORGE_CHECK(tokens >= 0 && n_positions >= 1 && n_rot >= 0, FORGE_ERR_INVALID_ARG,
+              "bad tokens / n_positions / n_rot");
+  const int64_t width = (int64_t)n_rot * cfg->head_dim;
+  FORGE_CHECK(ldx % 8 == 0 && ldy % 8 == 0 && width <= ldx && width <= ldy, FORGE_ERR_INVALID_ARG,
+              "ldx and ldy must be multiples of 8 holding n_rot heads");
+  if (tokens == 0 || n_rot == 0) return ok();
+  FORGE_CHECK(width < (1LL << 31) && (int64_t)tokens * width < (1LL << 31), FORGE_ERR_UNSUPPORTED,
+              "tokens * n_rot * head_dim exceeds 2^31");
+  FORGE_PTR(x);
+  FORGE_PTR(y);
+  FORGE_PTR(rope_cos);
+  FORGE_PTR(rope_sin);
+  FORGE_CHECK((reinterpret_cast<uintptr_t>(positions) & 3u) == 0, FORGE_ERR_ALIGNMENT,
+              "positions is not 4-byte aligned");
+  const auto extent = [&](int64_t ld) { return ((size_t)(tokens - 1) * ld + width) * 2; };
+  const bool in_place = x == y && ldx == ldy;
+  FORGE_CHECK(in_place || !overlap(x, extent(ldx), y, extent(ldy)), FORGE_ERR_INVALID_ARG,
+              "y overlaps x");
+  forge::RopePart a{};
+  a.x = x;
+  a.y = y;
+  a.ldx = ldx;
+  a.ldy = ldy;
+  a.cos_t = rope_cos;
+  a.sin_t = rope_sin;
+  a.pos = positions;
+  a.T = (uint32_t)tokens;
+  a.rows = n_positions;
+  a.nrot = (uint32_t)n_rot;
+  a.d = (uint32_t)cfg->head_dim;
+  a.rot = (uint32_t)cfg->rot_dim;
+  a.offset = (uint32_t)cfg->rot_offset;
+  a.interleaved = cfg->interleaved != 0;
+  a.copy = !in_place;
+  a.sign = backward ? -1.0f : 1.0f;
+  FORGE_HIP(forge::rope_part(a, (hipStream_t)stream));
+  return ok();
+}
+
 forge_status forge_swiglu_fwd(const forge_bf16* gu, forge_bf16* a, int32_t tokens, int32_t ffn,
                               forge_stream stream) {
   FORGE_CHECK(tokens >= 0 && ffn >= 8 && ffn % 8 == 0, FORGE_ERR_INVALID_ARG,

@@ -160,6 +160,25 @@ hipError_t rope_axes(const RopeAxes& ax, const uint16_t* x, long ldx, uint16_t* 
                      const float* cos_t, const float* sin_t, const int32_t* pos, int T, int rows,
                      int nrot, int d, bool inverse, hipStream_t s);
 
+// --------------------------- rotary positions, a part of each head ----
+// Tables of amplitude cos and amplitude sin of `half` pairs.
+hipError_t rope_part_table(const RopeFreqs& f, float amplitude, int rows, int half, float* cos_t,
+                           float* sin_t, hipStream_t s);
+struct RopePart {
+  const uint16_t* x;
+  uint16_t* y;                  // may be x
+  long ldx, ldy;
+  const float *cos_t, *sin_t;   // [rows, rot / 2]
+  const int32_t* pos;           // [T], NULL: index modulo rows
+  uint32_t T;
+  int rows;
+  uint32_t nrot, d, rot, offset;
+  bool interleaved, copy;       // copy: y is not x, the other columns go with the part
+  float sign;                   // of the sine: -1 backward
+};
+// (T * nrot * d < 2^31)
+hipError_t rope_part(const RopePart& a, hipStream_t s);
+
 // ----------------------------------------------------------- attention ----
 struct AttnArgs {
   const uint16_t* q;    // [T, *] rows, head n at column n*d, row stride ld_qkv
