@@ -571,6 +571,75 @@ forge_status forge_adamw_step(float* master, forge_bf16* param, const float* gra
                               const forge_adamw_hparams* hp, const float* dev_scalars,
                               forge_stream stream);
 
+/*
+ * AdamW over many tensors at once, for parameters that do not lie in one flat
+ * buffer, with moments in 32 or 8 bits and gradients in fp32 or bf16. A tensor:
+ *   master fp32 [n], param bf16 [n], grad fp32 or bf16 [n], as in
+ *     forge_adamw_step (16-byte aligned); its rate is lr * lr_scale, its decay
+ *     hp->weight_decay * decay_scale (0 for norms and biases; both finite).
+ *   state_bits 32: m, v fp32 [n] (16-byte aligned); scales unused. With both
+ *     scales 1 and fp32 gradients a tensor gets the bits of forge_adamw_step.
+ *   state_bits 8: m int8 [n], v uint8 [n] (16-byte aligned) and fp32 m_scale,
+ *     v_scale [ceil(n / 256)] (4-byte aligned): elements 256 b .. 256 b + 255
+ *     share scales b. Codes stand for
+ *       m = q |q| / 127^2 * m_scale, v = (q / 255)^4 * v_scale,
+ *     all zeros (codes and scales) before the first step.
+ * A step with 8 bits decodes the moments, updates them in fp32,
+ *   g = grad clip; m = b1 m + (1-b1) g; v = b2 v + (1-b2) g^2,
+ * every operation rounded once, applies the update of these m and v, and stores
+ * them: each scale is its block's largest magnitude (0 below 2^-94, whose block
+ * is kept as zeros), a code the one below the value or the one above,
+ *   q + 1 iff u * (value(q + 1) - value(q)) < x - value(q),
+ * and a v above zero keeps a code above zero (an m without its v would be a huge
+ * step). dev_seed: device int32, u is uniform in (0, 1), so that the codes keep
+ * the mean: a moment that moves by less than half a code per step, as those of
+ * a beta near 1 do, would stand still if it were rounded to the nearest (the price
+ * is a spread of v of about (4 / q) / sqrt(12 (1 - b2)) of itself). With
+ * h(x): x ^= x >> 16, x *= 0xE699D49D, x ^= x >> 15, x *= 0xC570DA33, x ^= x >> 16
+ * (32 bits), element i of tensor t of the list draws r = h(i ^ h(h(seed) + t)),
+ * u = ((r mod 2^16) + 1/2) / 2^16 for m and ((r / 2^16) + 1/2) / 2^16 for v (i
+ * modulo 2^32), so a step repeats bit for bit; change the seed each step (dev_step
+ * of forge_adamw_advance does). dev_seed NULL: to the nearest, u = 1/2. Not finite
+ * m or v make their block's scale NaN, and its moments with it; other blocks are
+ * not touched.
+ */
+typedef struct {
+  float* master;
+  forge_bf16* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int64_t n;
+  float lr_scale, decay_scale;
+} forge_adamw_multi_tensor;
+
+/* Elements that share a scale (state_bits 8). */
+#define FORGE_ADAMW_BLOCK 256
+
+/*
+ * tensors: host array [n_tensors], read during the call (a captured graph keeps
+ * the pointers). Every buffer that is written has to be a tensor's own. n may be
+ * 0 (the tensor is skipped, its pointers may be NULL); n < 2^40 each, n_tensors
+ * <= 2^20. hp, dev_scalars: as in forge_adamw_step. state_bits other than 8 and
+ * 32: INVALID_ARG.
+ */
+forge_status forge_adamw_multi_step(const forge_adamw_multi_tensor* tensors, int32_t n_tensors,
+                                    int32_t state_bits, int32_t grad_bf16,
+                                    const forge_adamw_hparams* hp, const float* dev_scalars,
+                                    const int32_t* dev_seed, forge_stream stream);
+
+/*
+ * The values that moments in 8 bits stand for (for a checkpoint, or to go on
+ * with 32): m_out[i] and v_out[i] (host arrays of n_tensors device pointers,
+ * 16-byte aligned) get tensor i's, fp32 or (out_bf16) rounded to bf16. Either
+ * array may be NULL: those moments are not read. Other members are not used.
+ */
+forge_status forge_adamw_multi_read(const forge_adamw_multi_tensor* tensors, int32_t n_tensors,
+                                    void* const* m_out, void* const* v_out, int32_t out_bf16,
+                                    forge_stream stream);
+
 /* The step scalars of forge_adamw_step kept on the device, so a whole
  * training step needs no host writes and can be captured into a graph and
  * replayed (App. F, "Deep customization": step scalars on the device):

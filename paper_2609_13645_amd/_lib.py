@@ -79,6 +79,15 @@ class AdamwTensor(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("master", "param", "m", "v")]
 
 
+class AdamwMultiTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ("master", "param", "grad", "m", "v", "m_scale", "v_scale")] + [
+        ("n", ctypes.c_int64), ("lr_scale", ctypes.c_float), ("decay_scale", ctypes.c_float)]
+
+
+ADAMW_BLOCK = 256      # elements that share a scale (moments in 8 bits)
+
+
 class LayerOptim(ctypes.Structure):
     _fields_ = [(n, AdamwTensor) for n in
                 ("attn_norm", "w_qkv", "w_o", "ffn_norm", "w_gate_up", "w_down",
@@ -177,6 +186,10 @@ def load():
                                                  ctypes.POINTER(LayerOptim),
                                                  ctypes.POINTER(AdamwHparams), P, P, P]),
         "forge_adamw_advance": (ctypes.c_int, [P, P, F32, ctypes.c_double, ctypes.c_double, P]),
+        "forge_adamw_multi_step": (ctypes.c_int, [ctypes.POINTER(AdamwMultiTensor), I32, I32, I32,
+                                                  ctypes.POINTER(AdamwHparams), P, P, P]),
+        "forge_adamw_multi_read": (ctypes.c_int, [ctypes.POINTER(AdamwMultiTensor), I32,
+                                                  ctypes.POINTER(P), ctypes.POINTER(P), I32, P]),
         "forge_grad_norm_sq": (ctypes.c_int, [P, I64, P, P, P]),
         "forge_clip_coeff": (ctypes.c_int, [P, F32, F32, P, P]),
         "forge_gemm": (ctypes.c_int, [I32, I32, I32, P, P, P, P, I32, I32, I32,
@@ -276,6 +289,22 @@ def layer_optim(t: dict) -> LayerOptim:
         if name in t:
             setattr(o, name, AdamwTensor(*[_ptr(t[name][k]) for k in ("master", "param", "m", "v")]))
     return o
+
+
+def adamw_multi_tensors(tensors):
+    """The list that forge_adamw_multi_step takes, of dicts with master, param, grad, m, v, with
+    8 bits m_scale and v_scale, n (else master's elements), lr_scale and decay_scale (else 1).
+    Built once for the buffers that it names; it keeps no reference to them."""
+    names = [n for n, _ in AdamwMultiTensor._fields_[:7]]
+    return (AdamwMultiTensor * len(tensors))(*[
+        AdamwMultiTensor(*[_ptr(t.get(k)) for k in names],
+                         t["n"] if "n" in t else t["master"].numel(),
+                         t.get("lr_scale", 1.0), t.get("decay_scale", 1.0)) for t in tensors])
+
+
+def pointers(buffers):
+    """A host array of device pointers (forge_adamw_multi_read's outputs)."""
+    return (ctypes.c_void_p * len(buffers))(*[_ptr(b) for b in buffers])
 
 
 def attn_cfg(c: dict) -> AttnCfg:
@@ -476,6 +505,23 @@ def forge_adamw_step(master, param, grad, m, v, n, hparams: AdamwHparams, dev_sc
     _check(load().forge_adamw_step(_ptr(master), _ptr(param), _ptr(grad), _ptr(m), _ptr(v),
                                    int(n), ctypes.byref(hparams), _ptr(dev_scalars),
                                    _stream(stream)))
+
+
+def forge_adamw_multi_step(tensors, state_bits, grad_bf16, hparams: AdamwHparams, dev_scalars,
+                           dev_seed=None, stream=None):
+    """tensors: of adamw_multi_tensors()."""
+    _check(load().forge_adamw_multi_step(tensors, len(tensors), int(state_bits),
+                                         int(bool(grad_bf16)), ctypes.byref(hparams),
+                                         _ptr(dev_scalars), _ptr(dev_seed), _stream(stream)))
+
+
+def forge_adamw_multi_read(tensors, m_out, v_out, out_bf16=False, stream=None):
+    """m_out, v_out: of pointers(), or None."""
+    for out in (m_out, v_out):
+        if out is not None and len(out) != len(tensors):
+            raise ValueError(f"{len(tensors)} outputs are wanted (got {len(out)})")
+    _check(load().forge_adamw_multi_read(tensors, len(tensors), m_out, v_out, int(bool(out_bf16)),
+                                         _stream(stream)))
 
 
 def forge_layer_bwd_adamw(cfg, weights, saved, x_in, d_out, d_in, grads, optim: LayerOptim,

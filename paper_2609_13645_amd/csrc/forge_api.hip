@@ -1766,6 +1766,106 @@ forge_status forge_adamw_step(float* master, forge_bf16* param, const float* gra
   return ok();
 }
 
+namespace {
+forge_status check_adamw_list(const forge_adamw_multi_tensor* t, int32_t n) {
+  FORGE_CHECK(n >= 0, FORGE_ERR_INVALID_ARG, "n_tensors must be >= 0");
+  FORGE_CHECK(n <= 1 << 20, FORGE_ERR_UNSUPPORTED, "n_tensors > 2^20 (got %d)", n);
+  FORGE_CHECK(n == 0 || t != nullptr, FORGE_ERR_INVALID_ARG, "tensors is NULL");
+  for (int i = 0; i < n; ++i) {
+    FORGE_CHECK(t[i].n >= 0, FORGE_ERR_INVALID_ARG, "tensors[%d].n must be >= 0", i);
+    FORGE_CHECK(t[i].n < 1LL << 40, FORGE_ERR_UNSUPPORTED, "tensors[%d].n >= 2^40", i);
+  }
+  return FORGE_OK;
+}
+struct AdamwBuffer {
+  const void* p;
+  const char* name;
+  unsigned align;
+};
+forge_status check_adamw_buffer(const AdamwBuffer& b, int i) {
+  FORGE_CHECK(b.p != nullptr, FORGE_ERR_INVALID_ARG, "tensors[%d]: %s is NULL", i, b.name);
+  FORGE_CHECK((reinterpret_cast<uintptr_t>(b.p) & (b.align - 1)) == 0, FORGE_ERR_ALIGNMENT,
+              "tensors[%d]: %s is not %u-byte aligned", i, b.name, b.align);
+  return FORGE_OK;
+}
+forge::AdamTensor adamw_tensor(const forge_adamw_multi_tensor& t, int i) {
+  return {t.master,  t.param, t.grad,     t.m,           t.v,        t.m_scale,
+          t.v_scale, t.n,     t.lr_scale, t.decay_scale, (uint32_t)i,
+          nullptr,   nullptr};
+}
+}  // namespace
+
+forge_status forge_adamw_multi_step(const forge_adamw_multi_tensor* tensors, int32_t n_tensors,
+                                    int32_t state_bits, int32_t grad_bf16,
+                                    const forge_adamw_hparams* hp, const float* dev_scalars,
+                                    const int32_t* dev_seed, forge_stream stream) {
+  FORGE_CHECK(state_bits == 8 || state_bits == 32, FORGE_ERR_INVALID_ARG,
+              "state_bits must be 8 or 32 (got %d)", state_bits);
+  if (forge_status e = check_hparams(hp)) return e;
+  if (forge_status e = check_adamw_list(tensors, n_tensors)) return e;
+  bool any = false;
+  for (int i = 0; i < n_tensors; ++i) {
+    const forge_adamw_multi_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    any = true;
+    const AdamwBuffer each[] = {{t.master, "master", 16}, {t.param, "param", 16},
+                                {t.grad, "grad", 16},     {t.m, "m", 16},
+                                {t.v, "v", 16},           {t.m_scale, "m_scale", 4},
+                                {t.v_scale, "v_scale", 4}};
+    for (int k = 0; k < (state_bits == 8 ? 7 : 5); ++k)
+      if (forge_status e = check_adamw_buffer(each[k], i)) return e;
+    FORGE_CHECK(std::isfinite(t.lr_scale) && std::isfinite(t.decay_scale), FORGE_ERR_INVALID_ARG,
+                "tensors[%d]: lr_scale and decay_scale must be finite", i);
+  }
+  if (!any) return ok();
+  FORGE_PTR(dev_scalars);
+  FORGE_CHECK((reinterpret_cast<uintptr_t>(dev_seed) & 3u) == 0, FORGE_ERR_ALIGNMENT,
+              "dev_seed is not 4-byte aligned");
+  const forge::AdamHyper h{hp->beta1,        hp->beta2,   hp->eps,
+                           hp->weight_decay, dev_scalars, state_bits == 8 ? dev_seed : nullptr};
+  forge::AdamTensor batch[forge::kAdamBatch];
+  for (int i = 0, n = 0; i < n_tensors; ++i) {
+    if (tensors[i].n > 0) batch[n++] = adamw_tensor(tensors[i], i);
+    if (n < forge::kAdamBatch && (i + 1 < n_tensors || n == 0)) continue;
+    FORGE_HIP(forge::adamw_multi(batch, n, state_bits, grad_bf16 != 0, h, (hipStream_t)stream));
+    n = 0;
+  }
+  return ok();
+}
+
+forge_status forge_adamw_multi_read(const forge_adamw_multi_tensor* tensors, int32_t n_tensors,
+                                    void* const* m_out, void* const* v_out, int32_t out_bf16,
+                                    forge_stream stream) {
+  if (forge_status e = check_adamw_list(tensors, n_tensors)) return e;
+  if (!m_out && !v_out) return ok();
+  for (int i = 0; i < n_tensors; ++i) {
+    const forge_adamw_multi_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    const AdamwBuffer m[] = {{t.m, "m", 16}, {t.m_scale, "m_scale", 4},
+                             {m_out ? m_out[i] : nullptr, "m_out", 16}};
+    const AdamwBuffer v[] = {{t.v, "v", 16}, {t.v_scale, "v_scale", 4},
+                             {v_out ? v_out[i] : nullptr, "v_out", 16}};
+    for (int k = 0; k < 3; ++k) {
+      if (m_out)
+        if (forge_status e = check_adamw_buffer(m[k], i)) return e;
+      if (v_out)
+        if (forge_status e = check_adamw_buffer(v[k], i)) return e;
+    }
+  }
+  forge::AdamTensor batch[forge::kAdamBatch];
+  for (int i = 0, n = 0; i < n_tensors; ++i) {
+    if (tensors[i].n > 0) {
+      batch[n] = adamw_tensor(tensors[i], i);
+      batch[n].m_out = m_out ? m_out[i] : nullptr;
+      batch[n++].v_out = v_out ? v_out[i] : nullptr;
+    }
+    if (n < forge::kAdamBatch && (i + 1 < n_tensors || n == 0)) continue;
+    FORGE_HIP(forge::adamw_multi_read(batch, n, out_bf16 != 0, (hipStream_t)stream));
+    n = 0;
+  }
+  return ok();
+}
+
 forge_status forge_adamw_advance(float* dev_scalars, int32_t* dev_step, float lr, double beta1,
                                  double beta2, forge_stream stream) {
   FORGE_CHECK(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0,

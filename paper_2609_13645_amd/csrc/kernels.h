@@ -133,6 +133,30 @@ hipError_t sumsq_finish(const float* partials, float* accum, hipStream_t s);
 hipError_t clip_coeff(const float* norm_sq, float max_norm, float eps, float* scalars,
                       hipStream_t s);
 
+// ------------------------------------------- AdamW over many tensors ----
+// (the members of forge_adamw_multi_tensor, and the tensor's place in the list)
+struct AdamTensor {
+  float* master;
+  uint16_t* param;
+  const void* grad;     // fp32 or bf16
+  void *m, *v;          // fp32, or int8 and uint8
+  float *m_scale, *v_scale;
+  int64_t n;
+  float lr_scale, decay_scale;
+  uint32_t index;
+  void *m_out, *v_out;  // of a read: where the moments' values go (NULL: nowhere)
+};
+constexpr int kAdamBatch = 32;   // tensors of a call below, at most
+struct AdamHyper {
+  float b1, b2, eps, wd;
+  const float* sc;      // device {lr, 1 - b1^t, 1 - b2^t, clip}
+  const int32_t* seed;  // device, NULL: codes to the nearest
+};
+// t: host array of 1 to kAdamBatch tensors, none of them empty; bits 32 or 8.
+hipError_t adamw_multi(const AdamTensor* t, int n, int bits, bool grad_bf16, const AdamHyper& h,
+                       hipStream_t s);
+hipError_t adamw_multi_read(const AdamTensor* t, int n, bool out_bf16, hipStream_t s);
+
 // ----------------------------------------------------------- LayerNorm ----
 hipError_t layernorm_fwd(const uint16_t* x, const uint16_t* g, const uint16_t* b, uint16_t* y,
                          float* mean, float* rstd, int T, int h, float eps, hipStream_t s);

@@ -115,3 +115,65 @@ def test_rope_part_apply_refusals():
     assert st(tokens=1 << 24) == UNSUPPORTED
     assert st(tokens=0, x=None, y=None, pos=None) == OK
     assert st(n_rot=0) == OK
+
+
+# ------------------------------------------------- AdamW over many tensors ----
+
+def test_adamw_multi_struct_matches_the_c_header(tmp_path):
+    structs = {"forge_adamw_multi_tensor": _lib.AdamwMultiTensor}
+    assert layout(tmp_path, structs, ["FORGE_ADAMW_BLOCK"]) == [_lib.ADAMW_BLOCK] + ours(structs)
+
+
+HP = _lib.AdamwHparams(0.9, 0.95, 1e-8, 0.1)
+T8 = dict(master=X, param=Y, grad=C, m=S, v=P, m_scale=0x6000000, v_scale=0x7000000, n=100)
+SC, SEED = 0x8000000, 0x9000000
+
+
+def step(tensors, bits=8, hp=HP, sc=SC, seed=SEED):
+    return status(_lib.forge_adamw_multi_step, _lib.adamw_multi_tensors(tensors), bits, 0, hp, sc,
+                  seed, 0)
+
+
+def test_adamw_multi_refusals():
+    for name in ("master", "param", "grad", "m", "v"):
+        for bits in (8, 32):
+            assert step([T8, dict(T8, **{name: None})], bits) == INVALID, name
+            assert step([T8, dict(T8, **{name: T8[name] + 8})], bits) == ALIGNMENT, name
+    for name in ("m_scale", "v_scale"):
+        assert step([dict(T8, **{name: None})]) == INVALID, name
+        assert step([dict(T8, **{name: T8[name] + 2})]) == ALIGNMENT, name
+    for bits in (0, 16, 4, -8):
+        assert step([T8], bits) == INVALID
+    assert step([dict(T8, n=-1)]) == INVALID and step([dict(T8, n=1 << 40)]) == UNSUPPORTED
+    for bad in (float("nan"), float("inf")):
+        assert step([dict(T8, lr_scale=bad)]) == INVALID
+        assert step([dict(T8, decay_scale=bad)]) == INVALID
+    assert step([T8], sc=None) == INVALID and step([T8], sc=SC + 4) == ALIGNMENT
+    assert step([T8], seed=SEED + 1) == ALIGNMENT
+    assert step([T8], hp=_lib.AdamwHparams(1.0, 0.95, 1e-8, 0.1)) == INVALID
+    assert step([T8], hp=_lib.AdamwHparams(0.9, 0.95, -1e-8, 0.1)) == INVALID
+    # nothing to do
+    empty = dict(master=None, n=0)
+    assert step([]) == OK and step([empty, empty], sc=None) == OK
+    f = _lib.load().forge_adamw_multi_step
+    import ctypes as ct
+    assert f(None, 1, 8, 0, ct.byref(HP), SC, None, None) == INVALID
+    assert f(None, -1, 8, 0, ct.byref(HP), SC, None, None) == INVALID
+    assert f(None, (1 << 20) + 1, 8, 0, ct.byref(HP), SC, None, None) == UNSUPPORTED
+    assert f(None, 0, 8, 0, None, SC, None, None) == INVALID
+
+
+def test_adamw_multi_read_refusals():
+    def read(tensors, m, v):
+        p = [None if x is None else _lib.pointers(x) for x in (m, v)]
+        return status(_lib.forge_adamw_multi_read, _lib.adamw_multi_tensors(tensors), *p, 0, 0)
+    assert read([T8], [None], None) == INVALID and read([T8], None, [None]) == INVALID
+    assert read([T8], [X + 8], None) == ALIGNMENT
+    for name in ("m", "m_scale"):
+        assert read([dict(T8, **{name: None})], [X], None) == INVALID
+    for name in ("v", "v_scale"):
+        assert read([dict(T8, **{name: None})], None, [X]) == INVALID
+    assert read([dict(T8, n=-1)], [X], None) == INVALID
+    assert read([T8], None, None) == OK and read([dict(n=0, master=None)], [None], [None]) == OK
+    with pytest.raises(ValueError):
+        read([T8, T8], [X], None)

@@ -82,3 +82,92 @@ def test_rope_part_backward_finite_differences(rot, offset, inter):
     got = packed.rope_part(dy, pos, rot, offset, inter, w, 1.3, backward=True)
     # (the columns that pass through are not scaled)
     assert rel_err(got.ravel(), central_diff(f, x, np.arange(x.size))) <= 1e-6
+
+
+# ------------------------------------------------------- moments of 8 bits ----
+
+def _moments(rng, n):
+    m = (rng.standard_normal(n) * 10.0 ** rng.uniform(-6, 0, n)).astype(np.float32)
+    return m, (rng.standard_normal(n).astype(np.float32) ** 2 * 10.0 ** rng.uniform(
+        -9, 0, n)).astype(np.float32)
+
+
+def test_codes_bracket_the_value():
+    """The nearest code is within half a step; a drawn one within a step."""
+    rng = np.random.default_rng(11)
+    m, v = _moments(rng, 3000)
+    for seed, share in ((None, 0.5), (7, 1.0)):
+        um, uv = packed.moment_draws(3000, 0, seed)
+        q, s = packed.encode_m(m, um)
+        top = np.repeat(s, 256)[:3000]
+        step = (2 * np.abs(q.astype(np.float64)) + 1) / 16129 * top
+        assert np.all(np.abs(packed.decode_m(q, s) - m) <= share * step * 1.0001 + 1e-12)
+        q, s = packed.encode_v(v, uv)
+        top, c = np.repeat(s, 256)[:3000], q.astype(np.float64)
+        step = ((c + 1) ** 4 - c ** 4) / 255.0 ** 4 * top
+        assert np.all(np.abs(packed.decode_v(q, s) - v) <= share * step * 1.0001 + 1e-12)
+
+
+def test_the_largest_of_a_block_is_exact_and_codes_are_kept():
+    rng = np.random.default_rng(12)
+    m, v = _moments(rng, 1024)
+    for seed in (None, 3):
+        um, uv = packed.moment_draws(1024, 5, seed)
+        for x, u, enc, dec in ((m, um, packed.encode_m, packed.decode_m),
+                               (v, uv, packed.encode_v, packed.decode_v)):
+            q, s = enc(x, u)
+            y = dec(q, s)
+            at = np.abs(x.reshape(-1, 256)).argmax(axis=1) + 256 * np.arange(4)
+            # (a largest value a rounding below its code's may be drawn down: not here)
+            assert np.allclose(y[at], x[at], rtol=1e-6)
+            # a value that is a code's already keeps it, whatever is drawn
+            q2, s2 = enc(y, u)
+            assert np.mean(q2 != q) <= 2e-3 and np.allclose(s2, s)
+
+
+def test_drawn_codes_keep_the_mean():
+    """4000 seeds: the mean of 256 values each is theirs within 5 standard deviations of a
+    step's uniform rounding (step / 2 / sqrt(4000))."""
+    rng = np.random.default_rng(13)
+    m, v = _moments(rng, 256)
+    n = 4000
+    am, av = np.zeros(256), np.zeros(256)
+    for seed in range(n):
+        um, uv = packed.moment_draws(256, 1, seed)
+        am += packed.decode_m(*packed.encode_m(m, um))
+        av += packed.decode_v(*packed.encode_v(v, uv))
+    qm = np.floor(np.sqrt(np.abs(m) / np.abs(m).max()) * 127)
+    qv = np.floor((v.astype(np.float64) / v.max()) ** 0.25 * 255)
+    sm = (2 * qm + 1) / 16129 * np.abs(m).max()
+    sv = ((qv + 1) ** 4 - qv ** 4) / 255.0 ** 4 * v.max()
+    assert np.all(np.abs(am / n - m) <= 5 * sm / 2 / np.sqrt(n) + 1e-6 * np.abs(m))
+    # (v keeps a code above zero: below it the mean is the first code's)
+    up = qv >= 1
+    assert np.all((np.abs(av / n - v) <= 5 * sv / 2 / np.sqrt(n) + 1e-6 * v)[up])
+
+
+def test_draws_are_uniform_and_differ():
+    um, uv = packed.moment_draws(1 << 16, 0, 42)
+    for u in (um, uv):
+        assert 0 < u.min() and u.max() < 1
+        count = np.bincount((u * 64).astype(int), minlength=64)
+        # chi-square of 63 degrees of freedom: mean 63, 5 deviations 56
+        assert np.sum((count - 1024.0) ** 2 / 1024.0) < 63 + 56
+        assert abs(np.corrcoef(u[:-1], u[1:])[0, 1]) < 5 / 256
+    assert abs(np.corrcoef(um, uv)[0, 1]) < 5 / 256
+    for other in (packed.moment_draws(1 << 16, 1, 42), packed.moment_draws(1 << 16, 0, 43)):
+        assert abs(np.corrcoef(um, other[0])[0, 1]) < 5 / 256
+
+
+def test_zero_tiny_and_small_blocks():
+    z = np.zeros(300, np.float32)
+    half = np.full(300, np.float32(0.5))
+    for enc, dec in ((packed.encode_m, packed.decode_m), (packed.encode_v, packed.decode_v)):
+        q, s = enc(z, half)
+        assert not q.any() and not s.any() and not dec(q, s).any()
+        q, s = enc(z + np.float32(2.0 ** -96), half)
+        assert not q.any() and not s.any()
+    v = np.zeros(256, np.float32)
+    v[0], v[1] = 1.0, 1e-30
+    q, s = packed.encode_v(v, np.full(256, np.float32(0.99)))
+    assert q[0] == 255 and q[1] == 1 and not q[2:].any()
