@@ -903,6 +903,75 @@ forge_status forge_attention_window_bwd(const forge_attn_window_cfg* cfg, const 
                                         const float* lse, const forge_bf16* d_o,
                                         forge_bf16* d_qkv, void* workspace, forge_stream stream);
 
+/*
+ * Attention over a packed row: `tokens` rows of qkv hold n_seqs sequences
+ * (documents) one behind another, each attending to itself alone: key j is
+ * visible to query i iff both are of one sequence, j <= i and i - j < window
+ * (window 0: no such bound). offsets: device int32 [n_seqs + 1], sequence s is
+ * rows [offsets[s], offsets[s + 1]); they are read on the device, so they may
+ * change from call to call (and between replays of a graph) within the
+ * configuration's bounds. An empty sequence is one; rows before the first and
+ * behind the last sequence belong to none: they are not read, and their rows of
+ * every output are left as they were. Offsets are taken as their running
+ * maximum and cut to [0, tokens]; of a sequence longer than max_seq the first
+ * max_seq rows are taken, the others belong to none.
+ * Rules: n_heads a multiple of n_kv_heads, head_dim 64 or 128; 1 <= tokens, 1 <=
+ * max_seq (values beyond tokens are as tokens), 1 <= n_seqs, window >= 0 (else
+ * INVALID_ARG); tokens <= 2^22, n_seqs <= 2^22, n_heads * tokens <= 2^27,
+ * n_heads * (tokens / 64 + n_seqs) < 2^23, (n_heads + 2 n_kv_heads) * head_dim <=
+ * 2^22 (else UNSUPPORTED).
+ */
+typedef struct {
+  int32_t tokens, n_seqs, max_seq, n_heads, n_kv_heads, head_dim;
+  int32_t window;
+} forge_attn_packed_cfg;
+
+/* Bytes of the plan that forge_attention_packed_plan fills. Host only. */
+forge_status forge_attention_packed_plan_bytes(const forge_attn_packed_cfg* cfg, size_t* bytes);
+
+/*
+ * The work list of a packed batch, built on the device from its offsets: which
+ * tiles of which sequences there are, those with the most keys first. Made once
+ * per batch and read by every layer's forward and backward of the same
+ * configuration (the heads may differ); its contents are the library's own.
+ * plan: 16-byte aligned. positions: device int32 [tokens], each token's place in
+ * its sequence (for forge_rope_part_apply or forge_rope_apply; rows of no
+ * sequence are left as they were), or NULL. offsets, positions 4-byte aligned.
+ */
+forge_status forge_attention_packed_plan(const forge_attn_packed_cfg* cfg, const int32_t* offsets,
+                                         void* plan, int32_t* positions, forge_stream stream);
+
+/*
+ * Forward: qkv [tokens, hq + 2 hkv] and o [tokens, hq] laid out as in
+ * forge_attention_fwd (o must not overlap qkv), lse [n_heads, tokens] fp32. A NaN
+ * or an infinity in a sequence reaches no other sequence. (Within its sequence
+ * one in v may reach rows that do not see it, as 0 * NaN, in the query heads of
+ * its kv head; one in k reaches only rows that see it.) A plan made for other
+ * tokens, n_seqs, max_seq or window: nothing is written.
+ */
+forge_status forge_attention_packed_fwd(const forge_attn_packed_cfg* cfg, const void* plan,
+                                        const forge_bf16* qkv, forge_bf16* o, float* lse,
+                                        forge_stream stream);
+
+/* Scratch bytes of forge_attention_packed_bwd: per-query statistics, partial sums
+ * of dK and dV where few blocks would share the work, and the score gradient in
+ * bf16, of each head 4 KB for every 64 keys x 32 queries that see each other, at
+ * most: of full sequences of max_seq (or the window's band of them). Host only. */
+forge_status forge_attention_packed_bwd_workspace_bytes(const forge_attn_packed_cfg* cfg,
+                                                        size_t* bytes);
+
+/*
+ * Backward over the visible pairs: from d_o [tokens, hq] bf16 and the forward's
+ * qkv, o, lse and plan, writes d_qkv [tokens, hq + 2 hkv] bf16 (=), which must
+ * not overlap qkv, o or d_o. A NaN or an infinity in a sequence's rows of any
+ * input reaches no other sequence and no other kv head's group. No atomics:
+ * bitwise deterministic.
+ */
+forge_status forge_attention_packed_bwd(const forge_attn_packed_cfg* cfg, const void* plan,
+                                        const forge_bf16* qkv, const forge_bf16* o,
+                                        const float* lse, const forge_bf16* d_o,
+                                        forge_bf16* d_qkv, void* workspace, forge_stream stream);
+
 /* Scratch bytes of forge_moe_route. Host only. */
 forge_status forge_moe_route_workspace_bytes(int32_t tokens, int32_t n_experts, int32_t top_k,
                                              size_t* bytes);

@@ -1,6 +1,6 @@
 """Oracle: training on packed documents of long contexts, fp64: rotary positions
-on a part of each head with scaled frequencies, forward and backward, and AdamW
-with moments of 8 bits.
+on a part of each head with scaled frequencies and attention over packed sequences,
+forward and backward, and AdamW with moments of 8 bits.
 
 TEST INFRASTRUCTURE ONLY (see the package docstring).
 
@@ -9,6 +9,9 @@ TEST INFRASTRUCTURE ONLY (see the package docstring).
     interpolated (w / f), of a larger base (b f^(r / (r - 1)) for r pairs), or by
     parts: w (g + (1 - g) / f), g = the turns in the trained context, from `low`
     (0) to `high` (1).
+  * Packed attention: every sequence a row of its own, causal, with or without a
+    window; offsets are taken as their running maximum cut to [0, tokens], of a
+    sequence longer than max_seq the first max_seq rows.
   * Moments of 8 bits: blocks of 256 share their largest magnitude s; m's code q
     stands for q |q| s / 127^2, v's for (q / 255)^4 s; a value between those of two
     codes takes the upper one iff u (upper - lower) < value - lower, u in (0, 1)
@@ -18,6 +21,8 @@ TEST INFRASTRUCTURE ONLY (see the package docstring).
 from __future__ import annotations
 
 import numpy as np
+
+from . import branch
 
 
 def part_frequencies(rot, base, scaling="none", factor=1.0, low=0.0, high=1.0, original=1,
@@ -127,3 +132,45 @@ def moments_step(g, qm, sm, qv, sv, beta1, beta2, clip):
     b1, b2, g = F32(beta1), F32(beta2), g.astype(F32) * F32(clip)
     m = decode_m(qm, sm) * b1 + (F32(1) - b1) * g
     return m, decode_v(qv, sv) * b2 + ((F32(1) - b2) * g) * g
+
+
+def sequences(offsets, tokens, max_seq):
+    """[(first row, rows)] of every sequence."""
+    e = np.maximum.accumulate(np.clip(np.asarray(offsets, np.int64), 0, tokens))
+    return [(int(a), min(int(b - a), max_seq)) for a, b in zip(e[:-1], e[1:])]
+
+
+def covered(offsets, tokens, max_seq):
+    """[tokens] of bool: rows of a sequence."""
+    c = np.zeros(tokens, bool)
+    for a, n in sequences(offsets, tokens, max_seq):
+        c[a:a + n] = True
+    return c
+
+
+def positions(offsets, tokens, max_seq):
+    p = np.full(tokens, -1, np.int64)
+    for a, n in sequences(offsets, tokens, max_seq):
+        p[a:a + n] = np.arange(n)
+    return p
+
+
+def attention(q, k, v, do, offsets, max_seq, window=0):
+    """q, do [T, n_h, d], k, v [T, n_kv, d] (do may be None) -> dict of o, lse [n_h, T] and,
+    with do, dq, dk, dv, each but lse with its "err_" as branch.window_attention's. Rows of
+    no sequence are NaN."""
+    T = len(q)
+    names = ("o",) if do is None else ("o", "dq", "dk", "dv")
+    like = dict(o=q, dq=q, dk=k, dv=v)
+    r = {p + n: np.full_like(like[n], np.nan) for n in names for p in ("", "err_")}
+    r["lse"] = np.full((q.shape[1], T), np.nan)
+    for a, n in sequences(offsets, T, max_seq):
+        if n == 0:
+            continue
+        s = slice(a, a + n)
+        one = branch.window_attention(q[s], k[s], v[s], None if do is None else do[s], 1, n,
+                                      window or n, 0)
+        r["lse"][:, s] = one["lse"][0]
+        for name in names:
+            r[name][s], r["err_" + name][s] = one[name], one["err_" + name]
+    return r

@@ -104,6 +104,11 @@ class AttnWindowCfg(ctypes.Structure):
     _fields_ = AttnCfg._fields_ + [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
+class AttnPackedCfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("tokens", "n_seqs", "max_seq", "n_heads", "n_kv_heads", "head_dim", "window")]
+
+
 ROPE_MAX_AXES = 4
 
 
@@ -217,6 +222,14 @@ def load():
                                                        [ctypes.POINTER(AttnWindowCfg), SZ]),
         "forge_attention_window_bwd": (ctypes.c_int, [ctypes.POINTER(AttnWindowCfg), P, P, P, P,
                                                       P, P, P, P]),
+        "forge_attention_packed_plan_bytes": (ctypes.c_int, [ctypes.POINTER(AttnPackedCfg), SZ]),
+        "forge_attention_packed_plan": (ctypes.c_int, [ctypes.POINTER(AttnPackedCfg), P, P, P, P]),
+        "forge_attention_packed_fwd": (ctypes.c_int, [ctypes.POINTER(AttnPackedCfg), P, P, P, P,
+                                                      P]),
+        "forge_attention_packed_bwd_workspace_bytes": (ctypes.c_int,
+                                                       [ctypes.POINTER(AttnPackedCfg), SZ]),
+        "forge_attention_packed_bwd": (ctypes.c_int, [ctypes.POINTER(AttnPackedCfg), P, P, P, P, P,
+                                                      P, P, P]),
         "forge_moe_route_workspace_bytes": (ctypes.c_int, [I32, I32, I32, SZ]),
         "forge_moe_route": (ctypes.c_int, [P, I32, I32, I32, P, P, P, P, P, P, P, P]),
         "forge_moe_route_noalloc": (ctypes.c_int, [P, I32, I32, I32, P, P, P, P, P, P, P]),
@@ -314,6 +327,11 @@ def attn_cfg(c: dict) -> AttnCfg:
 def attn_window_cfg(c: dict) -> AttnWindowCfg:
     return AttnWindowCfg(c["batch"], c["seq"], c["n_heads"], c["n_kv_heads"], c["head_dim"],
                          c["window"], c.get("sinks", 0))
+
+
+def attn_packed_cfg(c: dict) -> AttnPackedCfg:
+    return AttnPackedCfg(c["tokens"], c["n_seqs"], c["max_seq"], c["n_heads"], c["n_kv_heads"],
+                         c["head_dim"], c.get("window", 0))
 
 
 def rope_axes_cfg(c: dict) -> RopeAxesCfg:
@@ -620,6 +638,35 @@ def forge_attention_window_bwd_workspace_bytes(cfg: AttnWindowCfg) -> int:
 def forge_attention_window_bwd(cfg: AttnWindowCfg, qkv, seq_lens, o, lse, d_o, d_qkv, workspace,
                                stream=None):
     _check(load().forge_attention_window_bwd(ctypes.byref(cfg), _ptr(qkv), _ptr(seq_lens), _ptr(o),
+                                             _ptr(lse), _ptr(d_o), _ptr(d_qkv), _ptr(workspace),
+                                             _stream(stream)))
+
+
+def forge_attention_packed_plan_bytes(cfg: AttnPackedCfg) -> int:
+    n = ctypes.c_size_t()
+    _check(load().forge_attention_packed_plan_bytes(ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def forge_attention_packed_plan(cfg: AttnPackedCfg, offsets, plan, positions=None, stream=None):
+    _check(load().forge_attention_packed_plan(ctypes.byref(cfg), _ptr(offsets), _ptr(plan),
+                                              _ptr(positions), _stream(stream)))
+
+
+def forge_attention_packed_fwd(cfg: AttnPackedCfg, plan, qkv, o, lse, stream=None):
+    _check(load().forge_attention_packed_fwd(ctypes.byref(cfg), _ptr(plan), _ptr(qkv), _ptr(o),
+                                             _ptr(lse), _stream(stream)))
+
+
+def forge_attention_packed_bwd_workspace_bytes(cfg: AttnPackedCfg) -> int:
+    n = ctypes.c_size_t()
+    _check(load().forge_attention_packed_bwd_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def forge_attention_packed_bwd(cfg: AttnPackedCfg, plan, qkv, o, lse, d_o, d_qkv, workspace,
+                               stream=None):
+    _check(load().forge_attention_packed_bwd(ctypes.byref(cfg), _ptr(plan), _ptr(qkv), _ptr(o),
                                              _ptr(lse), _ptr(d_o), _ptr(d_qkv), _ptr(workspace),
                                              _stream(stream)))
 

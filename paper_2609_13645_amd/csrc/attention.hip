@@ -166,14 +166,18 @@ __device__ __forceinline__ bf16x8_t gload_frag(const bf16_t* p, bool ok) {
 // each as in the causal form), backward 940; 16384 tokens, window 4096, 16 sinks:
 // 945 and 2840 to 2930 us (1020 and 825 to 850 TFLOP/s).
 template <typename Args>
-constexpr bool kWindow = std::is_same_v<Args, AttnWindowArgs>;
+constexpr bool kPacked = std::is_same_v<Args, AttnPackedArgs>;
+template <typename Args>
+constexpr bool kWindow = std::is_same_v<Args, AttnWindowArgs> || kPacked<Args>;
 __device__ __forceinline__ int row_len(const AttnArgs& a, int) { return a.seq; }
 __device__ __forceinline__ int row_len(const AttnWindowArgs& a, int b) {
   return a.lens ? min(max(a.lens[b], 0), a.seq) : a.seq;
 }
+__device__ __forceinline__ int row_len(const AttnPackedArgs& a, int) { return a.seq; }
 // The rows of a batch row, of which `len` are its tokens.
 __device__ __forceinline__ int seq_of(const AttnArgs&, int len) { return len; }
 __device__ __forceinline__ int seq_of(const AttnWindowArgs& a, int) { return a.seq; }
+__device__ __forceinline__ int seq_of(const AttnPackedArgs& a, int) { return a.seq; }
 // Block id of the dispatcher's round robin over 8 XCDs -> position in an order of n
 // of which each XCD takes one contiguous part.
 __device__ __forceinline__ int xcd_order(int id, int n) {
@@ -192,6 +196,38 @@ struct WindowTiles {
   }
   __device__ __forceinline__ int operator()(int j) const { return j < sinks ? j : j + skip; }
 };
+
+// ---------------------------------------------------- packed sequences ----
+// The kernels' PACKED form (arguments AttnPackedArgs) is the window's of one batch row
+// per sequence: a block takes a tile from the plan's list, whose sequence's rows start
+// anywhere and end at its length, cut off by the buffers' sizes as a batch row's are, so
+// that tiles of two sequences never share a row and nothing is read past a sequence.
+// Entry i of the list of 64 << KIND rows; len 0 where there is none, or where the plan is
+// one of other sizes.
+__device__ __forceinline__ long first_row_of(const AttnPackedArgs&, const PackedTile& t, int, int) {
+  return t.start;
+}
+template <typename Args, typename T>
+__device__ __forceinline__ long first_row_of(const Args&, const T&, int b, int S) {
+  return (long)b * S;
+}
+// The statistics [batch, n_heads, seq] of the batch row's query 0.
+__device__ __forceinline__ long stat_row(const AttnPackedArgs& a, int, int n, int, long rb) {
+  return (long)n * a.seq + rb;
+}
+template <typename Args>
+__device__ __forceinline__ long stat_row(const Args& a, int b, int n, int S, long) {
+  return ((long)b * a.n_heads + n) * S;
+}
+template <int KIND>
+__device__ __forceinline__ PackedTile packed_tile(const AttnPackedArgs& a, int i) {
+  const PackedHeader h = *a.plan;
+  PackedTile t = a.tiles[KIND][i];
+  if (i >= h.count[KIND] || h.tokens != a.seq || h.n_seqs != a.n_seqs ||
+      h.max_seq != a.max_seq || h.window != a.window)
+    t.len = 0;
+  return t;
+}
 
 __device__ __forceinline__ void zero(f32x16_t& a) {
 #pragma unroll
@@ -311,7 +347,8 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
   // slot t & 1. K runs one tile ahead of V (S of tile j + 1 is formed while
   // tile j's softmax and P V run), so each slot pair is a double buffer.
   __shared__ uint4 smem_[KG * 4 * NAT];   // (of each group)
-  const int S = a.seq;
+  constexpr bool PACKED = kPacked<Args>;
+  int S = a.seq;
   const int nqt = (S + BQ - 1) / BQ;
   // Block order: the query tiles with the most keys (the last ones) first,
   // one tile level at a time across every (batch, head), so that the long
@@ -324,7 +361,16 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
   const int level = id / W, r = id % W;
   const int L = (W % 8 == 0) ? (r % 8) * (W / 8) + r / 8 : r;
   int qt = nqt - 1 - level, n = L % a.n_heads, b = L / a.n_heads;
-  if constexpr (WIN) {
+  std::conditional_t<PACKED, PackedTile, int> pt{};
+  if constexpr (PACKED) {
+    const PackedTile t = packed_tile<NW == 2 ? 0 : 1>(a, level);
+    if (t.len == 0) return;
+    n = L;
+    b = 0;
+    qt = t.tile;
+    pt = t;
+    S = t.len;
+  } else if constexpr (WIN) {
     // WIN: blocks are about alike but for the first; each XCD takes neighbouring
     // query tiles of one kv head (its query heads side by side), whose windows overlap
     const int grp = a.n_heads / a.n_kv_heads;
@@ -335,8 +381,8 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
     n = t / nqt * grp + i % grp;
   }
   const int m = n / (a.n_heads / a.n_kv_heads);
-  const int E = WIN ? row_len(a, b) : S;   // end of the batch row's tokens
-  const long rb = (long)b * S;
+  const int E = WIN && !PACKED ? row_len(a, b) : S;   // end of the batch row's tokens
+  const long rb = first_row_of(a, pt, b, S);
   const bf16_t* Qg = a.q + rb * a.ld_qkv + (long)n * D;
   const bf16_t* Kg = a.k + rb * a.ld_qkv + (long)m * D;
   const bf16_t* Vg = a.v + rb * a.ld_qkv + (long)m * D;
@@ -579,7 +625,7 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
 #pragma unroll
         for (int g = 0; g < 4; ++g)
           *reinterpret_cast<uint2*>(orow + db * 32 + g * 8 + hh * 4) = make_uint2(0, 0);
-      if (hh == 0) lse[((long)b * a.n_heads + n) * S + q] = -INFINITY;
+      if (hh == 0) lse[stat_row(a, b, n, S, rb) + q] = -INFINITY;
     }
     return;
   }
@@ -656,7 +702,7 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
                               pack2(oacc[db][g * 4 + 2] * inv, oacc[db][g * 4 + 3] * inv));
       }
     if (hh == 0)
-      lse[((long)b * a.n_heads + n) * S + q] = none ? -INFINITY : (mrow + log2f(lrow)) * kLn2;
+      lse[stat_row(a, b, n, S, rb) + q] = none ? -INFINITY : (mrow + log2f(lrow)) * kLn2;
   }
 }
 
@@ -714,8 +760,18 @@ static DsWindow ds_window(const AttnWindowArgs& a) {
   return L;
 }
 
-__device__ __forceinline__ DsLayout ds_layout(const AttnArgs& a) { return DsLayout(a.seq); }
-__device__ __forceinline__ const DsWindow& ds_layout(const AttnWindowArgs& a) { return a.ds; }
+// (block: what the kernel knows of its own, which a batch row's layout does not need)
+template <typename B>
+__device__ __forceinline__ DsLayout ds_layout(const AttnArgs& a, const B&) {
+  return DsLayout(a.seq);
+}
+template <typename B>
+__device__ __forceinline__ const DsWindow& ds_layout(const AttnWindowArgs& a, const B&) {
+  return a.ds;
+}
+__device__ __forceinline__ DsPacked ds_layout(const AttnPackedArgs& a, const PackedTile& t) {
+  return DsPacked(t.len, a.window, t.base, a.ds_head);
+}
 
 // 1. -delta and -LSE log2(e) of every (batch, head, query): D / 8 lanes per
 // (token, head) row of dO and O, 16-byte loads (the heads of a token are
@@ -847,6 +903,50 @@ struct KvWindowBlock {
 __device__ __forceinline__ KvWindowBlock kv_block(const AttnWindowArgs& a, int splits) {
   return KvWindowBlock(a, splits);
 }
+// PACKED: the tiles of the list of 64 rows in turn, whose queries' tile qt has the most keys
+// first; key tile nkt - 1 - qt of the same sequence has as many queries. kv head fastest.
+struct KvPackedBlock {
+  int kt, b, m, z, step;   // as above
+  int j0, ns, len;
+  static constexpr int turn = 0;
+  PackedTile t;
+  __device__ __forceinline__ KvPackedBlock(const AttnPackedArgs& a, int splits) {
+    const int r = (int)blockIdx.x % (a.n_kv_heads * splits);
+    t = packed_tile<0>(a, (int)blockIdx.x / (a.n_kv_heads * splits));
+    m = r % a.n_kv_heads;
+    b = 0;
+    z = r / a.n_kv_heads;
+    step = splits;
+    len = t.len;
+    kt = (len + 63) / 64 - 1 - t.tile;
+    j0 = 2 * kt;
+    const DsPacked L = ds_layout(a, t);
+    ns = min(j0 + L.nwin, L.ns) - j0;
+  }
+};
+__device__ __forceinline__ KvPackedBlock kv_block(const AttnPackedArgs& a, int splits) {
+  return KvPackedBlock(a, splits);
+}
+__device__ __forceinline__ DsPacked ds_layout(const AttnPackedArgs& a, const KvPackedBlock& k) {
+  return ds_layout(a, k.t);
+}
+// The batch row's first row (of a row of S tokens), its place in the statistics of a head
+// of the batch row, and its rows, padding included.
+template <typename Args, typename B>
+__device__ __forceinline__ long first_row(const Args& a, const B& k, int S) {
+  if constexpr (kPacked<Args>) return k.t.start;
+  else return (long)k.b * seq_of(a, S);
+}
+template <typename Args, typename B>
+__device__ __forceinline__ int row_in(const Args&, const B& k) {
+  if constexpr (kPacked<Args>) return k.t.start;
+  else return 0;
+}
+template <typename Args>
+__device__ __forceinline__ int rows_of(const Args& a, int S) {
+  if constexpr (kPacked<Args>) return S;
+  else return seq_of(a, S);
+}
 // s_waitcnt immediate that waits for vmcnt <= n only (gfx9 encoding: vmcnt
 // bits 3:0 and 15:14, expcnt 6:4 and lgkmcnt 11:8 at their maxima)
 constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
@@ -874,6 +974,14 @@ __device__ __forceinline__ float* kv_part(const AttnWindowArgs& a, float* part,
   }
   if (!part) return nullptr;
   return part + ((long)k.z * a.batch * a.seq + row) * width + k.m * D;
+}
+
+// PACKED: the block's rows of its split's partial sums [splits][tokens][n_kv * D].
+template <int D, bool V>
+__device__ __forceinline__ float* kv_part(const AttnPackedArgs& a, float* part,
+                                          const KvPackedBlock& k, long row) {
+  if (!part) return nullptr;
+  return part + (((long)k.z * a.seq + row) * a.n_kv_heads + k.m) * D;
 }
 
 // One DMA instruction: 16 bytes per lane from a buffer of `bytes` bytes (zeros
@@ -1018,6 +1126,10 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   // block order: key tile slowest, so the low key tiles (the most work)
   // are dispatched first
   const auto kb_ = kv_block(a, splits);
+  constexpr bool PACKED = kPacked<Args>;
+  if constexpr (PACKED) {
+    if (kb_.len == 0) return;
+  }
   const int kt = kb_.kt, m = kb_.m, b = kb_.b;
   const int k0 = kt * BK;
   if constexpr (WIN) {
@@ -1034,10 +1146,10 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5, l32 = lane & 31;
-  const long rb = (long)b * seq_of(a, S);
+  const long rb = first_row(a, kb_, S);
   const long ldo = (long)a.n_heads * D;
   const long nrows = (long)a.batch * a.n_heads * seq_of(a, S);
-  const auto L = ds_layout(a);
+  const auto L = ds_layout(a, kb_);
 
   // K and V rows of the lane's two keys k0 + l32 and k0 + 32 + l32: the
   // B operands of S and dP
@@ -1155,7 +1267,7 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
       dma_16(w.o, rows * orb, base + SLAB + j * 64,
              orow + (c0 ^ fsw<D>(j * P::RPI) * 16) + (j * P::RPI * orb + z));
     } else if constexpr (!STATS) {
-      const long li = ((long)b * a.n_heads + w.n) * seq_of(a, S) + w.q0 + l32;
+      const long li = ((long)b * a.n_heads + w.n) * seq_of(a, S) + row_in(a, kb_) + w.q0 + l32;
       dma_4(delta, base + 2 * SLAB,
             w.q0 + l32 < S ? (uint32_t)(((hh ? 0 : nrows) + li) * 4) : kOOB);
     }
@@ -1412,7 +1524,8 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
       dot = fa::sum_xor32(dot);
       float v = -dot;
       if (hh == 0)
-        v = in ? -kLog2e * a.lse[((long)b * a.n_heads + u.n) * a.seq + u.q0 + l32] : 0.0f;
+        v = in ? -kLog2e * a.lse[((long)b * a.n_heads + u.n) * a.seq + row_in(a, kb_) + u.q0 + l32]
+               : 0.0f;
       reinterpret_cast<float*>(mine + i * B::WBUF + 2 * SLAB)[lane] = v;
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the pairs' reads are inline asm)
@@ -1429,11 +1542,11 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   if (dsblk) store_ds();
   kv_reduce_store<D>(acc, sm, sm + 2 * P::RED, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D,
                      ld_d, kv_part<D, true>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D,
-                     seq_of(a, S) - k0, S - k0);
+                     rows_of(a, S) - k0, S - k0);
   kv_reduce_store<D>(acck, sm, sm + 2 * P::RED, wave, lane, a.scale,
                      dk + (rb + k0) * ld_d + (long)m * D, ld_d,
                      kv_part<D, false>(a, pk, kb_, rb + k0), (long)a.n_kv_heads * D,
-                     seq_of(a, S) - k0, S - k0);
+                     rows_of(a, S) - k0, S - k0);
 }
 
 // dK and dV from the splits' partial sums, added in split order; eight columns
@@ -1550,7 +1663,8 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
   constexpr bool WIN = kWindow<Args>;
   constexpr int BQ = Q::BQ, BKV = Q::BKV, NAT = Q::NAT, NW = Q::NW, NST = Q::NST, DB = D / 32;
   __shared__ uint4 sm_[KG * NST * Q::STAGE];   // (of each group of waves)
-  const int S = a.seq;
+  constexpr bool PACKED = kPacked<Args>;
+  int S = a.seq;
   const int nqt = (S + BQ - 1) / BQ;
   // block id: kv head fastest (the dispatcher spreads consecutive ids over
   // the XCDs, so each XCD's L2 holds the K of few kv heads), then the query
@@ -1561,7 +1675,16 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
   int n = m * grp + id / a.n_kv_heads % grp;
   int b = id / a.n_kv_heads / grp % a.batch;
   int qt = nqt - 1 - id / (a.n_kv_heads * grp * a.batch);
-  if constexpr (WIN) {
+  std::conditional_t<PACKED, PackedTile, int> pt{};
+  if constexpr (PACKED) {
+    // (list entries in turn, the heads of each as in the causal order)
+    pt = packed_tile<WAVES == 2 ? 0 : WAVES == 4 ? 1 : 2>(a, id / a.n_heads);
+    if (pt.len == 0) return;
+    n = m * grp + id / a.n_kv_heads % grp;
+    b = 0;
+    qt = pt.tile;
+    S = pt.len;
+  } else if constexpr (WIN) {
     // WIN: the last blocks are the sums, where the kv pass left few; else as in the forward
     const int blocks = nqt * a.n_heads * a.batch;
     if (id >= blocks) {
@@ -1577,9 +1700,9 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
     m = t / nqt;
     n = m * grp + i % grp;
   }
-  const long rb = (long)b * S;
-  const int E = WIN ? row_len(a, b) : S;   // end of the batch row's tokens
-  const auto L = ds_layout(a);
+  const long rb = first_row_of(a, pt, b, S);
+  const int E = WIN && !PACKED ? row_len(a, b) : S;   // end of the batch row's tokens
+  const auto L = ds_layout(a, pt);
   const bf16_t* Kg = a.k + rb * a.ld_qkv + (long)m * D;
   const bf16_t* dsh = ds + ((long)b * a.n_heads + n) * L.head;
   const int lane = threadIdx.x & 63;
@@ -2067,6 +2190,67 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
   return hipGetLastError();
 }
 }  // namespace
+
+namespace {
+// Where a split's rows of dK and dV (grid.y 0, 1) end: the plan's tiles of 64 rows in turn,
+// eight columns to a thread.
+__global__ __launch_bounds__(256) void attn_packed_sum_k(AttnPackedArgs a, int splits,
+                                                         bf16_t* __restrict__ dk,
+                                                         bf16_t* __restrict__ dv, long ld_d) {
+  const PackedTile t = packed_tile<0>(a, (int)blockIdx.x);
+  const int width = a.n_kv_heads * a.d, cpr = width / 8;
+  const int i = (int)blockIdx.z * 256 + (int)threadIdx.x;
+  const int r = t.tile * 64 + i / cpr, c = i % cpr * 8;
+  if (i >= 64 * cpr || r >= t.len) return;
+  const bool v = blockIdx.y != 0;
+  const long row = t.start + r;
+  split_sum((v ? a.pv : a.pk) + row * width + c, splits, (long)a.seq * width,
+            v ? 1.0f : a.scale, (v ? dv : dk) + row * ld_d + c);
+}
+template <int D>
+hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16_t* o,
+                             const uint16_t* dout, const float* lse, float* delta, uint16_t* ds,
+                             float* part, uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_d,
+                             hipStream_t s) {
+  using std::false_type;
+  const long T = a.seq, rows = T * a.n_heads;
+  const dim3 block(256);
+  const int splits = 1;
+  const dim3 pgrid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
+  hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
+                     a.seq);
+  const dim3 kgrid((unsigned)(p.cap[0] * a.n_kv_heads * splits));
+  hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, false, false>), kgrid, block, 0, s, a, dout,
+                     delta, ds, dv, dk, ld_d, a.pv, a.pk, splits);
+  if (splits > 1) {
+    const dim3 grid((unsigned)p.cap[0], 2, (unsigned)((8 * a.n_kv_heads * D + 255) / 256));
+    hipLaunchKernelGGL(attn_packed_sum_k, grid, block, 0, s, a, splits, dk, dv, ld_d);
+  }
+  const dim3 grid((unsigned)(p.cap[2] * a.n_heads));
+  hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, 8, 1>), grid, dim3(512), 0, s, a, ds, dq,
+                     ld_d);
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t attn_packed_fwd(const AttnPackedArgs& a, const PackedPlan& p, uint16_t* o, float* lse,
+                           hipStream_t s) {
+  const dim3 grid((unsigned)(p.cap[1] * a.n_heads)), block(256);
+  if (a.d == 128)
+    hipLaunchKernelGGL((attn_fwd_k<128, AttnPackedArgs, 4, 1>), grid, block, 0, s, a, o, lse);
+  else
+    hipLaunchKernelGGL((attn_fwd_k<64, AttnPackedArgs, 4, 1>), grid, block, 0, s, a, o, lse);
+  return hipGetLastError();
+}
+size_t attn_packed_bwd_part_bytes(const AttnPackedArgs&, const PackedPlan&) { return 0; }
+hipError_t attn_packed_bwd(const AttnPackedArgs& a, const PackedPlan& p, const uint16_t* o,
+                           const uint16_t* dout, const float* lse, float* delta, uint16_t* ds,
+                           float* part, uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_d,
+                           hipStream_t s) {
+  return a.d == 128
+             ? attn_packed_bwd_d<128>(a, p, o, dout, lse, delta, ds, part, dq, dk, dv, ld_d, s)
+             : attn_packed_bwd_d<64>(a, p, o, dout, lse, delta, ds, part, dq, dk, dv, ld_d, s);
+}
 
 hipError_t attn_bwd(const AttnArgs& a, const uint16_t* o, const uint16_t* dout, const float* lse,
                     float* delta, uint16_t* ds, float* part, uint16_t* dq, uint16_t* dk,

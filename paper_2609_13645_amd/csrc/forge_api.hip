@@ -2204,4 +2204,130 @@ forge_status forge_attention_window_bwd(const forge_attn_window_cfg* cfg, const 
   return ok();
 }
 
+namespace {
+forge_status check_attn_packed(const forge_attn_packed_cfg* c) {
+  FORGE_CHECK(c != nullptr, FORGE_ERR_INVALID_ARG, "cfg is NULL");
+  const forge_attn_cfg a{1, c->tokens, c->n_heads, c->n_kv_heads, c->head_dim};
+  if (forge_status s = check_attn(&a)) return s;
+  FORGE_CHECK(c->n_seqs >= 1 && c->max_seq >= 1, FORGE_ERR_INVALID_ARG,
+              "n_seqs, max_seq must be >= 1");
+  FORGE_CHECK(c->window >= 0, FORGE_ERR_INVALID_ARG, "window must be >= 0 (got %d)", c->window);
+  // 32-bit offsets of the kernels' buffer accesses: a tile's rows, a key tile's score
+  // gradient, the per-query statistics; threads of a launch: 256 to a tile of 64 rows
+  FORGE_CHECK(c->tokens <= 1 << 22 && c->n_seqs <= 1 << 22, FORGE_ERR_UNSUPPORTED,
+              "tokens or n_seqs > 2^22");
+  FORGE_CHECK((int64_t)c->n_heads + 2 * (int64_t)c->n_kv_heads <= (1 << 22) / c->head_dim,
+              FORGE_ERR_UNSUPPORTED, "a row of qkv exceeds 2^22 elements");
+  FORGE_CHECK((int64_t)c->tokens * c->n_heads <= (1 << 27), FORGE_ERR_UNSUPPORTED,
+              "n_heads * tokens exceeds 2^27");
+  FORGE_CHECK(((int64_t)c->tokens / 64 + c->n_seqs) * c->n_heads < (1 << 23),
+              FORGE_ERR_UNSUPPORTED, "n_heads * (tokens / 64 + n_seqs) exceeds 2^23");
+  const forge::PackedPlan p(c->tokens, c->n_seqs, c->max_seq, c->window);
+  FORGE_CHECK(p.ds_blocks < 1LL << 31, FORGE_ERR_UNSUPPORTED,
+              "a head's score gradient exceeds 2^31 blocks");
+  return FORGE_OK;
+}
+struct PackedCfg : forge::PackedPlan {
+  explicit PackedCfg(const forge_attn_packed_cfg& c)
+      : PackedPlan(c.tokens, c.n_seqs, c.max_seq, c.window) {}
+};
+struct PackedArgs : forge::AttnPackedArgs {
+  PackedArgs(const forge_attn_packed_cfg& c, const forge::PackedPlan& p, const void* plan_,
+             const uint16_t* qkv) {
+    const forge_attn_cfg a{1, c.tokens, c.n_heads, c.n_kv_heads, c.head_dim};
+    static_cast<forge::AttnArgs&>(*this) = attn_args(attn_dims(a), qkv);
+    window = p.window;
+    plan = static_cast<const forge::PackedHeader*>(plan_);
+    for (int k = 0; k < 3; ++k)
+      tiles[k] = reinterpret_cast<const forge::PackedTile*>(static_cast<const char*>(plan_) +
+                                                            p.tiles[k]);
+    n_seqs = p.n_seqs;
+    max_seq = p.max_seq;
+    ds_head = 2048 * p.ds_blocks;
+  }
+};
+}  // namespace
+
+forge_status forge_attention_packed_plan_bytes(const forge_attn_packed_cfg* cfg, size_t* bytes) {
+  if (forge_status s = check_attn_packed(cfg)) return s;
+  FORGE_CHECK(bytes != nullptr, FORGE_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = PackedCfg(*cfg).bytes;
+  return ok();
+}
+
+forge_status forge_attention_packed_plan(const forge_attn_packed_cfg* cfg, const int32_t* offsets,
+                                         void* plan, int32_t* positions, forge_stream stream) {
+  if (forge_status s = check_attn_packed(cfg)) return s;
+  FORGE_CHECK(offsets != nullptr, FORGE_ERR_INVALID_ARG, "offsets is NULL");
+  FORGE_CHECK(((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(positions)) &
+               3u) == 0,
+              FORGE_ERR_ALIGNMENT, "offsets or positions is not 4-byte aligned");
+  FORGE_PTR(plan);
+  const PackedCfg p(*cfg);
+  FORGE_CHECK(!overlap(plan, p.bytes, offsets, ((size_t)cfg->n_seqs + 1) * 4) &&
+                  !overlap(plan, p.bytes, positions, (size_t)cfg->tokens * 4) &&
+                  !overlap(positions, (size_t)cfg->tokens * 4, offsets,
+                           ((size_t)cfg->n_seqs + 1) * 4),
+              FORGE_ERR_INVALID_ARG, "plan, positions and offsets overlap");
+  FORGE_HIP(forge::attn_packed_plan(p, offsets, plan, positions, (hipStream_t)stream));
+  return ok();
+}
+
+forge_status forge_attention_packed_fwd(const forge_attn_packed_cfg* cfg, const void* plan,
+                                        const forge_bf16* qkv, forge_bf16* o, float* lse,
+                                        forge_stream stream) {
+  if (forge_status s = check_attn_packed(cfg)) return s;
+  FORGE_PTR(plan);
+  FORGE_PTR(qkv);
+  FORGE_PTR(o);
+  FORGE_PTR(lse);
+  const PackedCfg p(*cfg);
+  const PackedArgs a(*cfg, p, plan, qkv);
+  const size_t rows = (size_t)cfg->tokens * 2;
+  FORGE_CHECK(!overlap(o, rows * cfg->n_heads * cfg->head_dim, qkv, rows * a.ld_qkv),
+              FORGE_ERR_INVALID_ARG, "o overlaps qkv");
+  FORGE_HIP(forge::attn_packed_fwd(a, p, o, lse, (hipStream_t)stream));
+  return ok();
+}
+
+forge_status forge_attention_packed_bwd_workspace_bytes(const forge_attn_packed_cfg* cfg,
+                                                        size_t* bytes) {
+  if (forge_status s = check_attn_packed(cfg)) return s;
+  FORGE_CHECK(bytes != nullptr, FORGE_ERR_INVALID_ARG, "bytes is NULL");
+  const PackedCfg p(*cfg);
+  const PackedArgs a(*cfg, p, nullptr, nullptr);
+  *bytes = up(2 * (size_t)cfg->n_heads * cfg->tokens * 4) +
+           up((size_t)cfg->n_heads * a.ds_head * 2) + up(forge::attn_packed_bwd_part_bytes(a, p));
+  return ok();
+}
+
+forge_status forge_attention_packed_bwd(const forge_attn_packed_cfg* cfg, const void* plan,
+                                        const forge_bf16* qkv, const forge_bf16* o,
+                                        const float* lse, const forge_bf16* d_o,
+                                        forge_bf16* d_qkv, void* workspace, forge_stream stream) {
+  if (forge_status s = check_attn_packed(cfg)) return s;
+  FORGE_PTR(plan);
+  FORGE_PTR(qkv);
+  FORGE_PTR(o);
+  FORGE_PTR(lse);
+  FORGE_PTR(d_o);
+  FORGE_PTR(d_qkv);
+  FORGE_PTR(workspace);
+  const PackedCfg p(*cfg);
+  const PackedArgs a(*cfg, p, plan, qkv);
+  const size_t rows = (size_t)cfg->tokens * 2;
+  const size_t n = rows * a.ld_qkv, no = rows * cfg->n_heads * cfg->head_dim;
+  FORGE_CHECK(!overlap(d_qkv, n, qkv, n) && !overlap(d_qkv, n, o, no) &&
+                  !overlap(d_qkv, n, d_o, no),
+              FORGE_ERR_INVALID_ARG, "d_qkv overlaps an input");
+  const long hq = (long)cfg->n_heads * cfg->head_dim, hkv = (long)cfg->n_kv_heads * cfg->head_dim;
+  const size_t ds_off = up(2 * (size_t)cfg->n_heads * cfg->tokens * 4);
+  const size_t part_off = ds_off + up((size_t)cfg->n_heads * a.ds_head * 2);
+  FORGE_HIP(forge::attn_packed_bwd(a, p, o, d_o, lse, static_cast<float*>(workspace),
+                                   at<uint16_t>(workspace, ds_off), at<float>(workspace, part_off),
+                                   d_qkv, d_qkv + hq, d_qkv + hq + hkv, a.ld_qkv,
+                                   (hipStream_t)stream));
+  return ok();
+}
+
 }  // extern "C"

@@ -251,9 +251,64 @@ struct AttnWindowArgs : AttnArgs {
   const uint16_t* o = nullptr;
   const float* lse = nullptr;
 };
+// Packed sequences: rows [start, start + len) of a packed row, one sequence of many.
+struct PackedTile {
+  int32_t start, len;   // the sequence's
+  int32_t tile;         // which of its tiles
+  int32_t base;         // its first block of dS (DsPacked)
+};
+// Where a sequence's dS lies within a head's: as that of a window over one batch row,
+// from block `base` on.
+struct DsPacked : DsWindow {
+  long base = 0;
+  __host__ __device__ DsPacked(int len, int window, long base_, long head_) : base(base_) {
+    ns = (len + 31) / 32;
+    nwin = min((62 + window) / 32 + 1, ns);
+    cut = (ns - nwin + 1) / 2;
+    tail = (long)cut * nwin - (long)cut * (ns + 1 - cut);
+    head = head_;
+  }
+  __host__ __device__ static int min(int a, int b) { return a < b ? a : b; }
+  __host__ __device__ long blocks() const { return DsWindow::tile((ns + 1) / 2) / 2048; }
+  __host__ __device__ long tile(int kt) const { return 2048L * base + DsWindow::tile(kt); }
+  __host__ __device__ long block(int kt, int j) const { return tile(kt) + 2048L * (j - 2 * kt); }
+};
+// The plan of a packed batch: a header (for which sizes it was made; how many tiles of
+// 64, 128 and 256 rows there are), a list of each kind of tile, and what the builder
+// keeps of every sequence. All of it from the host's bounds alone: each list has room for
+// what the sequences can come to.
+struct PackedHeader {
+  int32_t tokens, n_seqs, max_seq, window;
+  int32_t count[3];
+  int32_t pad;
+};
+struct PackedPlan {
+  int tokens, n_seqs, max_seq, window;   // max_seq and window cut to tokens
+  int cap[3];                            // entries of each list, 64 << i rows
+  size_t tiles[3], bytes;                // where the lists lie
+  long ds_blocks;                        // blocks of dS of a head, at most
+  __host__ PackedPlan(int tokens_, int n_seqs_, int max_seq_, int window_);
+};
+// batch 1, seq the tokens of the packed row.
+struct AttnPackedArgs : AttnArgs {
+  int window;
+  const PackedHeader* plan;
+  const PackedTile* tiles[3];
+  int n_seqs, max_seq;
+  long ds_head;                          // elements of a head's dS
+  float *pk = nullptr, *pv = nullptr;    // the kv pass' partial sums
+  // the forward's outputs
+  const uint16_t* o = nullptr;
+  const float* lse = nullptr;
+};
+// pos (may be NULL): every token's place in its sequence.
+hipError_t attn_packed_plan(const PackedPlan& p, const int32_t* offsets, void* plan, int32_t* pos,
+                            hipStream_t s);
 // o [T, n_heads*d] bf16; lse [batch, n_heads, seq] fp32 (natural log).
 hipError_t attn_fwd(const AttnArgs& a, uint16_t* o, float* lse, hipStream_t s);
 hipError_t attn_window_fwd(const AttnWindowArgs& a, uint16_t* o, float* lse, hipStream_t s);
+hipError_t attn_packed_fwd(const AttnPackedArgs& a, const PackedPlan& p, uint16_t* o, float* lse,
+                           hipStream_t s);
 // Backward. delta: 2 * batch * n_heads * seq fp32 scratch ([b,n,i] =
 // -sum_d dO*O, then [b,n,i] = -lse * log2(e)); ds: attn_bwd_ds_bytes scratch
 // (dS in bf16, the causal half per (batch, head)); part: attn_bwd_part_bytes
@@ -272,6 +327,12 @@ size_t attn_window_bwd_part_bytes(const AttnWindowArgs& a);
 hipError_t attn_window_bwd(const AttnWindowArgs& a, const uint16_t* o, const uint16_t* dout,
                            const float* lse, float* delta, uint16_t* ds, float* part, uint16_t* dq,
                            uint16_t* dk, uint16_t* dv, long ld_dqkv, hipStream_t s);
+// The same of packed sequences; dS: 4096 * n_heads * p.ds_blocks bytes.
+size_t attn_packed_bwd_part_bytes(const AttnPackedArgs& a, const PackedPlan& p);
+hipError_t attn_packed_bwd(const AttnPackedArgs& a, const PackedPlan& p, const uint16_t* o,
+                           const uint16_t* dout, const float* lse, float* delta, uint16_t* ds,
+                           float* part, uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_dqkv,
+                           hipStream_t s);
 
 // ----------------------------------------------------------------- MoE ----
 // Routing of fp32 logits [T, E] (E <= 256): idx / gates [T, k], probs [T, E];

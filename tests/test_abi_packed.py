@@ -177,3 +177,93 @@ def test_adamw_multi_read_refusals():
     assert read([T8], None, None) == OK and read([dict(n=0, master=None)], [None], [None]) == OK
     with pytest.raises(ValueError):
         read([T8, T8], [X], None)
+
+
+# ------------------------------------------------------- packed attention ----
+
+def test_attn_packed_struct_matches_the_c_header(tmp_path):
+    structs = {"forge_attn_packed_cfg": _lib.AttnPackedCfg}
+    assert layout(tmp_path, structs) == ours(structs)
+
+
+def pcfg(**kw):
+    return _lib.attn_packed_cfg(dict(dict(tokens=1000, n_seqs=7, max_seq=300, n_heads=4,
+                                          n_kv_heads=2, head_dim=64, window=0), **kw))
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(tokens=0), INVALID), (dict(n_seqs=0), INVALID), (dict(max_seq=0), INVALID),
+    (dict(window=-1), INVALID), (dict(n_heads=3), INVALID), (dict(n_kv_heads=0), INVALID),
+    (dict(head_dim=96), UNSUPPORTED), (dict(tokens=(1 << 22) + 1), UNSUPPORTED),
+    (dict(n_seqs=(1 << 22) + 1, n_heads=1, n_kv_heads=1), UNSUPPORTED),
+    (dict(tokens=1 << 22, n_heads=64), UNSUPPORTED),
+    (dict(n_seqs=1 << 21, n_heads=4), UNSUPPORTED),
+    (dict(n_heads=1 << 16, n_kv_heads=1 << 16, tokens=1, n_seqs=1), UNSUPPORTED),
+    (dict(tokens=1 << 22, max_seq=1 << 22, n_seqs=1 << 17, n_heads=32), UNSUPPORTED),
+    (dict(tokens=(1 << 31) - 1, n_seqs=(1 << 31) - 1, max_seq=(1 << 31) - 1), UNSUPPORTED)])
+def test_packed_cfg_refusals(kw, want):
+    assert status(_lib.forge_attention_packed_plan_bytes, pcfg(**kw)) == want
+    assert status(_lib.forge_attention_packed_bwd_workspace_bytes, pcfg(**kw)) == want
+    assert status(_lib.forge_attention_packed_plan, pcfg(**kw), X, Y, C, 0) == want
+    assert status(_lib.forge_attention_packed_fwd, pcfg(**kw), P, X, Y, C, 0) == want
+    assert status(_lib.forge_attention_packed_bwd, pcfg(**kw), P, X, Y, C, S, 0x7000000, 0x8000000,
+                  0) == want
+
+
+def test_packed_pointer_refusals():
+    p = _lib.forge_attention_packed_plan
+    assert status(p, pcfg(), None, Y, C, 0) == INVALID
+    assert status(p, pcfg(), X, None, C, 0) == INVALID
+    assert status(p, pcfg(), X + 2, Y, C, 0) == ALIGNMENT
+    assert status(p, pcfg(), X, Y + 8, C, 0) == ALIGNMENT
+    assert status(p, pcfg(), X, Y, C + 1, 0) == ALIGNMENT
+    assert status(p, pcfg(), X, X + 16, C, 0) == INVALID            # plan over offsets
+    assert status(p, pcfg(), X, Y, Y + 16, 0) == INVALID            # positions over plan
+    assert status(p, pcfg(), X, Y, X + 4, 0) == INVALID             # and over offsets
+    f = _lib.forge_attention_packed_fwd
+    ok = dict(plan=P, qkv=X, o=Y, lse=C, stream=0)
+    for name in ("plan", "qkv", "o", "lse"):
+        assert status(f, pcfg(), *dict(ok, **{name: None}).values()) == INVALID, name
+        assert status(f, pcfg(), *dict(ok, **{name: ok[name] + 8}).values()) == ALIGNMENT, name
+    assert status(f, pcfg(), *dict(ok, o=X + 1024).values()) == INVALID
+    b = _lib.forge_attention_packed_bwd
+    ok = dict(plan=P, qkv=X, o=Y, lse=C, do=S, dqkv=0x7000000, ws=0x8000000, stream=0)
+    for name in ("plan", "qkv", "o", "lse", "do", "dqkv", "ws"):
+        assert status(b, pcfg(), *dict(ok, **{name: None}).values()) == INVALID, name
+        assert status(b, pcfg(), *dict(ok, **{name: ok[name] + 8}).values()) == ALIGNMENT, name
+    for name in ("qkv", "o", "do"):
+        assert status(b, pcfg(), *dict(ok, dqkv=ok[name]).values()) == INVALID, name
+
+
+def _blocks(n, window):
+    """4 KB blocks of dS that a sequence of n tokens takes per head."""
+    ns = -(-n // 32)
+    return sum(min(ns - 2 * t, (62 + window) // 32 + 1) for t in range(-(-n // 64)))
+
+
+@pytest.mark.parametrize("tokens,n_seqs,max_seq,window", [
+    (16384, 1, 16384, 0), (16384, 41, 1605, 0), (16384, 4, 6000, 0), (16384, 4, 6000, 500),
+    (5000, 5000, 1, 0), (5000, 5000, 64, 0), (1, 1, 1, 0), (8191, 31, 716, 300), (300, 9, 10 ** 9, 0),
+    (4096, 3, 4096, 1), (130, 3, 65, 0), (100000, 700, 3000, 2000)])
+def test_packed_workspace_holds_whatever_the_lengths(tokens, n_seqs, max_seq, window):
+    """Lengths drawn to the configuration's bounds, long and short: their score gradients fit,
+    and the bound is that of full sequences and a tile more for each."""
+    import random
+    heads = 4
+    cfg = _lib.AttnPackedCfg(tokens, n_seqs, max_seq, heads, 2, 64, window)
+    got = _lib.forge_attention_packed_bwd_workspace_bytes(cfg)
+    room = (got - 8 * heads * tokens) // (4096 * heads)
+    m, w = min(max_seq, tokens), window or tokens
+    rng = random.Random(1)
+    for k in range(40):
+        left, used = tokens, 0
+        for s in range(n_seqs):
+            n = min(left, m if k == 0 or rng.random() < 0.5 else rng.choice(
+                (0, 1, 63, 64, 65, rng.randint(0, m))), m)
+            left -= n
+            used += _blocks(n, w)
+        assert used <= room
+    tiles = (tokens + 63 * min(n_seqs, tokens)) // 64
+    full = -(-m // 64)
+    assert got <= 8 * heads * tokens + 4096 * heads * tiles * (_blocks(full * 64, w) // full + 1) \
+        + 1024 + (64 << 20)

@@ -171,3 +171,59 @@ def test_zero_tiny_and_small_blocks():
     v[0], v[1] = 1.0, 1e-30
     q, s = packed.encode_v(v, np.full(256, np.float32(0.99)))
     assert q[0] == 255 and q[1] == 1 and not q[2:].any()
+
+
+# ------------------------------------------------------- packed attention ----
+
+def _qkv(rng, T, nh=2, nkv=1, d=4):
+    return (rng.standard_normal((T, nh, d)), rng.standard_normal((T, nkv, d)),
+            rng.standard_normal((T, nkv, d)), rng.standard_normal((T, nh, d)))
+
+
+def test_sequences_of_offsets():
+    assert packed.sequences([0, 3, 3, 8], 10, 10) == [(0, 3), (3, 0), (3, 5)]
+    assert packed.sequences([2, 7, 99], 10, 4) == [(2, 4), (7, 3)]
+    assert packed.sequences([-5, 4, 2, 6], 10, 10) == [(0, 4), (4, 0), (4, 2)]
+    assert packed.covered([2, 7, 99], 10, 4).tolist() == [False] * 2 + [True] * 4 + [False] + [True] * 3
+    assert packed.positions([1, 3, 5], 6, 9).tolist() == [-1, 0, 1, 0, 1, -1]
+
+
+def test_packed_attention_is_each_sequence_s_own():
+    rng = np.random.default_rng(21)
+    q, k, v, do = _qkv(rng, 12)
+    off = [0, 5, 5, 6, 11]
+    r = packed.attention(q, k, v, do, off, 12)
+    for a, b in ((0, 5), (5, 6), (6, 11)):
+        o, lse = dense.attention_fwd(q[a:b], k[a:b], v[a:b], 1, b - a)
+        assert np.allclose(r["o"][a:b], o) and np.allclose(r["lse"][:, a:b], lse[0])
+        for got, ref in zip((r["dq"], r["dk"], r["dv"]),
+                            dense.attention_bwd(q[a:b], k[a:b], v[a:b], do[a:b], 1, b - a)):
+            assert np.allclose(got[a:b], ref)
+    assert np.isnan(r["o"][11]).all() and np.isnan(r["dk"][11]).all()
+    # a sequence of one token attends to itself
+    assert np.allclose(r["o"][5], v[5])
+    # other sequences' rows change nothing
+    q2, k2, v2 = (x.copy() for x in (q, k, v))
+    for x in (q2, k2, v2):
+        x[:6] += 3.0
+    r2 = packed.attention(q2, k2, v2, do, off, 12)
+    assert all(np.array_equal(r[n][6:11], r2[n][6:11]) for n in ("o", "dq", "dk", "dv"))
+
+
+@pytest.mark.parametrize("window", [0, 1, 3])
+def test_packed_attention_backward_finite_differences(window):
+    rng = np.random.default_rng(22)
+    q, k, v, do = _qkv(rng, 9)
+    off = [0, 4, 5, 9]
+
+    def f():
+        return float((packed.attention(q, k, v, None, off, 9, window)["o"] * do).sum())
+    r = packed.attention(q, k, v, do, off, 9, window)
+    for got, wrt in ((r["dq"], q), (r["dk"], k), (r["dv"], v)):
+        diff = central_diff(f, wrt, np.arange(wrt.size))
+        if window == 1 and wrt is not v:
+            # one visible key has weight 1 whatever its score: no gradient but fp64 rounding
+            # of dP - delta (two sums of four products below 20 each), and no relative error
+            assert not diff.any() and np.abs(got).max() <= 4 * 20 * 2.0 ** -52
+        else:
+            assert rel_err(got.ravel(), diff) <= 1e-6
