@@ -621,8 +621,8 @@ typedef struct {
 /*
  * tensors: host array [n_tensors], read during the call (a captured graph keeps
  * the pointers). Every buffer that is written has to be a tensor's own. n may be
- * 0 (the tensor is skipped, its pointers may be NULL); n < 2^40 each, n_tensors
- * <= 2^20. hp, dev_scalars: as in forge_adamw_step. state_bits other than 8 and
+ * 0 (the tensor is skipped, its pointers may be NULL); n <= 2^35 each, n_tensors
+ * <= 2^20 (else UNSUPPORTED). hp, dev_scalars: as in forge_adamw_step. state_bits other than 8 and
  * 32: INVALID_ARG.
  */
 forge_status forge_adamw_multi_step(const forge_adamw_multi_tensor* tensors, int32_t n_tensors,

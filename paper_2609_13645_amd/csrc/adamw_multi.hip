@@ -56,107 +56,237 @@ __device__ __forceinline__ int encode_v(float v, float inv, float u) {
   return x > 0.0f ? (int)c : 0;
 }
 
-__device__ __forceinline__ float grad_at(const void* g, int64_t i, bool bf16) {
-  return bf16 ? bf2f(static_cast<const bf16_t*>(g)[i]) : static_cast<const float*>(g)[i];
+// The workgroup's tensor and its first element there.
+__device__ __forceinline__ const AdamTensor& tensor_of(const AdamBatch& b, int64_t& first) {
+  int i = 0;
+#pragma unroll
+  for (int step = kAdamBatch / 2; step; step /= 2)
+    if ((int)blockIdx.x >= b.end[i + step - 1]) i += step;
+  first = (int64_t)((int)blockIdx.x - (i ? b.end[i - 1] : 0)) * kAdamChunk;
+  return b.t[i];
 }
 
-// Moments in 32 bits: a thread an element.
-__global__ __launch_bounds__(256) void adamw_multi_32_k(AdamTensor t, AdamHyper h, bool bf16) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= t.n) return;
-  float p = t.master[i], m = static_cast<float*>(t.m)[i], v = static_cast<float*>(t.v)[i];
-  adam1(p, m, v, grad_at(t.grad, i, bf16), h.b1, h.b2, h.eps, h.wd * t.decay_scale,
-        h.sc[0] * t.lr_scale, 1.0f / h.sc[1], 1.0f / h.sc[2], h.sc[3]);
-  t.master[i] = p;
-  static_cast<float*>(t.m)[i] = m;
-  static_cast<float*>(t.v)[i] = v;
-  t.param[i] = f2bf(p);
-}
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
-// Moments in 8 bits: a wave a block of 256, four neighbours to a lane.
-__global__ __launch_bounds__(256) void adamw_multi_8_k(AdamTensor t, AdamHyper h, bool bf16) {
-#pragma clang fp contract(off)
-  const int lane = threadIdx.x & 63;
-  const int64_t b = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t i0 = b * kBlock + lane * 4;
-  if (b * kBlock >= t.n) return;
+// Four neighbours from element i on, as floats; those at or past n are zeros. Every buffer
+// is read and written once in a step: nontemporal, as in the plain update.
+template <typename T>
+__device__ __forceinline__ T load_nt(const void* p, int64_t i) {
+  return __builtin_nontemporal_load(reinterpret_cast<const T*>(static_cast<const char*>(p)) + i);
+}
+template <typename T>
+__device__ __forceinline__ void store_nt(void* p, int64_t i, T x) {
+  __builtin_nontemporal_store(x, reinterpret_cast<T*>(p) + i);
+}
+__device__ __forceinline__ f32x4_t load4(const float* p, int64_t i, int64_t n) {
+  if (i + 4 <= n) return load_nt<f32x4_t>(p, i / 4);
+  f32x4_t x = {};
+  for (int e = 0; e < 4; ++e)
+    if (i + e < n) x[e] = p[i + e];
+  return x;
+}
+__device__ __forceinline__ void store4(float* p, int64_t i, int64_t n, f32x4_t x) {
+  if (i + 4 <= n) return store_nt<f32x4_t>(p, i / 4, x);
+  for (int e = 0; e < 4; ++e)
+    if (i + e < n) p[i + e] = x[e];
+}
+// (bf16 and codes stay packed until they are used)
+__device__ __forceinline__ u32x2_t load4(const bf16_t* p, int64_t i, int64_t n) {
+  if (i + 4 <= n) return load_nt<u32x2_t>(p, i / 4);
+  u32x2_t x = {};
+  for (int e = 0; e < 4; ++e)
+    if (i + e < n) x[e / 2] |= (uint32_t)p[i + e] << 16 * (e % 2);
+  return x;
+}
+__device__ __forceinline__ void store4(bf16_t* p, int64_t i, int64_t n, f32x4_t f) {
+  const u32x2_t x = {pack2(f[0], f[1]), pack2(f[2], f[3])};
+  if (i + 4 <= n) return store_nt<u32x2_t>(p, i / 4, x);
+  for (int e = 0; e < 4; ++e)
+    if (i + e < n) p[i + e] = (bf16_t)(x[e / 2] >> 16 * (e % 2));
+}
+__device__ __forceinline__ uint32_t load4(const uint8_t* p, int64_t i, int64_t n) {
+  if (i + 4 <= n) return load_nt<uint32_t>(p, i / 4);
+  uint32_t x = 0;
+  for (int e = 0; e < 4; ++e)
+    if (i + e < n) x |= (uint32_t)p[i + e] << 8 * e;
+  return x;
+}
+__device__ __forceinline__ void store4(uint8_t* p, int64_t i, int64_t n, uint32_t x) {
+  if (i + 4 <= n) return store_nt<uint32_t>(p, i / 4, x);
+  for (int e = 0; e < 4; ++e)
+    if (i + e < n) p[i + e] = (uint8_t)(x >> 8 * e);
+}
+// Gradients of four neighbours.
+template <bool BF16>
+struct Grad;
+template <>
+struct Grad<false> {
+  f32x4_t x;
+  __device__ __forceinline__ Grad(const void* p, int64_t i, int64_t n)
+      : x(load4(static_cast<const float*>(p), i, n)) {}
+  __device__ __forceinline__ float operator[](int e) const { return x[e]; }
+};
+template <>
+struct Grad<true> {
+  u32x2_t x;
+  __device__ __forceinline__ Grad(const void* p, int64_t i, int64_t n)
+      : x(load4(static_cast<const bf16_t*>(p), i, n)) {}
+  __device__ __forceinline__ float operator[](int e) const {
+    return e % 2 ? hi_f(x[e / 2]) : lo_f(x[e / 2]);
+  }
+};
+
+// Moments in 32 bits: four times four neighbours to a thread, 4 KB apart.
+template <bool BF16>
+__global__ __launch_bounds__(256) void adamw_multi_32_k(AdamBatch b, AdamHyper h) {
+  int64_t i0;
+  const AdamTensor& t = tensor_of(b, i0);
   const float lr = h.sc[0] * t.lr_scale, ibc1 = 1.0f / h.sc[1], ibc2 = 1.0f / h.sc[2];
-  const float unit_m = t.m_scale[b] * (1.0f / 16129.0f), sv = t.v_scale[b];
-  const uint32_t key = h.seed ? mixed(mixed((uint32_t)*h.seed) + t.index) : 0;
-  float m[4], v[4];
-  float top_m = 0.0f, top_v = 0.0f;
-  bool bad = false;
-  for (int e = 0; e < 4; ++e) {
-    m[e] = v[e] = 0.0f;
-    const int64_t i = i0 + e;
-    if (i >= t.n) continue;
-    const float g = grad_at(t.grad, i, bf16) * h.sc[3];
-    m[e] = decode_m(static_cast<int8_t*>(t.m)[i], unit_m) * h.b1 + (1.0f - h.b1) * g;
-    v[e] = decode_v(static_cast<uint8_t*>(t.v)[i], sv) * h.b2 + ((1.0f - h.b2) * g) * g;
-    bad = bad || !(fabsf(m[e]) < INFINITY) || !(v[e] < INFINITY);
-    top_m = fmaxf(top_m, fabsf(m[e]));
-    top_v = fmaxf(top_v, v[e]);
-    const float p = t.master[i];
-    const float upd = __builtin_fmaf(h.wd * t.decay_scale, p,
-                                     (m[e] * ibc1) / (sqrtf(v[e] * ibc2) + h.eps));
-    const float q = __builtin_fmaf(-lr, upd, p);
-    t.master[i] = q;
-    t.param[i] = f2bf(q);
-  }
-  top_m = wave_max(top_m);
-  top_v = wave_max(top_v);
-  bad = __any(bad);
-  const float inv_m = top_m < kTiny ? 0.0f : 16129.0f * (1.0f / top_m);
-  const float inv_v = top_v < kTiny ? 0.0f : 4228250625.0f * (1.0f / top_v);
-  for (int e = 0; e < 4; ++e) {
-    const int64_t i = i0 + e;
-    if (i >= t.n) continue;
-    const uint32_t r = mixed((uint32_t)i ^ key);
-    const float um = h.seed ? ((float)(r & 0xFFFF) + 0.5f) * 0x1p-16f : 0.5f;
-    const float uv = h.seed ? ((float)(r >> 16) + 0.5f) * 0x1p-16f : 0.5f;
-    static_cast<int8_t*>(t.m)[i] = (int8_t)(bad ? 0 : encode_m(m[e], inv_m, um));
-    static_cast<uint8_t*>(t.v)[i] = (uint8_t)(bad ? 0 : encode_v(v[e], inv_v, uv));
-  }
-  if (lane == 0) {
-    t.m_scale[b] = bad ? NAN : top_m < kTiny ? 0.0f : top_m;
-    t.v_scale[b] = bad ? NAN : top_v < kTiny ? 0.0f : top_v;
+  const float clip = h.sc[3], wd = h.wd * t.decay_scale;
+#pragma unroll
+  for (int k = 0; k < kAdamChunk / 1024; ++k) {
+    const int64_t i = i0 + k * 1024 + threadIdx.x * 4;
+    if (i >= t.n) return;
+    f32x4_t p = load4(t.master, i, t.n), m = load4(static_cast<float*>(t.m), i, t.n);
+    f32x4_t v = load4(static_cast<float*>(t.v), i, t.n);
+    const Grad<BF16> g(t.grad, i, t.n);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float pe = p[e], me = m[e], ve = v[e];
+      adam1(pe, me, ve, g[e], h.b1, h.b2, h.eps, wd, lr, ibc1, ibc2, clip);
+      p[e] = pe;
+      m[e] = me;
+      v[e] = ve;
+    }
+    store4(t.master, i, t.n, p);
+    store4(static_cast<float*>(t.m), i, t.n, m);
+    store4(static_cast<float*>(t.v), i, t.n, v);
+    store4(t.param, i, t.n, p);
   }
 }
 
-// A thread an element's values.
-__global__ __launch_bounds__(256) void adamw_multi_read_k(AdamTensor t, bool bf16) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= t.n) return;
-  const auto put = [&](void* out, float x) {
-    if (bf16) static_cast<bf16_t*>(out)[i] = f2bf(x);
-    else static_cast<float*>(out)[i] = x;
-  };
-  if (t.m_out)
-    put(t.m_out,
-        decode_m(static_cast<int8_t*>(t.m)[i], t.m_scale[i / kBlock] * (1.0f / 16129.0f)));
-  if (t.v_out) put(t.v_out, decode_v(static_cast<uint8_t*>(t.v)[i], t.v_scale[i / kBlock]));
+// Moments in 8 bits: a wave takes kPer blocks of 256 one behind another, four neighbours
+// of each to a lane, all of them loaded first.
+constexpr int kPer = kAdamChunk / kBlock / 4;
+template <bool BF16>
+__global__ __launch_bounds__(256) void adamw_multi_8_k(AdamBatch bt, AdamHyper h) {
+#pragma clang fp contract(off)
+  int64_t i0;
+  const AdamTensor& t = tensor_of(bt, i0);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n = t.n, b0 = i0 / kBlock + wave * kPer;
+  const float lr = h.sc[0] * t.lr_scale, ibc1 = 1.0f / h.sc[1], ibc2 = 1.0f / h.sc[2];
+  const float clip = h.sc[3], wd = h.wd * t.decay_scale;
+  const uint32_t key = h.seed ? mixed(mixed((uint32_t)*h.seed) + t.index) : 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int64_t b = b0 + k, i = b * kBlock + lane * 4;
+    if (b * kBlock >= n) return;
+    f32x4_t p = load4(t.master, i, n);
+    const Grad<BF16> g(t.grad, i, n);
+    uint32_t qm = load4(static_cast<uint8_t*>(t.m), i, n);
+    uint32_t qv = load4(static_cast<uint8_t*>(t.v), i, n);
+    const float unit_m = t.m_scale[b] * (1.0f / 16129.0f), sv = t.v_scale[b];
+    float m[4], v[4], top_m = 0.0f, top_v = 0.0f;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = g[e] * clip;
+      m[e] = decode_m((int8_t)(qm >> 8 * e), unit_m) * h.b1 + (1.0f - h.b1) * x;
+      v[e] = decode_v((uint8_t)(qv >> 8 * e), sv) * h.b2 + ((1.0f - h.b2) * x) * x;
+      bad = bad || !(fabsf(m[e]) < INFINITY) || !(v[e] < INFINITY);
+      top_m = fmaxf(top_m, fabsf(m[e]));
+      top_v = fmaxf(top_v, v[e]);
+      const float upd =
+          __builtin_fmaf(wd, p[e], (m[e] * ibc1) / (sqrtf(v[e] * ibc2) + h.eps));
+      p[e] = __builtin_fmaf(-lr, upd, p[e]);
+    }
+    store4(t.master, i, n, p);
+    store4(t.param, i, n, p);
+    top_m = wave_max(top_m);
+    top_v = wave_max(top_v);
+    bad = __any(bad);
+    const float inv_m = top_m < kTiny ? 0.0f : 16129.0f * (1.0f / top_m);
+    const float inv_v = top_v < kTiny ? 0.0f : 4228250625.0f * (1.0f / top_v);
+    qm = qv = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t r = mixed((uint32_t)(i + e) ^ key);
+      const float um = h.seed ? ((float)(r & 0xFFFF) + 0.5f) * 0x1p-16f : 0.5f;
+      const float uv = h.seed ? ((float)(r >> 16) + 0.5f) * 0x1p-16f : 0.5f;
+      qm |= (uint32_t)(encode_m(m[e], inv_m, um) & 255) << 8 * e;
+      qv |= (uint32_t)encode_v(v[e], inv_v, uv) << 8 * e;
+    }
+    store4(static_cast<uint8_t*>(t.m), i, n, bad ? 0u : qm);
+    store4(static_cast<uint8_t*>(t.v), i, n, bad ? 0u : qv);
+    if (lane == 0) {
+      t.m_scale[b] = bad ? NAN : top_m < kTiny ? 0.0f : top_m;
+      t.v_scale[b] = bad ? NAN : top_v < kTiny ? 0.0f : top_v;
+    }
+  }
+}
+
+// Values of four times four neighbours to a thread, a lane's of a wave's block.
+template <bool BF16>
+__global__ __launch_bounds__(256) void adamw_multi_read_k(AdamBatch bt) {
+  int64_t i0;
+  const AdamTensor& t = tensor_of(bt, i0);
+  const int64_t n = t.n;
+#pragma unroll
+  for (int k = 0; k < kAdamChunk / 1024; ++k) {
+    const int64_t i = i0 + k * 1024 + threadIdx.x * 4;
+    if (i >= n) return;
+    const auto put = [&](void* out, f32x4_t x) {
+      if constexpr (BF16) store4(static_cast<bf16_t*>(out), i, n, x);
+      else store4(static_cast<float*>(out), i, n, x);
+    };
+    f32x4_t x;
+    if (t.m_out) {
+      const uint32_t q = load4(static_cast<uint8_t*>(t.m), i, n);
+      const float unit = t.m_scale[i / kBlock] * (1.0f / 16129.0f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = decode_m((int8_t)(q >> 8 * e), unit);
+      put(t.m_out, x);
+    }
+    if (t.v_out) {
+      const uint32_t q = load4(static_cast<uint8_t*>(t.v), i, n);
+      const float scale = t.v_scale[i / kBlock];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = decode_v((uint8_t)(q >> 8 * e), scale);
+      put(t.v_out, x);
+    }
+  }
+}
+
+// The batch's ends padded for the search, and the grid of its launch.
+dim3 close(AdamBatch& b) {
+  for (int i = b.count; i < kAdamBatch; ++i) b.end[i] = INT32_MAX;
+  return dim3((unsigned)b.chunks);
 }
 
 }  // namespace
 
-hipError_t adamw_multi(const AdamTensor* t, int n, int bits, bool grad_bf16, const AdamHyper& h,
-                       hipStream_t s) {
-  for (int i = 0; i < n; ++i) {
-    if (bits == 32) {
-      hipLaunchKernelGGL(adamw_multi_32_k, dim3((unsigned)((t[i].n + 255) / 256)), dim3(256), 0, s,
-                         t[i], h, grad_bf16);
-    } else {
-      hipLaunchKernelGGL(adamw_multi_8_k, dim3((unsigned)((t[i].n + 1023) / 1024)), dim3(256), 0,
-                         s, t[i], h, grad_bf16);
-    }
+hipError_t adamw_multi(AdamBatch& b, int bits, bool grad_bf16, const AdamHyper& h, hipStream_t s) {
+  if (b.count == 0) return hipSuccess;
+  const dim3 grid = close(b), block(256);
+  if (bits == 32) {
+    if (grad_bf16) hipLaunchKernelGGL(adamw_multi_32_k<true>, grid, block, 0, s, b, h);
+    else hipLaunchKernelGGL(adamw_multi_32_k<false>, grid, block, 0, s, b, h);
+  } else {
+    if (grad_bf16) hipLaunchKernelGGL(adamw_multi_8_k<true>, grid, block, 0, s, b, h);
+    else hipLaunchKernelGGL(adamw_multi_8_k<false>, grid, block, 0, s, b, h);
   }
+  b.count = b.chunks = 0;
   return hipGetLastError();
 }
 
-hipError_t adamw_multi_read(const AdamTensor* t, int n, bool out_bf16, hipStream_t s) {
-  for (int i = 0; i < n; ++i)
-    hipLaunchKernelGGL(adamw_multi_read_k, dim3((unsigned)((t[i].n + 255) / 256)), dim3(256), 0, s,
-                       t[i], out_bf16);
+hipError_t adamw_multi_read(AdamBatch& b, bool out_bf16, hipStream_t s) {
+  if (b.count == 0) return hipSuccess;
+  const dim3 grid = close(b), block(256);
+  if (out_bf16) hipLaunchKernelGGL(adamw_multi_read_k<true>, grid, block, 0, s, b);
+  else hipLaunchKernelGGL(adamw_multi_read_k<false>, grid, block, 0, s, b);
+  b.count = b.chunks = 0;
   return hipGetLastError();
 }
 

@@ -1773,7 +1773,7 @@ forge_status check_adamw_list(const forge_adamw_multi_tensor* t, int32_t n) {
   FORGE_CHECK(n == 0 || t != nullptr, FORGE_ERR_INVALID_ARG, "tensors is NULL");
   for (int i = 0; i < n; ++i) {
     FORGE_CHECK(t[i].n >= 0, FORGE_ERR_INVALID_ARG, "tensors[%d].n must be >= 0", i);
-    FORGE_CHECK(t[i].n < 1LL << 40, FORGE_ERR_UNSUPPORTED, "tensors[%d].n >= 2^40", i);
+    FORGE_CHECK(t[i].n <= 1LL << 35, FORGE_ERR_UNSUPPORTED, "tensors[%d].n > 2^35", i);
   }
   return FORGE_OK;
 }
@@ -1823,13 +1823,18 @@ forge_status forge_adamw_multi_step(const forge_adamw_multi_tensor* tensors, int
               "dev_seed is not 4-byte aligned");
   const forge::AdamHyper h{hp->beta1,        hp->beta2,   hp->eps,
                            hp->weight_decay, dev_scalars, state_bits == 8 ? dev_seed : nullptr};
-  forge::AdamTensor batch[forge::kAdamBatch];
-  for (int i = 0, n = 0; i < n_tensors; ++i) {
-    if (tensors[i].n > 0) batch[n++] = adamw_tensor(tensors[i], i);
-    if (n < forge::kAdamBatch && (i + 1 < n_tensors || n == 0)) continue;
-    FORGE_HIP(forge::adamw_multi(batch, n, state_bits, grad_bf16 != 0, h, (hipStream_t)stream));
-    n = 0;
+  forge::AdamBatch batch;
+  const auto launch = [&] {
+    return forge::adamw_multi(batch, state_bits, grad_bf16 != 0, h, (hipStream_t)stream);
+  };
+  for (int i = 0; i < n_tensors; ++i) {
+    if (tensors[i].n == 0) continue;
+    const forge::AdamTensor t = adamw_tensor(tensors[i], i);
+    if (batch.add(t)) continue;
+    FORGE_HIP(launch());
+    batch.add(t);
   }
+  FORGE_HIP(launch());
   return ok();
 }
 
@@ -1852,17 +1857,17 @@ forge_status forge_adamw_multi_read(const forge_adamw_multi_tensor* tensors, int
         if (forge_status e = check_adamw_buffer(v[k], i)) return e;
     }
   }
-  forge::AdamTensor batch[forge::kAdamBatch];
-  for (int i = 0, n = 0; i < n_tensors; ++i) {
-    if (tensors[i].n > 0) {
-      batch[n] = adamw_tensor(tensors[i], i);
-      batch[n].m_out = m_out ? m_out[i] : nullptr;
-      batch[n++].v_out = v_out ? v_out[i] : nullptr;
-    }
-    if (n < forge::kAdamBatch && (i + 1 < n_tensors || n == 0)) continue;
-    FORGE_HIP(forge::adamw_multi_read(batch, n, out_bf16 != 0, (hipStream_t)stream));
-    n = 0;
+  forge::AdamBatch batch;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (tensors[i].n == 0) continue;
+    forge::AdamTensor t = adamw_tensor(tensors[i], i);
+    t.m_out = m_out ? m_out[i] : nullptr;
+    t.v_out = v_out ? v_out[i] : nullptr;
+    if (batch.add(t)) continue;
+    FORGE_HIP(forge::adamw_multi_read(batch, out_bf16 != 0, (hipStream_t)stream));
+    batch.add(t);
   }
+  FORGE_HIP(forge::adamw_multi_read(batch, out_bf16 != 0, (hipStream_t)stream));
   return ok();
 }
 

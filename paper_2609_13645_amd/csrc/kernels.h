@@ -146,16 +146,30 @@ struct AdamTensor {
   uint32_t index;
   void *m_out, *v_out;  // of a read: where the moments' values go (NULL: nowhere)
 };
-constexpr int kAdamBatch = 32;   // tensors of a call below, at most
 struct AdamHyper {
   float b1, b2, eps, wd;
   const float* sc;      // device {lr, 1 - b1^t, 1 - b2^t, clip}
   const int32_t* seed;  // device, NULL: codes to the nearest
 };
-// t: host array of 1 to kAdamBatch tensors, none of them empty; bits 32 or 8.
-hipError_t adamw_multi(const AdamTensor* t, int n, int bits, bool grad_bf16, const AdamHyper& h,
-                       hipStream_t s);
-hipError_t adamw_multi_read(const AdamTensor* t, int n, bool out_bf16, hipStream_t s);
+// The tensors of a launch, which takes them by value: tensor i has the workgroups from
+// end[i - 1] (0) to end[i], one for kAdamChunk of its elements.
+constexpr int kAdamBatch = 32, kAdamChunk = 4096;
+struct AdamBatch {
+  AdamTensor t[kAdamBatch];
+  int32_t end[kAdamBatch];
+  int32_t count = 0, chunks = 0;
+  // false: the launch is full (n <= 2^35)
+  bool add(const AdamTensor& x) {
+    const int32_t c = (int32_t)((x.n + kAdamChunk - 1) / kAdamChunk);
+    if (count == kAdamBatch || (count > 0 && chunks + c > 1 << 23)) return false;
+    t[count] = x;
+    end[count++] = chunks += c;
+    return true;
+  }
+};
+// Launches of the batch's tensors, which is empty again behind them; bits 32 or 8.
+hipError_t adamw_multi(AdamBatch& b, int bits, bool grad_bf16, const AdamHyper& h, hipStream_t s);
+hipError_t adamw_multi_read(AdamBatch& b, bool out_bf16, hipStream_t s);
 
 // ----------------------------------------------------------- LayerNorm ----
 hipError_t layernorm_fwd(const uint16_t* x, const uint16_t* g, const uint16_t* b, uint16_t* y,
