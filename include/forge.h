@@ -621,7 +621,7 @@ typedef struct {
 /*
  * tensors: host array [n_tensors], read during the call (a captured graph keeps
  * the pointers). Every buffer that is written has to be a tensor's own. n may be
- * 0 (the tensor is skipped, its pointers may be NULL); n <= 2^35 each, n_tensors
+ * 0 (the tensor is skipped, its pointers may be NULL); n <= 2^33 each, n_tensors
  * <= 2^20 (else UNSUPPORTED). hp, dev_scalars: as in forge_adamw_step. state_bits other than 8 and
  * 32: INVALID_ARG.
  */

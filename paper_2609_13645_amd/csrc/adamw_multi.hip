@@ -12,6 +12,8 @@
 // whatever computes it. The roots are the hardware's, one step of the last bit off at
 // most: at a border the code below has probability 2^-17 or less of being taken,
 // which no drawn number reaches.)
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -27,33 +29,51 @@ __host__ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ float decode_m(int q, float unit) {
-  return (float)(q * abs(q)) * unit;
-}
-__device__ __forceinline__ float decode_v(int q, float scale) {
+// (Multiply-adds below stand where the product is exact, so that they round once as the
+// operations that they join.)
+__device__ __forceinline__ float decode_m(int8_t code, float unit) {
 #pragma clang fp contract(off)
-  const float c = (float)(q * q) * (1.0f / 65025.0f);
+  const float q = (float)code;
+  return (q * fabsf(q)) * unit;
+}
+__device__ __forceinline__ float decode_v(uint8_t code, float scale) {
+#pragma clang fp contract(off)
+  const float q = (float)code, c = (q * q) * (1.0f / 65025.0f);
   return (c * c) * scale;
 }
 // Code of |m|: a = |m| / scale * 127^2 lies between q^2 and (q + 1)^2.
 __device__ __forceinline__ int encode_m(float m, float inv, float u) {
 #pragma clang fp contract(off)
-  const float a = fabsf(m) * inv;
-  const float q = floorf(__builtin_amdgcn_sqrtf(a));
-  const float up = u * (2.0f * q + 1.0f) < a - q * q ? 1.0f : 0.0f;
-  const int c = (int)fminf(q + up, 127.0f);
+  const float a = fabsf(m) * inv, q = floorf(__builtin_amdgcn_sqrtf(a));
+  const bool up = u * __builtin_fmaf(2.0f, q, 1.0f) < __builtin_fmaf(-q, q, a);
+  const int c = (int)fminf(q, up ? 126.0f : 127.0f) + up;
   return m < 0.0f ? -c : c;
 }
 // Code of v: x = v / scale * 255^4 lies between q^4 and (q + 1)^4.
-__device__ __forceinline__ int encode_v(float v, float inv, float u) {
+__device__ __forceinline__ float encode_v(float v, float inv, float u) {
 #pragma clang fp contract(off)
-  const float x = v * inv;
-  const float q = floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(x)));
-  const float lo2 = q * q, hi2 = (q + 1.0f) * (q + 1.0f);
-  const float lo = lo2 * lo2, hi = hi2 * hi2;
-  const float up = u * (hi - lo) < x - lo ? 1.0f : 0.0f;
-  const float c = fminf(fmaxf(q + up, 1.0f), 255.0f);
-  return x > 0.0f ? (int)c : 0;
+  const float x = v * inv, q = floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(x)));
+  const float q1 = q + 1.0f, lo2 = q * q, hi2 = q1 * q1, lo = lo2 * lo2, hi = hi2 * hi2;
+  const float c = u * (hi - lo) < x - lo ? q1 : q;
+  return x > 0.0f ? __builtin_amdgcn_fmed3f(c, 1.0f, 255.0f) : 0.0f;
+}
+
+// Largest of the wave's 64 unsigned values, in every lane: the rows of 16 by shifted
+// moves on the VALU, then across rows; lane 63 has it.
+__device__ __forceinline__ uint32_t wave_top(uint32_t x) {
+  const auto step = [&](auto ctrl) {
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF,
+                                                             0xF, false);
+    x = x > y ? x : y;
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{});   // from 1, 2, 4, 8 lanes before, in the row
+  step(integral_constant<int, 0x112>{});
+  step(integral_constant<int, 0x114>{});
+  step(integral_constant<int, 0x118>{});
+  step(integral_constant<int, 0x142>{});   // the row before's last lane
+  step(integral_constant<int, 0x143>{});   // lane 31
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
 // The workgroup's tensor and its first element there.
@@ -62,7 +82,7 @@ __device__ __forceinline__ const AdamTensor& tensor_of(const AdamBatch& b, int64
 #pragma unroll
   for (int step = kAdamBatch / 2; step; step /= 2)
     if ((int)blockIdx.x >= b.end[i + step - 1]) i += step;
-  first = (int64_t)((int)blockIdx.x - (i ? b.end[i - 1] : 0)) * kAdamChunk;
+  first = (int64_t)((int)blockIdx.x - (i ? b.end[i - 1] : 0)) * b.chunk;
   return b.t[i];
 }
 
@@ -136,38 +156,38 @@ struct Grad<true> {
   }
 };
 
-// Moments in 32 bits: four times four neighbours to a thread, 4 KB apart.
+// Moments in 32 bits: four neighbours to a thread. 218 M parameters in five tensors: 1088 us,
+// 6.0 TB/s; as four times four to a thread 1165.
 template <bool BF16>
 __global__ __launch_bounds__(256) void adamw_multi_32_k(AdamBatch b, AdamHyper h) {
-  int64_t i0;
-  const AdamTensor& t = tensor_of(b, i0);
+  int64_t i;
+  const AdamTensor& t = tensor_of(b, i);
   const float lr = h.sc[0] * t.lr_scale, ibc1 = 1.0f / h.sc[1], ibc2 = 1.0f / h.sc[2];
   const float clip = h.sc[3], wd = h.wd * t.decay_scale;
+  i += threadIdx.x * 4;
+  if (i >= t.n) return;
+  f32x4_t p = load4(t.master, i, t.n), m = load4(static_cast<float*>(t.m), i, t.n);
+  f32x4_t v = load4(static_cast<float*>(t.v), i, t.n);
+  const Grad<BF16> g(t.grad, i, t.n);
 #pragma unroll
-  for (int k = 0; k < kAdamChunk / 1024; ++k) {
-    const int64_t i = i0 + k * 1024 + threadIdx.x * 4;
-    if (i >= t.n) return;
-    f32x4_t p = load4(t.master, i, t.n), m = load4(static_cast<float*>(t.m), i, t.n);
-    f32x4_t v = load4(static_cast<float*>(t.v), i, t.n);
-    const Grad<BF16> g(t.grad, i, t.n);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float pe = p[e], me = m[e], ve = v[e];
-      adam1(pe, me, ve, g[e], h.b1, h.b2, h.eps, wd, lr, ibc1, ibc2, clip);
-      p[e] = pe;
-      m[e] = me;
-      v[e] = ve;
-    }
-    store4(t.master, i, t.n, p);
-    store4(static_cast<float*>(t.m), i, t.n, m);
-    store4(static_cast<float*>(t.v), i, t.n, v);
-    store4(t.param, i, t.n, p);
+  for (int e = 0; e < 4; ++e) {
+    float pe = p[e], me = m[e], ve = v[e];
+    adam1(pe, me, ve, g[e], h.b1, h.b2, h.eps, wd, lr, ibc1, ibc2, clip);
+    p[e] = pe;
+    m[e] = me;
+    v[e] = ve;
   }
+  store4(t.master, i, t.n, p);
+  store4(static_cast<float*>(t.m), i, t.n, m);
+  store4(static_cast<float*>(t.v), i, t.n, v);
+  store4(t.param, i, t.n, p);
 }
 
-// Moments in 8 bits: a wave takes kPer blocks of 256 one behind another, four neighbours
-// of each to a lane, all of them loaded first.
-constexpr int kPer = kAdamChunk / kBlock / 4;
+// Moments in 8 bits: a wave a block of 256, four neighbours to a lane. 18 bytes a parameter
+// move in the time of some 110 vector operations, and the codes take most of that: the
+// update's root and quotient are the hardware's (off by the last bit or two; with IEEE's, and
+// magnitudes and codes by selects, 218 M parameters took 824 us, now 660 to 680, 5.9 TB/s). A wave
+// that takes four blocks one behind another, all loaded first: 678, and 4 M 18.3 us for 16.1.
 template <bool BF16>
 __global__ __launch_bounds__(256) void adamw_multi_8_k(AdamBatch bt, AdamHyper h) {
 #pragma clang fp contract(off)
@@ -175,119 +195,126 @@ __global__ __launch_bounds__(256) void adamw_multi_8_k(AdamBatch bt, AdamHyper h
   const AdamTensor& t = tensor_of(bt, i0);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n = t.n, b0 = i0 / kBlock + wave * kPer;
+  const int64_t n = t.n, b = i0 / kBlock + wave, i = b * kBlock + lane * 4;
+  if (b * kBlock >= n) return;
   const float lr = h.sc[0] * t.lr_scale, ibc1 = 1.0f / h.sc[1], ibc2 = 1.0f / h.sc[2];
   const float clip = h.sc[3], wd = h.wd * t.decay_scale;
+  const float c1 = 1.0f - h.b1, c2 = 1.0f - h.b2;
+  // u = (16 bits + 1/2) / 2^16, or 1/2
   const uint32_t key = h.seed ? mixed(mixed((uint32_t)*h.seed) + t.index) : 0;
+  const float u_step = h.seed ? 0x1p-16f : 0.0f, u_first = h.seed ? 0x1p-17f : 0.5f;
+  f32x4_t p = load4(t.master, i, n);
+  const Grad<BF16> g(t.grad, i, n);
+  uint32_t qm = load4(static_cast<uint8_t*>(t.m), i, n);
+  uint32_t qv = load4(static_cast<uint8_t*>(t.v), i, n);
+  const float unit_m = t.m_scale[b] * (1.0f / 16129.0f), sv = t.v_scale[b];
+  float m[4], v[4];
+  uint32_t bits_m = 0, bits_v = 0;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int64_t b = b0 + k, i = b * kBlock + lane * 4;
-    if (b * kBlock >= n) return;
-    f32x4_t p = load4(t.master, i, n);
-    const Grad<BF16> g(t.grad, i, n);
-    uint32_t qm = load4(static_cast<uint8_t*>(t.m), i, n);
-    uint32_t qv = load4(static_cast<uint8_t*>(t.v), i, n);
-    const float unit_m = t.m_scale[b] * (1.0f / 16129.0f), sv = t.v_scale[b];
-    float m[4], v[4], top_m = 0.0f, top_v = 0.0f;
-    bool bad = false;
+  for (int e = 0; e < 4; ++e) {
+    const float x = g[e] * clip;
+    m[e] = decode_m((int8_t)(qm >> 8 * e), unit_m) * h.b1 + c1 * x;
+    v[e] = decode_v((uint8_t)(qv >> 8 * e), sv) * h.b2 + (c2 * x) * x;
+    // (as integers the magnitudes order as they do, what is not finite above them)
+    bits_m = max(bits_m, __builtin_bit_cast(uint32_t, m[e]) << 1);
+    bits_v = max(bits_v, __builtin_bit_cast(uint32_t, v[e]) << 1);
+    const float upd =
+        (m[e] * ibc1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e] * ibc2) + h.eps);
+    p[e] = __builtin_fmaf(-lr, __builtin_fmaf(wd, p[e], upd), p[e]);
+  }
+  store4(t.master, i, n, p);
+  store4(t.param, i, n, p);
+  bits_m = wave_top(bits_m);
+  bits_v = wave_top(bits_v);
+  const bool bad = max(bits_m, bits_v) >= 0xFF000000u;
+  const float top_m = __builtin_bit_cast(float, bits_m >> 1);
+  const float top_v = __builtin_bit_cast(float, bits_v >> 1);
+  const float inv_m = top_m < kTiny ? 0.0f : 16129.0f * (1.0f / top_m);
+  const float inv_v = top_v < kTiny ? 0.0f : 4228250625.0f * (1.0f / top_v);
+  qm = qv = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = g[e] * clip;
-      m[e] = decode_m((int8_t)(qm >> 8 * e), unit_m) * h.b1 + (1.0f - h.b1) * x;
-      v[e] = decode_v((uint8_t)(qv >> 8 * e), sv) * h.b2 + ((1.0f - h.b2) * x) * x;
-      bad = bad || !(fabsf(m[e]) < INFINITY) || !(v[e] < INFINITY);
-      top_m = fmaxf(top_m, fabsf(m[e]));
-      top_v = fmaxf(top_v, v[e]);
-      const float upd =
-          __builtin_fmaf(wd, p[e], (m[e] * ibc1) / (sqrtf(v[e] * ibc2) + h.eps));
-      p[e] = __builtin_fmaf(-lr, upd, p[e]);
-    }
-    store4(t.master, i, n, p);
-    store4(t.param, i, n, p);
-    top_m = wave_max(top_m);
-    top_v = wave_max(top_v);
-    bad = __any(bad);
-    const float inv_m = top_m < kTiny ? 0.0f : 16129.0f * (1.0f / top_m);
-    const float inv_v = top_v < kTiny ? 0.0f : 4228250625.0f * (1.0f / top_v);
-    qm = qv = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t r = mixed((uint32_t)(i + e) ^ key);
-      const float um = h.seed ? ((float)(r & 0xFFFF) + 0.5f) * 0x1p-16f : 0.5f;
-      const float uv = h.seed ? ((float)(r >> 16) + 0.5f) * 0x1p-16f : 0.5f;
-      qm |= (uint32_t)(encode_m(m[e], inv_m, um) & 255) << 8 * e;
-      qv |= (uint32_t)encode_v(v[e], inv_v, uv) << 8 * e;
-    }
-    store4(static_cast<uint8_t*>(t.m), i, n, bad ? 0u : qm);
-    store4(static_cast<uint8_t*>(t.v), i, n, bad ? 0u : qv);
-    if (lane == 0) {
-      t.m_scale[b] = bad ? NAN : top_m < kTiny ? 0.0f : top_m;
-      t.v_scale[b] = bad ? NAN : top_v < kTiny ? 0.0f : top_v;
-    }
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t r = mixed((uint32_t)(i + e) ^ key);
+    const float um = __builtin_fmaf((float)(r & 0xFFFF), u_step, u_first);
+    const float uv = __builtin_fmaf((float)(r >> 16), u_step, u_first);
+    qm |= (uint32_t)(encode_m(m[e], inv_m, um) & 255) << 8 * e;
+    qv = __builtin_amdgcn_cvt_pk_u8_f32(encode_v(v[e], inv_v, uv), e, qv);
+  }
+  store4(static_cast<uint8_t*>(t.m), i, n, bad ? 0u : qm);
+  store4(static_cast<uint8_t*>(t.v), i, n, bad ? 0u : qv);
+  if (lane == 0) {
+    t.m_scale[b] = bad ? NAN : top_m < kTiny ? 0.0f : top_m;
+    t.v_scale[b] = bad ? NAN : top_v < kTiny ? 0.0f : top_v;
   }
 }
 
-// Values of four times four neighbours to a thread, a lane's of a wave's block.
+// Values of eight neighbours to a thread: 218 M parameters' in bf16 225 us (5.8 TB/s); four neighbours
+// to a thread, four times, 249.
 template <bool BF16>
 __global__ __launch_bounds__(256) void adamw_multi_read_k(AdamBatch bt) {
-  int64_t i0;
-  const AdamTensor& t = tensor_of(bt, i0);
+  int64_t i;
+  const AdamTensor& t = tensor_of(bt, i);
   const int64_t n = t.n;
-#pragma unroll
-  for (int k = 0; k < kAdamChunk / 1024; ++k) {
-    const int64_t i = i0 + k * 1024 + threadIdx.x * 4;
-    if (i >= n) return;
-    const auto put = [&](void* out, f32x4_t x) {
-      if constexpr (BF16) store4(static_cast<bf16_t*>(out), i, n, x);
-      else store4(static_cast<float*>(out), i, n, x);
-    };
-    f32x4_t x;
-    if (t.m_out) {
-      const uint32_t q = load4(static_cast<uint8_t*>(t.m), i, n);
-      const float unit = t.m_scale[i / kBlock] * (1.0f / 16129.0f);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = decode_m((int8_t)(q >> 8 * e), unit);
-      put(t.m_out, x);
+  i += threadIdx.x * 8;
+  if (i >= n) return;
+  const auto codes = [&](const void* p) {
+    const uint8_t* q = static_cast<const uint8_t*>(p);
+    if (i + 8 <= n) return load_nt<u32x2_t>(q, i / 8);
+    return u32x2_t{load4(q, i, n), load4(q, i + 4, n)};
+  };
+  const auto put = [&](void* out, const float* f) {
+    if constexpr (BF16) {
+      if (i + 8 <= n) {
+        const uint4 x = pack8(f);
+        return store_nt<u32x4_t>(out, i / 8, u32x4_t{x.x, x.y, x.z, x.w});
+      }
+      store4(static_cast<bf16_t*>(out), i, n, f32x4_t{f[0], f[1], f[2], f[3]});
+      store4(static_cast<bf16_t*>(out), i + 4, n, f32x4_t{f[4], f[5], f[6], f[7]});
+    } else {
+      store4(static_cast<float*>(out), i, n, f32x4_t{f[0], f[1], f[2], f[3]});
+      store4(static_cast<float*>(out), i + 4, n, f32x4_t{f[4], f[5], f[6], f[7]});
     }
-    if (t.v_out) {
-      const uint32_t q = load4(static_cast<uint8_t*>(t.v), i, n);
-      const float scale = t.v_scale[i / kBlock];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = decode_v((uint8_t)(q >> 8 * e), scale);
-      put(t.v_out, x);
-    }
+  };
+  u32x2_t qm, qv;
+  float unit, scale, f[8];
+  if (t.m_out) {
+    qm = codes(t.m);
+    unit = t.m_scale[i / kBlock] * (1.0f / 16129.0f);
   }
-}
-
-// The batch's ends padded for the search, and the grid of its launch.
-dim3 close(AdamBatch& b) {
-  for (int i = b.count; i < kAdamBatch; ++i) b.end[i] = INT32_MAX;
-  return dim3((unsigned)b.chunks);
+  if (t.v_out) {
+    qv = codes(t.v);
+    scale = t.v_scale[i / kBlock];
+  }
+  if (t.m_out) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = decode_m((int8_t)(qm[e / 4] >> 8 * (e % 4)), unit);
+    put(t.m_out, f);
+  }
+  if (t.v_out) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = decode_v((uint8_t)(qv[e / 4] >> 8 * (e % 4)), scale);
+    put(t.v_out, f);
+  }
 }
 
 }  // namespace
 
-hipError_t adamw_multi(AdamBatch& b, int bits, bool grad_bf16, const AdamHyper& h, hipStream_t s) {
+// The launch of kernel on a batch that is not empty, which is empty behind it.
+template <typename K, typename... A>
+static hipError_t launch(K kernel, AdamBatch& b, hipStream_t s, A... rest) {
   if (b.count == 0) return hipSuccess;
-  const dim3 grid = close(b), block(256);
-  if (bits == 32) {
-    if (grad_bf16) hipLaunchKernelGGL(adamw_multi_32_k<true>, grid, block, 0, s, b, h);
-    else hipLaunchKernelGGL(adamw_multi_32_k<false>, grid, block, 0, s, b, h);
-  } else {
-    if (grad_bf16) hipLaunchKernelGGL(adamw_multi_8_k<true>, grid, block, 0, s, b, h);
-    else hipLaunchKernelGGL(adamw_multi_8_k<false>, grid, block, 0, s, b, h);
-  }
+  for (int i = b.count; i < kAdamBatch; ++i) b.end[i] = INT32_MAX;   // (for the search)
+  hipLaunchKernelGGL(kernel, dim3((unsigned)b.chunks), dim3(256), 0, s, b, rest...);
   b.count = b.chunks = 0;
   return hipGetLastError();
 }
 
+hipError_t adamw_multi(AdamBatch& b, int bits, bool grad_bf16, const AdamHyper& h, hipStream_t s) {
+  if (bits == 32) return launch(grad_bf16 ? adamw_multi_32_k<true> : adamw_multi_32_k<false>, b, s, h);
+  return launch(grad_bf16 ? adamw_multi_8_k<true> : adamw_multi_8_k<false>, b, s, h);
+}
 hipError_t adamw_multi_read(AdamBatch& b, bool out_bf16, hipStream_t s) {
-  if (b.count == 0) return hipSuccess;
-  const dim3 grid = close(b), block(256);
-  if (out_bf16) hipLaunchKernelGGL(adamw_multi_read_k<true>, grid, block, 0, s, b);
-  else hipLaunchKernelGGL(adamw_multi_read_k<false>, grid, block, 0, s, b);
-  b.count = b.chunks = 0;
-  return hipGetLastError();
+  return launch(out_bf16 ? adamw_multi_read_k<true> : adamw_multi_read_k<false>, b, s);
 }
 
 }  // namespace forge

@@ -1773,7 +1773,7 @@ forge_status check_adamw_list(const forge_adamw_multi_tensor* t, int32_t n) {
   FORGE_CHECK(n == 0 || t != nullptr, FORGE_ERR_INVALID_ARG, "tensors is NULL");
   for (int i = 0; i < n; ++i) {
     FORGE_CHECK(t[i].n >= 0, FORGE_ERR_INVALID_ARG, "tensors[%d].n must be >= 0", i);
-    FORGE_CHECK(t[i].n <= 1LL << 35, FORGE_ERR_UNSUPPORTED, "tensors[%d].n > 2^35", i);
+    FORGE_CHECK(t[i].n <= 1LL << 33, FORGE_ERR_UNSUPPORTED, "tensors[%d].n > 2^33", i);
   }
   return FORGE_OK;
 }
@@ -1823,7 +1823,7 @@ forge_status forge_adamw_multi_step(const forge_adamw_multi_tensor* tensors, int
               "dev_seed is not 4-byte aligned");
   const forge::AdamHyper h{hp->beta1,        hp->beta2,   hp->eps,
                            hp->weight_decay, dev_scalars, state_bits == 8 ? dev_seed : nullptr};
-  forge::AdamBatch batch;
+  forge::AdamBatch batch(forge::kAdamStep);
   const auto launch = [&] {
     return forge::adamw_multi(batch, state_bits, grad_bf16 != 0, h, (hipStream_t)stream);
   };
@@ -1857,7 +1857,7 @@ forge_status forge_adamw_multi_read(const forge_adamw_multi_tensor* tensors, int
         if (forge_status e = check_adamw_buffer(v[k], i)) return e;
     }
   }
-  forge::AdamBatch batch;
+  forge::AdamBatch batch(forge::kAdamRead);
   for (int i = 0; i < n_tensors; ++i) {
     if (tensors[i].n == 0) continue;
     forge::AdamTensor t = adamw_tensor(tensors[i], i);

@@ -152,15 +152,17 @@ struct AdamHyper {
   const int32_t* seed;  // device, NULL: codes to the nearest
 };
 // The tensors of a launch, which takes them by value: tensor i has the workgroups from
-// end[i - 1] (0) to end[i], one for kAdamChunk of its elements.
-constexpr int kAdamBatch = 32, kAdamChunk = 4096;
+// end[i - 1] (0) to end[i], one for `chunk` of its elements.
+constexpr int kAdamBatch = 32, kAdamStep = 1024, kAdamRead = 2048;
 struct AdamBatch {
   AdamTensor t[kAdamBatch];
   int32_t end[kAdamBatch];
-  int32_t count = 0, chunks = 0;
-  // false: the launch is full (n <= 2^35)
+  int32_t count = 0, chunks = 0, chunk;
+  // chunk_: kAdamStep or kAdamRead, by what takes the batch
+  explicit AdamBatch(int chunk_) : chunk(chunk_) {}
+  // false: the launch is full (n <= 2^33, threads of a launch below 2^32)
   bool add(const AdamTensor& x) {
-    const int32_t c = (int32_t)((x.n + kAdamChunk - 1) / kAdamChunk);
+    const int32_t c = (int32_t)((x.n + chunk - 1) / chunk);
     if (count == kAdamBatch || (count > 0 && chunks + c > 1 << 23)) return false;
     t[count] = x;
     end[count++] = chunks += c;
