@@ -202,8 +202,8 @@ struct WindowTiles {
 // per sequence: a block takes a tile from the plan's list, whose sequence's rows start
 // anywhere and end at its length, cut off by the buffers' sizes as a batch row's are, so
 // that tiles of two sequences never share a row and nothing is read past a sequence.
-// Entry i of the list of 64 << KIND rows; len 0 where there is none, or where the plan is
-// one of other sizes.
+// Entry i of the list of ROWS rows; len 0 where there is none, or where the plan is
+// one of other sizes (or what stands there is no plan).
 __device__ __forceinline__ long first_row_of(const AttnPackedArgs&, const PackedTile& t, int, int) {
   return t.start;
 }
@@ -219,12 +219,15 @@ template <typename Args>
 __device__ __forceinline__ long stat_row(const Args& a, int b, int n, int S, long) {
   return ((long)b * a.n_heads + n) * S;
 }
-template <int KIND>
+template <int ROWS>
 __device__ __forceinline__ PackedTile packed_tile(const AttnPackedArgs& a, int i) {
+  constexpr int KIND = ROWS == 32 ? 0 : ROWS == 64 ? 1 : ROWS == 128 ? 2 : 3;
+  static_assert(32 << KIND == ROWS);
   const PackedHeader h = *a.plan;
   PackedTile t = a.tiles[KIND][i];
   if (i >= h.count[KIND] || h.tokens != a.seq || h.n_seqs != a.n_seqs ||
-      h.max_seq != a.max_seq || h.window != a.window)
+      h.max_seq != a.max_seq || h.window != a.window || t.start < 0 || t.len < 0 || t.tile < 0 ||
+      t.len > a.seq - t.start || t.tile > (t.len - 1) / ROWS)
     t.len = 0;
   return t;
 }
@@ -363,7 +366,7 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
   int qt = nqt - 1 - level, n = L % a.n_heads, b = L / a.n_heads;
   std::conditional_t<PACKED, PackedTile, int> pt{};
   if constexpr (PACKED) {
-    const PackedTile t = packed_tile<NW == 2 ? 0 : 1>(a, level);
+    const PackedTile t = packed_tile<BQ>(a, level);
     if (t.len == 0) return;
     n = L;
     b = 0;
@@ -912,7 +915,7 @@ struct KvPackedBlock {
   PackedTile t;
   __device__ __forceinline__ KvPackedBlock(const AttnPackedArgs& a, int splits) {
     const int r = (int)blockIdx.x % (a.n_kv_heads * splits);
-    t = packed_tile<0>(a, (int)blockIdx.x / (a.n_kv_heads * splits));
+    t = packed_tile<64>(a, (int)blockIdx.x / (a.n_kv_heads * splits));
     m = r % a.n_kv_heads;
     b = 0;
     z = r / a.n_kv_heads;
@@ -1678,7 +1681,7 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
   std::conditional_t<PACKED, PackedTile, int> pt{};
   if constexpr (PACKED) {
     // (list entries in turn, the heads of each as in the causal order)
-    pt = packed_tile<WAVES == 2 ? 0 : WAVES == 4 ? 1 : 2>(a, id / a.n_heads);
+    pt = packed_tile<BQ>(a, id / a.n_heads);
     if (pt.len == 0) return;
     n = m * grp + id / a.n_kv_heads % grp;
     b = 0;
@@ -2197,7 +2200,7 @@ namespace {
 __global__ __launch_bounds__(256) void attn_packed_sum_k(AttnPackedArgs a, int splits,
                                                          bf16_t* __restrict__ dk,
                                                          bf16_t* __restrict__ dv, long ld_d) {
-  const PackedTile t = packed_tile<0>(a, (int)blockIdx.x);
+  const PackedTile t = packed_tile<64>(a, (int)blockIdx.x);
   const int width = a.n_kv_heads * a.d, cpr = width / 8;
   const int i = (int)blockIdx.z * 256 + (int)threadIdx.x;
   const int r = t.tile * 64 + i / cpr, c = i % cpr * 8;
@@ -2219,14 +2222,14 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   const dim3 pgrid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
   hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
                      a.seq);
-  const dim3 kgrid((unsigned)(p.cap[0] * a.n_kv_heads * splits));
+  const dim3 kgrid((unsigned)(p.cap[1] * a.n_kv_heads * splits));
   hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, false, false>), kgrid, block, 0, s, a, dout,
                      delta, ds, dv, dk, ld_d, a.pv, a.pk, splits);
   if (splits > 1) {
-    const dim3 grid((unsigned)p.cap[0], 2, (unsigned)((8 * a.n_kv_heads * D + 255) / 256));
+    const dim3 grid((unsigned)p.cap[1], 2, (unsigned)((8 * a.n_kv_heads * D + 255) / 256));
     hipLaunchKernelGGL(attn_packed_sum_k, grid, block, 0, s, a, splits, dk, dv, ld_d);
   }
-  const dim3 grid((unsigned)(p.cap[2] * a.n_heads));
+  const dim3 grid((unsigned)(p.cap[3] * a.n_heads));
   hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, 8, 1>), grid, dim3(512), 0, s, a, ds, dq,
                      ld_d);
   return hipGetLastError();
@@ -2235,7 +2238,7 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
 
 hipError_t attn_packed_fwd(const AttnPackedArgs& a, const PackedPlan& p, uint16_t* o, float* lse,
                            hipStream_t s) {
-  const dim3 grid((unsigned)(p.cap[1] * a.n_heads)), block(256);
+  const dim3 grid((unsigned)(p.cap[2] * a.n_heads)), block(256);
   if (a.d == 128)
     hipLaunchKernelGGL((attn_fwd_k<128, AttnPackedArgs, 4, 1>), grid, block, 0, s, a, o, lse);
   else

@@ -1,5 +1,9 @@
 // The plan of a packed batch (PackedPlan, kernels.h): which tiles its sequences have,
-// built on the device from their offsets.
+// built on the device from their offsets. Tiles with the most keys come first, so that no
+// long block starts when the others have ended: sorted by the tile's place in its sequence.
+// With the sequences in order of their tiles, the ones that have a tile j are the first
+// count[j] of them, so the list needs no sort of its own: tile j of the r-th sequence is
+// entry (those of all later tiles) + r.
 #include "common.h"
 #include "kernels.h"
 
@@ -7,6 +11,7 @@ namespace forge {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kLdsBins = 4096;   // tiles of a sequence whose counts fit LDS
 
 // Inclusive sum (or maximum) over the workgroup's threads; every thread gets the total too.
 template <bool MAX>
@@ -23,6 +28,7 @@ __device__ __forceinline__ int scan(int x, int* lds, int& total) {
   __syncthreads();
   int before = MAX ? INT32_MIN : 0;
   total = before;
+#pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     const int y = lds[w];
     if (w < wave) before = join(before, y);
@@ -31,50 +37,119 @@ __device__ __forceinline__ int scan(int x, int* lds, int& total) {
   return join(before, x);
 }
 
-// One workgroup, a thread to a sequence, kThreads of them at a time.
+// The sequences, kThreads at a time, a thread to each.
+struct Sequences {
+  const PackedPlan& p;
+  const int32_t* offsets;
+  int* lds;
+  int end = 0, base = 0;   // of those before
+  __device__ __forceinline__ int offset(int i) const {
+    return min(max(offsets[min(i, p.n_seqs)], 0), p.tokens);
+  }
+  // sequence s0 + thread: its rows and its first block of dS
+  __device__ __forceinline__ PackedTile next(int s0) {
+    const int s = s0 + (int)threadIdx.x;
+    // the offsets' running maximum; a sequence starts where that before it ends
+    if (s0 == 0) end = offset(0);
+    const int last = end;
+    const int e = scan<true>(max(offset(s + 1), last), lds, end);
+    int start = __shfl_up(e, 1, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = e;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) start = threadIdx.x ? lds[(threadIdx.x >> 6) - 1] : last;
+    const int len = s < p.n_seqs ? min(e - start, p.max_seq) : 0;
+    const int blocks = len > 0 ? (int)DsPacked(len, p.window, 0, 0).blocks() : 0;
+    int total;
+    const int b = base + scan<false>(blocks, lds, total) - blocks;
+    base += total;
+    return PackedTile{start, len, 0, b};
+  }
+};
+
+// One workgroup for each kind of tile.
+template <bool LDS>
 __global__ __launch_bounds__(kThreads) void packed_plan_k(PackedPlan p,
                                                           const int32_t* __restrict__ offsets,
                                                           char* plan) {
   __shared__ int lds[kWaves];
-  int first = 0, base = 0, done[3] = {0, 0, 0};
-  for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
-    const int s = s0 + (int)threadIdx.x;
-    const auto offset = [&](int i) { return min(max(offsets[min(i, p.n_seqs)], 0), p.tokens); };
-    // running maximum of the offsets, the sequence's end among them
-    int total;
-    const int end = scan<true>(max(offset(s + 1), max(s0 == 0 ? offset(0) : 0, first)), lds, total);
-    int start = __shfl_up(end, 1, 64);
-    __shared__ int edge[kWaves];
-    if ((threadIdx.x & 63) == 63) edge[threadIdx.x >> 6] = end;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0)
-      start = threadIdx.x ? edge[(threadIdx.x >> 6) - 1] : max(s0 == 0 ? offset(0) : 0, first);
-    first = total;
-    const int len = s < p.n_seqs ? min(end - start, p.max_seq) : 0;
-    const int blocks = len > 0 ? (int)DsPacked(len, p.window, 0, 0).blocks() : 0;
-    const int my_base = base + scan<false>(blocks, lds, total) - blocks;
-    base += total;
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      const int nt = (len + (64 << k) - 1) >> (6 + k);
-      const int at = done[k] + scan<false>(nt, lds, total) - nt;
-      done[k] += total;
-      PackedTile* list = reinterpret_cast<PackedTile*>(plan + p.tiles[k]);
-      for (int t = 0; t < nt && at + t < p.cap[k]; ++t)
-        list[at + t] = PackedTile{start, len, t, my_base};
+  __shared__ int bins[LDS ? 2 * (kLdsBins + 1) : 1];
+  const int kind = (int)blockIdx.x, shift = 5 + kind, rows = 1 << shift;
+  const int nt = (p.max_seq + rows - 1) >> shift;   // tiles of a sequence, at most
+  // count[j]: sequences with more than j tiles (first, of exactly j); first[j]: entries of
+  // the tiles behind j
+  int* count = LDS ? bins : reinterpret_cast<int*>(plan + p.bins[kind]);
+  int* first = count + nt + 1;
+  PackedTile* order = reinterpret_cast<PackedTile*>(plan + p.order[kind]);
+  PackedTile* list = reinterpret_cast<PackedTile*>(plan + p.tiles[kind]);
+  for (int j = (int)threadIdx.x; j <= nt; j += kThreads) count[j] = 0;
+  __syncthreads();
+  PackedTile mine{};
+  {
+    Sequences seqs{p, offsets, lds};
+    for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
+      mine = seqs.next(s0);
+      if (mine.len > 0) atomicAdd(&count[(mine.len + rows - 1) >> shift], 1);
     }
+  }
+  __syncthreads();
+  // from the longest sequences down: those with more than j tiles, and their tiles
+  int more = 0, entries = 0;
+  for (int j0 = 0; j0 <= nt; j0 += kThreads) {
+    const int j = nt - j0 - (int)threadIdx.x;
+    const int exactly = j >= 0 ? count[j] : 0;
+    int total;
+    const int upto = more + scan<false>(exactly, lds, total);
+    more += total;
+    const int c = j >= 0 ? upto - exactly : 0;         // with more than j
+    const int behind = entries + scan<false>(c, lds, total) - c;
+    entries += total;
+    if (j >= 0) {
+      count[j] = c;
+      first[j] = behind;
+    }
+  }
+  __syncthreads();
+  // the sequences by their tiles: one of exactly nt stands behind the count[nt] of more
+  // (which of equals comes first decides nothing but the blocks' order)
+  {
+    Sequences seqs{p, offsets, lds};
+    for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
+      if (p.n_seqs > kThreads) mine = seqs.next(s0);
+      const int n = (mine.len + rows - 1) >> shift;
+      if (mine.len > 0) order[atomicAdd(&count[n], 1)] = mine;
+    }
+  }
+  __syncthreads();
+  // (count[n] is now what count[n - 1] was: sequences with n tiles and more)
+  const int total = min(entries, p.cap[kind]);
+  for (int e = (int)threadIdx.x; e < total; e += kThreads) {
+    int lo = 0, hi = nt - 1;                           // the first j with first[j] <= e
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (first[mid] <= e) hi = mid;
+      else lo = mid + 1;
+    }
+    PackedTile t = order[e - first[lo]];
+    t.tile = lo;
+    list[e] = t;
   }
   if (threadIdx.x == 0) {
     PackedHeader* h = reinterpret_cast<PackedHeader*>(plan);
-    *h = PackedHeader{p.tokens, p.n_seqs, p.max_seq, p.window, {}, 0};
-    for (int k = 0; k < 3; ++k) h->count[k] = min(done[k], p.cap[k]);
+    h->count[kind] = total;
+    if (kind == 0) {
+      h->tokens = p.tokens;
+      h->n_seqs = p.n_seqs;
+      h->max_seq = p.max_seq;
+      h->window = p.window;
+    }
   }
 }
 
 __global__ __launch_bounds__(64) void packed_positions_k(PackedPlan p, const char* plan,
                                                          int32_t* __restrict__ pos) {
-  if ((int)blockIdx.x >= reinterpret_cast<const PackedHeader*>(plan)->count[0]) return;
-  const PackedTile t = reinterpret_cast<const PackedTile*>(plan + p.tiles[0])[blockIdx.x];
+  if ((int)blockIdx.x >= reinterpret_cast<const PackedHeader*>(plan)->count[1]) return;
+  const PackedTile t = reinterpret_cast<const PackedTile*>(plan + p.tiles[1])[blockIdx.x];
   const int r = t.tile * 64 + (int)threadIdx.x;
   if (r < t.len) pos[t.start + r] = r;
 }
@@ -84,27 +159,33 @@ __global__ __launch_bounds__(64) void packed_positions_k(PackedPlan p, const cha
 PackedPlan::PackedPlan(int tokens_, int n_seqs_, int max_seq_, int window_)
     : tokens(tokens_), n_seqs(n_seqs_), max_seq(max_seq_ < tokens_ ? max_seq_ : tokens_),
       window(window_ > 0 && window_ < tokens_ ? window_ : tokens_) {
+  const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   const long n = n_seqs < tokens ? n_seqs : tokens;   // sequences with a row
   bytes = 256;
-  for (int k = 0; k < 3; ++k) {
-    const long rows = 64L << k;
+  for (int k = 0; k < kPackedKinds; ++k) {
+    const long rows = 32L << k, nt = (max_seq + rows - 1) / rows;
     cap[k] = (int)((tokens + (rows - 1) * n) / rows);
     tiles[k] = bytes;
-    bytes += ((size_t)cap[k] * sizeof(PackedTile) + 255) / 256 * 256;
+    order[k] = tiles[k] + up((size_t)cap[k] * sizeof(PackedTile));
+    bins[k] = order[k] + up((size_t)n * sizeof(PackedTile));
+    bytes = bins[k] + up((size_t)(nt + 1) * 8);
   }
   // a tile has on average no more blocks than one of a sequence of max_seq, whose later
   // tiles the end cuts least
   const long nt = (max_seq + 63) / 64;
   const long full = DsPacked((int)(nt * 64), window, 0, 0).blocks();
-  ds_blocks = cap[0] * ((full + nt - 1) / nt);
+  ds_blocks = cap[1] * ((full + nt - 1) / nt);
 }
 
 hipError_t attn_packed_plan(const PackedPlan& p, const int32_t* offsets, void* plan, int32_t* pos,
                             hipStream_t s) {
-  hipLaunchKernelGGL(packed_plan_k, dim3(1), dim3(kThreads), 0, s, p, offsets,
-                     static_cast<char*>(plan));
+  char* out = static_cast<char*>(plan);
+  const dim3 grid(kPackedKinds), block(kThreads);
+  if (p.max_seq <= 32 * (kLdsBins - 1))
+    hipLaunchKernelGGL(packed_plan_k<true>, grid, block, 0, s, p, offsets, out);
+  else hipLaunchKernelGGL(packed_plan_k<false>, grid, block, 0, s, p, offsets, out);
   if (pos)
-    hipLaunchKernelGGL(packed_positions_k, dim3((unsigned)p.cap[0]), dim3(64), 0, s, p,
+    hipLaunchKernelGGL(packed_positions_k, dim3((unsigned)p.cap[1]), dim3(64), 0, s, p,
                        static_cast<const char*>(plan), pos);
   return hipGetLastError();
 }

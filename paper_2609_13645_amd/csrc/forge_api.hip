@@ -2243,7 +2243,7 @@ struct PackedArgs : forge::AttnPackedArgs {
     static_cast<forge::AttnArgs&>(*this) = attn_args(attn_dims(a), qkv);
     window = p.window;
     plan = static_cast<const forge::PackedHeader*>(plan_);
-    for (int k = 0; k < 3; ++k)
+    for (int k = 0; k < forge::kPackedKinds; ++k)
       tiles[k] = reinterpret_cast<const forge::PackedTile*>(static_cast<const char*>(plan_) +
                                                             p.tiles[k]);
     n_seqs = p.n_seqs;

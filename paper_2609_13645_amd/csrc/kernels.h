@@ -290,18 +290,19 @@ struct DsPacked : DsWindow {
   __host__ __device__ long block(int kt, int j) const { return tile(kt) + 2048L * (j - 2 * kt); }
 };
 // The plan of a packed batch: a header (for which sizes it was made; how many tiles of
-// 64, 128 and 256 rows there are), a list of each kind of tile, and what the builder
-// keeps of every sequence. All of it from the host's bounds alone: each list has room for
-// what the sequences can come to.
+// each kind there are), a list of each kind of tile, and what the builder keeps of the
+// sequences. All of it from the host's bounds alone: each list has room for what the
+// sequences can come to.
+constexpr int kPackedKinds = 4;   // tiles of 32, 64, 128 and 256 rows
 struct PackedHeader {
   int32_t tokens, n_seqs, max_seq, window;
-  int32_t count[3];
-  int32_t pad;
+  int32_t count[kPackedKinds];
 };
 struct PackedPlan {
   int tokens, n_seqs, max_seq, window;   // max_seq and window cut to tokens
-  int cap[3];                            // entries of each list, 64 << i rows
-  size_t tiles[3], bytes;                // where the lists lie
+  int cap[kPackedKinds];                 // entries of each list
+  // bytes: where the lists lie, the sequences by their tiles, and how many have them
+  size_t tiles[kPackedKinds], order[kPackedKinds], bins[kPackedKinds], bytes;
   long ds_blocks;                        // blocks of dS of a head, at most
   __host__ PackedPlan(int tokens_, int n_seqs_, int max_seq_, int window_);
 };
@@ -309,7 +310,7 @@ struct PackedPlan {
 struct AttnPackedArgs : AttnArgs {
   int window;
   const PackedHeader* plan;
-  const PackedTile* tiles[3];
+  const PackedTile* tiles[kPackedKinds];
   int n_seqs, max_seq;
   long ds_head;                          // elements of a head's dS
   float *pk = nullptr, *pv = nullptr;    // the kv pass' partial sums
