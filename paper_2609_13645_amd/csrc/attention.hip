@@ -336,11 +336,12 @@ __device__ __forceinline__ float sum_xor32(float v) {
 
 // NW waves of 32 queries; KG groups of them share the block's key tiles (group g takes
 // tiles g, g + KG, ..) and add up their softmaxes at the end.
-template <int D, typename Args, int NW, int KG>
+// HW: query heads of one kv head in a block, NW / HW waves each (PACKED; else one).
+template <int D, typename Args, int NW, int KG, int HW = 1>
 __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k(
     Args a, bf16_t* __restrict__ o, float* __restrict__ lse) {
   constexpr bool WIN = kWindow<Args>;
-  constexpr int BQ = 32 * NW, BKV = 64, NAT = BKV * D / 8, KK = D / 16, DB = D / 32;
+  constexpr int BQ = 32 * NW / HW, BKV = 64, NAT = BKV * D / 8, KK = D / 16, DB = D / 32;
   constexpr int TILE_B = NAT * 16;       // bytes of one K or V tile
   constexpr int HALF_B = TILE_B / 2;     // rows 32..63 of a tile
   constexpr int ROW16_B = 16 * D * 2;    // 16 rows of a tile
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
   // consecutive blocks go to the 8 XCDs in turn; when the level's count is
   // a multiple of 8, XCD x takes a contiguous range of heads at every level,
   // so the heads that share a kv head keep its K / V in one L2.
-  const int W = a.n_heads * a.batch;
+  const int W = a.n_heads * a.batch / HW;
   const int id = (int)blockIdx.x;
   const int level = id / W, r = id % W;
   const int L = (W % 8 == 0) ? (r % 8) * (W / 8) + r / 8 : r;
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
   if constexpr (PACKED) {
     const PackedTile t = packed_tile<BQ>(a, level);
     if (t.len == 0) return;
-    n = L;
+    n = L * HW;
     b = 0;
     qt = t.tile;
     pt = t;
@@ -386,6 +387,7 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
   const int m = n / (a.n_heads / a.n_kv_heads);
   const int E = WIN && !PACKED ? row_len(a, b) : S;   // end of the batch row's tokens
   const long rb = first_row_of(a, pt, b, S);
+  if constexpr (HW > 1) n += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW / (NW / HW);
   const bf16_t* Qg = a.q + rb * a.ld_qkv + (long)n * D;
   const bf16_t* Kg = a.k + rb * a.ld_qkv + (long)m * D;
   const bf16_t* Vg = a.v + rb * a.ld_qkv + (long)m * D;
@@ -397,7 +399,7 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
   }
   uint4* smem = smem_ + kg * 4 * NAT;
   const int hh = lane >> 5, l32 = lane & 31;
-  const int q0w = qt * BQ + wave * 32;
+  const int q0w = qt * BQ + (HW > 1 ? wave % (NW / HW) : wave) * 32;
   const int q = q0w + l32;
   bf16x8_t qf[KK];
 #pragma unroll
@@ -1659,12 +1661,13 @@ struct DqPlan {
   static constexpr int MEM = DmaPlan<D, NW>::PER + NDS / 64 / NW;   // DMA per wave per tile
 };
 
-template <int D, typename Args, int WAVES, int KG>
+// (HW as in the forward)
+template <int D, typename Args, int WAVES, int KG, int HW = 1>
 __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
     Args a, const bf16_t* __restrict__ ds, bf16_t* __restrict__ dq, long ld_d) {
   using Q = DqPlan<D, WAVES>;
   constexpr bool WIN = kWindow<Args>;
-  constexpr int BQ = Q::BQ, BKV = Q::BKV, NAT = Q::NAT, NW = Q::NW, NST = Q::NST, DB = D / 32;
+  constexpr int BQ = Q::BQ / HW, BKV = Q::BKV, NAT = Q::NAT, NW = Q::NW, NST = Q::NST, DB = D / 32;
   __shared__ uint4 sm_[KG * NST * Q::STAGE];   // (of each group of waves)
   constexpr bool PACKED = kPacked<Args>;
   int S = a.seq;
@@ -1681,9 +1684,9 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
   std::conditional_t<PACKED, PackedTile, int> pt{};
   if constexpr (PACKED) {
     // (list entries in turn, the heads of each as in the causal order)
-    pt = packed_tile<BQ>(a, id / a.n_heads);
+    pt = packed_tile<BQ>(a, id / (a.n_heads / HW));
     if (pt.len == 0) return;
-    n = m * grp + id / a.n_kv_heads % grp;
+    n = m * grp + id / a.n_kv_heads % (grp / HW) * HW;
     b = 0;
     qt = pt.tile;
     S = pt.len;
@@ -1717,7 +1720,7 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
   uint4* sm = sm_ + kg * NST * Q::STAGE;
   const int hh = lane >> 5, l32 = lane & 31;
   const int qb0 = qt * BQ;
-  const int q0w = qb0 + wave * 32;
+  const int q0w = qb0 + (HW > 1 ? wave % (NW / HW) : wave) * 32;
   const int q = q0w + l32;
   f32x16_t dqa[DB];
 #pragma unroll
@@ -1742,11 +1745,16 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
       nb = (E + 31) / 32 - 2 * kt;
       if (kt >= L.nst) nb = min(nb, L.nwin);
     }
-    const __amdgpu_buffer_rsrc_t r = rsrc_n(dsh + L.tile(kt), 4096L * nb);
+    __amdgpu_buffer_rsrc_t r = rsrc_n(dsh + L.tile(kt), 4096L * nb);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int c = t * NW + wave;
-      const int blk = jb + c / 4;
+      int blk = jb + c / 4;
+      if constexpr (HW > 1) {
+        // block c / 4 is of the head and the slab of wave c / 4
+        r = rsrc_n(dsh + c / 4 / (NW / HW) * L.head + L.tile(kt), 4096L * nb);
+        blk = jb + c / 4 % (NW / HW);
+      }
       // non-temporal (cache policy 2): dS is read once here; K stays in L2
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           r, (lds_ptr_t)(stg + NAT + c * 64), 16,
@@ -1871,6 +1879,7 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
 #pragma unroll
       for (int db = 0; db < DB; ++db) zero(dqa[db]);
     }
+    if constexpr (HW > 1) n += wave / (NW / HW);
     bf16_t* dqr = dq + (rb + q) * ld_d + (long)n * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -2210,6 +2219,16 @@ __global__ __launch_bounds__(256) void attn_packed_sum_k(AttnPackedArgs a, int s
   split_sum((v ? a.pv : a.pk) + row * width + c, splits, (long)a.seq * width,
             v ? 1.0f : a.scale, (v ? dv : dk) + row * ld_d + c);
 }
+// The plan's list of tiles of so many rows.
+constexpr int packed_kind(int rows) { return rows == 32 ? 0 : rows == 64 ? 1 : rows == 128 ? 2 : 3; }
+// f of the query heads in a block.
+template <typename F>
+void packed_heads(const AttnPackedArgs& a, F&& f) {
+  const int grp = a.n_heads / a.n_kv_heads;
+  if (grp % 4 == 0) f(std::integral_constant<int, 4>{});
+  else if (grp % 2 == 0) f(std::integral_constant<int, 2>{});
+  else f(std::integral_constant<int, 1>{});
+}
 template <int D>
 hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16_t* o,
                              const uint16_t* dout, const float* lse, float* delta, uint16_t* ds,
@@ -2229,21 +2248,30 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
     const dim3 grid((unsigned)p.cap[1], 2, (unsigned)((8 * a.n_kv_heads * D + 255) / 256));
     hipLaunchKernelGGL(attn_packed_sum_k, grid, block, 0, s, a, splits, dk, dv, ld_d);
   }
-  const dim3 grid((unsigned)(p.cap[3] * a.n_heads));
-  hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, 8, 1>), grid, dim3(512), 0, s, a, ds, dq,
-                     ld_d);
+  packed_heads(a, [&](auto heads) {
+    constexpr int HW = decltype(heads)::value;
+    const dim3 grid((unsigned)(p.cap[packed_kind(256 / HW)] * (a.n_heads / HW)));
+    hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, 8, 1, HW>), grid, dim3(512), 0, s, a, ds,
+                       dq, ld_d);
+  });
+  return hipGetLastError();
+}
+template <int D>
+hipError_t attn_packed_fwd_d(const AttnPackedArgs& a, const PackedPlan& p, uint16_t* o, float* lse,
+                             hipStream_t s) {
+  packed_heads(a, [&](auto heads) {
+    constexpr int HW = decltype(heads)::value;
+    const dim3 grid((unsigned)(p.cap[packed_kind(128 / HW)] * (a.n_heads / HW)));
+    hipLaunchKernelGGL((attn_fwd_k<D, AttnPackedArgs, 4, 1, HW>), grid, dim3(256), 0, s, a, o,
+                       lse);
+  });
   return hipGetLastError();
 }
 }  // namespace
 
 hipError_t attn_packed_fwd(const AttnPackedArgs& a, const PackedPlan& p, uint16_t* o, float* lse,
                            hipStream_t s) {
-  const dim3 grid((unsigned)(p.cap[2] * a.n_heads)), block(256);
-  if (a.d == 128)
-    hipLaunchKernelGGL((attn_fwd_k<128, AttnPackedArgs, 4, 1>), grid, block, 0, s, a, o, lse);
-  else
-    hipLaunchKernelGGL((attn_fwd_k<64, AttnPackedArgs, 4, 1>), grid, block, 0, s, a, o, lse);
-  return hipGetLastError();
+  return a.d == 128 ? attn_packed_fwd_d<128>(a, p, o, lse, s) : attn_packed_fwd_d<64>(a, p, o, lse, s);
 }
 size_t attn_packed_bwd_part_bytes(const AttnPackedArgs&, const PackedPlan&) { return 0; }
 hipError_t attn_packed_bwd(const AttnPackedArgs& a, const PackedPlan& p, const uint16_t* o,
