@@ -202,7 +202,7 @@ struct WindowTiles {
 // per sequence: a block takes a tile from the plan's list, whose sequence's rows start
 // anywhere and end at its length, cut off by the buffers' sizes as a batch row's are, so
 // that tiles of two sequences never share a row and nothing is read past a sequence.
-// Entry i of the list of ROWS rows; len 0 where there is none, or where the plan is
+// Entry i of the list of ROWS rows (KEYS: of the kv pass' order); len 0 where there is none, or where the plan is
 // one of other sizes (or what stands there is no plan).
 __device__ __forceinline__ long first_row_of(const AttnPackedArgs&, const PackedTile& t, int, int) {
   return t.start;
@@ -219,10 +219,10 @@ template <typename Args>
 __device__ __forceinline__ long stat_row(const Args& a, int b, int n, int S, long) {
   return ((long)b * a.n_heads + n) * S;
 }
-template <int ROWS>
+template <int ROWS, bool KEYS = false>
 __device__ __forceinline__ PackedTile packed_tile(const AttnPackedArgs& a, int i) {
-  constexpr int KIND = ROWS == 32 ? 0 : ROWS == 64 ? 1 : ROWS == 128 ? 2 : 3;
-  static_assert(32 << KIND == ROWS);
+  constexpr int KIND = KEYS ? 4 : ROWS == 32 ? 0 : ROWS == 64 ? 1 : ROWS == 128 ? 2 : 3;
+  static_assert(32 << (KEYS ? 1 : KIND) == ROWS);
   const PackedHeader h = *a.plan;
   PackedTile t = a.tiles[KIND][i];
   if (i >= h.count[KIND] || h.tokens != a.seq || h.n_seqs != a.n_seqs ||
@@ -338,7 +338,9 @@ __device__ __forceinline__ float sum_xor32(float v) {
 // tiles g, g + KG, ..) and add up their softmaxes at the end.
 // HW: query heads of one kv head in a block, NW / HW waves each (PACKED; else one).
 template <int D, typename Args, int NW, int KG, int HW = 1>
-__global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k(
+__global__ __launch_bounds__(64 * NW * KG, KG * D > 128                          ? 1
+                                           : kPacked<Args> && D == 64 && KG == 1 ? 3
+                                                                                 : 2) void attn_fwd_k(
     Args a, bf16_t* __restrict__ o, float* __restrict__ lse) {
   constexpr bool WIN = kWindow<Args>;
   constexpr int BQ = 32 * NW / HW, BKV = 64, NAT = BKV * D / 8, KK = D / 16, DB = D / 32;
@@ -691,6 +693,31 @@ __global__ __launch_bounds__(64 * NW * KG, KG * D > 128 ? 1 : 2) void attn_fwd_k
     }
     mrow = m_all;
   }
+  if constexpr (PACKED && KG == 1) {
+    // Rows leave through LDS, whole ones 16 bytes to a lane: short sequences write as much
+    // as they read (512 documents of 32 tokens, 32/8 heads of 128: 89 us with 8 bytes to a
+    // lane of 32 rows each, now 72, of which the bytes are 65). The K slots are free: the last
+    // tile's scores ended before the last barrier. A wave's own rows, so no barrier.
+    constexpr int CPR = D / 8;   // 16-byte pieces of a row, piece c of row r at c ^ (r % CPR)
+    uint4* mine = smem + wave * 32 * CPR;
+    const float inv = 1.0f / lrow;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        reinterpret_cast<uint2*>(mine + l32 * CPR + ((db * 4 + g) ^ (l32 % CPR)))[hh] =
+            make_uint2(pack2(oacc[db][g * 4 + 0] * inv, oacc[db][g * 4 + 1] * inv),
+                       pack2(oacc[db][g * 4 + 2] * inv, oacc[db][g * 4 + 3] * inv));
+    if (hh == 0 && q < S) lse[stat_row(a, b, n, S, rb) + q] = (mrow + log2f(lrow)) * kLn2;
+#pragma unroll
+    for (int i = 0; i < CPR / 2; ++i) {
+      const int r = i * (64 / CPR) + lane / CPR, c = lane % CPR;
+      const uint4 x = mine[r * CPR + (c ^ (r % CPR))];
+      if (q0w + r < S)
+        *reinterpret_cast<uint4*>(o + (rb + q0w + r) * orow_ld + (long)n * D + c * 8) = x;
+    }
+    return;
+  }
   if (q < S) {
     // (WIN: rows past the tokens' end get zeros and -inf)
     const bool none = WIN && q >= E;
@@ -917,7 +944,7 @@ struct KvPackedBlock {
   PackedTile t;
   __device__ __forceinline__ KvPackedBlock(const AttnPackedArgs& a, int splits) {
     const int r = (int)blockIdx.x % (a.n_kv_heads * splits);
-    t = packed_tile<64>(a, (int)blockIdx.x / (a.n_kv_heads * splits));
+    t = packed_tile<64, true>(a, (int)blockIdx.x / (a.n_kv_heads * splits));
     m = r % a.n_kv_heads;
     b = 0;
     z = r / a.n_kv_heads;

@@ -1,9 +1,14 @@
 // The plan of a packed batch (PackedPlan, kernels.h): which tiles its sequences have,
-// built on the device from their offsets. Tiles with the most keys come first, so that no
-// long block starts when the others have ended: sorted by the tile's place in its sequence.
-// With the sequences in order of their tiles, the ones that have a tile j are the first
-// count[j] of them, so the list needs no sort of its own: tile j of the r-th sequence is
-// entry (those of all later tiles) + r.
+// built on the device from their offsets, and in which order blocks take them: those with
+// the most keys first, so that no long block starts when the others have ended.
+//  * The query passes: the longest sequences first, of each the last tile first. The blocks
+//    that run at once are then of few sequences, whose keys an XCD's L2 holds.
+//  * The kv pass, whose blocks are few and long: by the tiles' places, across all sequences
+//    (4 documents of 4096 tokens, 32/8 heads of 64: backward 1267 us in the other order,
+//    so 1141).
+// With the sequences in order of their tiles neither needs a sort: in the first order those
+// of k tiles stand behind the tiles of all longer ones, k to a sequence; in the second tile j
+// of the r-th sequence stands r behind all tiles further in.
 #include "common.h"
 #include "kernels.h"
 
@@ -74,10 +79,11 @@ __global__ __launch_bounds__(kThreads) void packed_plan_k(PackedPlan p,
                                                           char* plan) {
   __shared__ int lds[kWaves];
   __shared__ int bins[LDS ? 2 * (kLdsBins + 1) : 1];
-  const int kind = (int)blockIdx.x, shift = 5 + kind, rows = 1 << shift;
+  const int kind = (int)blockIdx.x, rows = packed_rows(kind), shift = 31 - __builtin_clz(rows);
+  const bool by_place = kind == 4;
   const int nt = (p.max_seq + rows - 1) >> shift;   // tiles of a sequence, at most
-  // count[j]: sequences with more than j tiles (first, of exactly j); first[j]: entries of
-  // the tiles behind j
+  // per number of tiles k: how many sequences have exactly k, then how many have more;
+  // the entries before those of k tiles (by_place: before tile k of any sequence)
   int* count = LDS ? bins : reinterpret_cast<int*>(plan + p.bins[kind]);
   int* first = count + nt + 1;
   PackedTile* order = reinterpret_cast<PackedTile*>(plan + p.order[kind]);
@@ -93,45 +99,51 @@ __global__ __launch_bounds__(kThreads) void packed_plan_k(PackedPlan p,
     }
   }
   __syncthreads();
-  // from the longest sequences down: those with more than j tiles, and their tiles
-  int more = 0, entries = 0;
-  for (int j0 = 0; j0 <= nt; j0 += kThreads) {
-    const int j = nt - j0 - (int)threadIdx.x;
-    const int exactly = j >= 0 ? count[j] : 0;
+  // from the most tiles down: the sequences with more, and the entries before
+  int longer = 0, entries = 0;
+  for (int k0 = 0; k0 <= nt; k0 += kThreads) {
+    const int k = nt - k0 - (int)threadIdx.x;
+    const int exactly = k >= 0 ? count[k] : 0;
     int total;
-    const int upto = more + scan<false>(exactly, lds, total);
-    more += total;
-    const int c = j >= 0 ? upto - exactly : 0;         // with more than j
-    const int behind = entries + scan<false>(c, lds, total) - c;
+    const int more = longer + scan<false>(exactly, lds, total) - exactly;
+    longer += total;
+    const int tiles = k < 0 ? 0 : by_place ? more : exactly * k;
+    const int before = entries + scan<false>(tiles, lds, total) - tiles;
     entries += total;
-    if (j >= 0) {
-      count[j] = c;
-      first[j] = behind;
+    if (k >= 0) {
+      count[k] = more;
+      first[k] = before;
     }
   }
   __syncthreads();
-  // the sequences by their tiles: one of exactly nt stands behind the count[nt] of more
-  // (which of equals comes first decides nothing but the blocks' order)
+  // the sequences in that order (which of equals comes first decides nothing but the
+  // blocks' order)
   {
     Sequences seqs{p, offsets, lds};
     for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
       if (p.n_seqs > kThreads) mine = seqs.next(s0);
-      const int n = (mine.len + rows - 1) >> shift;
-      if (mine.len > 0) order[atomicAdd(&count[n], 1)] = mine;
+      if (mine.len > 0) order[atomicAdd(&count[(mine.len + rows - 1) >> shift], 1)] = mine;
     }
   }
   __syncthreads();
-  // (count[n] is now what count[n - 1] was: sequences with n tiles and more)
+  // (count[k] is now the sequences with k tiles and more: those with exactly k end there)
   const int total = min(entries, p.cap[kind]);
   for (int e = (int)threadIdx.x; e < total; e += kThreads) {
-    int lo = 0, hi = nt - 1;                           // the first j with first[j] <= e
+    int lo = by_place ? 0 : 1, hi = nt;   // the smallest k with first[k] <= e
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (first[mid] <= e) hi = mid;
       else lo = mid + 1;
     }
-    PackedTile t = order[e - first[lo]];
-    t.tile = lo;
+    const int at = e - first[lo];
+    PackedTile t;
+    if (by_place) {
+      t = order[at];
+      t.tile = lo;
+    } else {
+      t = order[(lo < nt ? count[lo + 1] : 0) + at / lo];
+      t.tile = lo - 1 - at % lo;
+    }
     list[e] = t;
   }
   if (threadIdx.x == 0) {
@@ -163,7 +175,7 @@ PackedPlan::PackedPlan(int tokens_, int n_seqs_, int max_seq_, int window_)
   const long n = n_seqs < tokens ? n_seqs : tokens;   // sequences with a row
   bytes = 256;
   for (int k = 0; k < kPackedKinds; ++k) {
-    const long rows = 32L << k, nt = (max_seq + rows - 1) / rows;
+    const long rows = packed_rows(k), nt = (max_seq + rows - 1) / rows;
     cap[k] = (int)((tokens + (rows - 1) * n) / rows);
     tiles[k] = bytes;
     order[k] = tiles[k] + up((size_t)cap[k] * sizeof(PackedTile));

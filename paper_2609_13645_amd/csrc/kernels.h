@@ -293,10 +293,13 @@ struct DsPacked : DsWindow {
 // each kind there are), a list of each kind of tile, and what the builder keeps of the
 // sequences. All of it from the host's bounds alone: each list has room for what the
 // sequences can come to.
-constexpr int kPackedKinds = 4;   // tiles of 32, 64, 128 and 256 rows
+// Lists of tiles of 32, 64, 128 and 256 rows, the longest sequences first; and of 64 rows,
+// the tiles furthest into their sequence first.
+constexpr int kPackedKinds = 5;
+constexpr int packed_rows(int kind) { return kind == 4 ? 64 : 32 << kind; }
 struct PackedHeader {
   int32_t tokens, n_seqs, max_seq, window;
-  int32_t count[kPackedKinds];
+  int32_t count[kPackedKinds], pad[3];
 };
 struct PackedPlan {
   int tokens, n_seqs, max_seq, window;   // max_seq and window cut to tokens
