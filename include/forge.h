@@ -953,10 +953,10 @@ forge_status forge_attention_packed_fwd(const forge_attn_packed_cfg* cfg, const 
                                         const forge_bf16* qkv, forge_bf16* o, float* lse,
                                         forge_stream stream);
 
-/* Scratch bytes of forge_attention_packed_bwd: per-query statistics, partial sums
- * of dK and dV where few blocks would share the work, and the score gradient in
- * bf16, of each head 4 KB for every 64 keys x 32 queries that see each other, at
- * most: of full sequences of max_seq (or the window's band of them). Host only. */
+/* Scratch bytes of forge_attention_packed_bwd: per-query statistics, and the score
+ * gradient in bf16, of each head 4 KB for every 64 keys x 32 queries that see
+ * each other, at most: of full sequences of max_seq (or the window's band of
+ * them). Host only. */
 forge_status forge_attention_packed_bwd_workspace_bytes(const forge_attn_packed_cfg* cfg,
                                                         size_t* bytes);
 

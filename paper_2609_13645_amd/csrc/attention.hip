@@ -938,17 +938,13 @@ __device__ __forceinline__ KvWindowBlock kv_block(const AttnWindowArgs& a, int s
 // PACKED: the tiles of the list of 64 rows in turn, whose queries' tile qt has the most keys
 // first; key tile nkt - 1 - qt of the same sequence has as many queries. kv head fastest.
 struct KvPackedBlock {
-  int kt, b, m, z, step;   // as above
+  int kt, m;   // as above
   int j0, ns, len;
-  static constexpr int turn = 0;
+  static constexpr int b = 0, z = 0, step = 1, turn = 0;
   PackedTile t;
-  __device__ __forceinline__ KvPackedBlock(const AttnPackedArgs& a, int splits) {
-    const int r = (int)blockIdx.x % (a.n_kv_heads * splits);
-    t = packed_tile<64, true>(a, (int)blockIdx.x / (a.n_kv_heads * splits));
-    m = r % a.n_kv_heads;
-    b = 0;
-    z = r / a.n_kv_heads;
-    step = splits;
+  __device__ __forceinline__ explicit KvPackedBlock(const AttnPackedArgs& a) {
+    t = packed_tile<64, true>(a, (int)blockIdx.x / a.n_kv_heads);
+    m = (int)blockIdx.x % a.n_kv_heads;
     len = t.len;
     kt = (len + 63) / 64 - 1 - t.tile;
     j0 = 2 * kt;
@@ -956,8 +952,8 @@ struct KvPackedBlock {
     ns = min(j0 + L.nwin, L.ns) - j0;
   }
 };
-__device__ __forceinline__ KvPackedBlock kv_block(const AttnPackedArgs& a, int splits) {
-  return KvPackedBlock(a, splits);
+__device__ __forceinline__ KvPackedBlock kv_block(const AttnPackedArgs& a, int) {
+  return KvPackedBlock(a);
 }
 __device__ __forceinline__ DsPacked ds_layout(const AttnPackedArgs& a, const KvPackedBlock& k) {
   return ds_layout(a, k.t);
@@ -1008,12 +1004,11 @@ __device__ __forceinline__ float* kv_part(const AttnWindowArgs& a, float* part,
   return part + ((long)k.z * a.batch * a.seq + row) * width + k.m * D;
 }
 
-// PACKED: the block's rows of its split's partial sums [splits][tokens][n_kv * D].
+// PACKED: the pairs are not split.
 template <int D, bool V>
-__device__ __forceinline__ float* kv_part(const AttnPackedArgs& a, float* part,
-                                          const KvPackedBlock& k, long row) {
-  if (!part) return nullptr;
-  return part + (((long)k.z * a.seq + row) * a.n_kv_heads + k.m) * D;
+__device__ __forceinline__ float* kv_part(const AttnPackedArgs&, float*, const KvPackedBlock&,
+                                          long) {
+  return nullptr;
 }
 
 // One DMA instruction: 16 bytes per lane from a buffer of `bytes` bytes (zeros
@@ -2231,21 +2226,6 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
 }  // namespace
 
 namespace {
-// Where a split's rows of dK and dV (grid.y 0, 1) end: the plan's tiles of 64 rows in turn,
-// eight columns to a thread.
-__global__ __launch_bounds__(256) void attn_packed_sum_k(AttnPackedArgs a, int splits,
-                                                         bf16_t* __restrict__ dk,
-                                                         bf16_t* __restrict__ dv, long ld_d) {
-  const PackedTile t = packed_tile<64>(a, (int)blockIdx.x);
-  const int width = a.n_kv_heads * a.d, cpr = width / 8;
-  const int i = (int)blockIdx.z * 256 + (int)threadIdx.x;
-  const int r = t.tile * 64 + i / cpr, c = i % cpr * 8;
-  if (i >= 64 * cpr || r >= t.len) return;
-  const bool v = blockIdx.y != 0;
-  const long row = t.start + r;
-  split_sum((v ? a.pv : a.pk) + row * width + c, splits, (long)a.seq * width,
-            v ? 1.0f : a.scale, (v ? dv : dk) + row * ld_d + c);
-}
 // The plan's list of tiles of so many rows.
 constexpr int packed_kind(int rows) { return rows == 32 ? 0 : rows == 64 ? 1 : rows == 128 ? 2 : 3; }
 // f of the query heads in a block.
@@ -2259,22 +2239,17 @@ void packed_heads(const AttnPackedArgs& a, F&& f) {
 template <int D>
 hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16_t* o,
                              const uint16_t* dout, const float* lse, float* delta, uint16_t* ds,
-                             float* part, uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_d,
+                             uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_d,
                              hipStream_t s) {
-  using std::false_type;
   const long T = a.seq, rows = T * a.n_heads;
   const dim3 block(256);
-  const int splits = 1;
   const dim3 pgrid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
   hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
                      a.seq);
-  const dim3 kgrid((unsigned)(p.cap[1] * a.n_kv_heads * splits));
+  const dim3 kgrid((unsigned)(p.cap[1] * a.n_kv_heads));
   hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, false, false>), kgrid, block, 0, s, a, dout,
-                     delta, ds, dv, dk, ld_d, a.pv, a.pk, splits);
-  if (splits > 1) {
-    const dim3 grid((unsigned)p.cap[1], 2, (unsigned)((8 * a.n_kv_heads * D + 255) / 256));
-    hipLaunchKernelGGL(attn_packed_sum_k, grid, block, 0, s, a, splits, dk, dv, ld_d);
-  }
+                     delta, ds, dv, dk, ld_d, static_cast<float*>(nullptr),
+                     static_cast<float*>(nullptr), 1);
   packed_heads(a, [&](auto heads) {
     constexpr int HW = decltype(heads)::value;
     const dim3 grid((unsigned)(p.cap[packed_kind(256 / HW)] * (a.n_heads / HW)));
@@ -2300,14 +2275,12 @@ hipError_t attn_packed_fwd(const AttnPackedArgs& a, const PackedPlan& p, uint16_
                            hipStream_t s) {
   return a.d == 128 ? attn_packed_fwd_d<128>(a, p, o, lse, s) : attn_packed_fwd_d<64>(a, p, o, lse, s);
 }
-size_t attn_packed_bwd_part_bytes(const AttnPackedArgs&, const PackedPlan&) { return 0; }
 hipError_t attn_packed_bwd(const AttnPackedArgs& a, const PackedPlan& p, const uint16_t* o,
                            const uint16_t* dout, const float* lse, float* delta, uint16_t* ds,
-                           float* part, uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_d,
-                           hipStream_t s) {
+                           uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_d, hipStream_t s) {
   return a.d == 128
-             ? attn_packed_bwd_d<128>(a, p, o, dout, lse, delta, ds, part, dq, dk, dv, ld_d, s)
-             : attn_packed_bwd_d<64>(a, p, o, dout, lse, delta, ds, part, dq, dk, dv, ld_d, s);
+             ? attn_packed_bwd_d<128>(a, p, o, dout, lse, delta, ds, dq, dk, dv, ld_d, s)
+             : attn_packed_bwd_d<64>(a, p, o, dout, lse, delta, ds, dq, dk, dv, ld_d, s);
 }
 
 hipError_t attn_bwd(const AttnArgs& a, const uint16_t* o, const uint16_t* dout, const float* lse,

@@ -2302,7 +2302,7 @@ forge_status forge_attention_packed_bwd_workspace_bytes(const forge_attn_packed_
   const PackedCfg p(*cfg);
   const PackedArgs a(*cfg, p, nullptr, nullptr);
   *bytes = up(2 * (size_t)cfg->n_heads * cfg->tokens * 4) +
-           up((size_t)cfg->n_heads * a.ds_head * 2) + up(forge::attn_packed_bwd_part_bytes(a, p));
+           up((size_t)cfg->n_heads * a.ds_head * 2);
   return ok();
 }
 
@@ -2327,11 +2327,9 @@ forge_status forge_attention_packed_bwd(const forge_attn_packed_cfg* cfg, const 
               FORGE_ERR_INVALID_ARG, "d_qkv overlaps an input");
   const long hq = (long)cfg->n_heads * cfg->head_dim, hkv = (long)cfg->n_kv_heads * cfg->head_dim;
   const size_t ds_off = up(2 * (size_t)cfg->n_heads * cfg->tokens * 4);
-  const size_t part_off = ds_off + up((size_t)cfg->n_heads * a.ds_head * 2);
   FORGE_HIP(forge::attn_packed_bwd(a, p, o, d_o, lse, static_cast<float*>(workspace),
-                                   at<uint16_t>(workspace, ds_off), at<float>(workspace, part_off),
-                                   d_qkv, d_qkv + hq, d_qkv + hq + hkv, a.ld_qkv,
-                                   (hipStream_t)stream));
+                                   at<uint16_t>(workspace, ds_off), d_qkv, d_qkv + hq,
+                                   d_qkv + hq + hkv, a.ld_qkv, (hipStream_t)stream));
   return ok();
 }
 

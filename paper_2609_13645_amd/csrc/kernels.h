@@ -316,10 +316,6 @@ struct AttnPackedArgs : AttnArgs {
   const PackedTile* tiles[kPackedKinds];
   int n_seqs, max_seq;
   long ds_head;                          // elements of a head's dS
-  float *pk = nullptr, *pv = nullptr;    // the kv pass' partial sums
-  // the forward's outputs
-  const uint16_t* o = nullptr;
-  const float* lse = nullptr;
 };
 // pos (may be NULL): every token's place in its sequence.
 hipError_t attn_packed_plan(const PackedPlan& p, const int32_t* offsets, void* plan, int32_t* pos,
@@ -348,11 +344,9 @@ hipError_t attn_window_bwd(const AttnWindowArgs& a, const uint16_t* o, const uin
                            const float* lse, float* delta, uint16_t* ds, float* part, uint16_t* dq,
                            uint16_t* dk, uint16_t* dv, long ld_dqkv, hipStream_t s);
 // The same of packed sequences; dS: 4096 * n_heads * p.ds_blocks bytes.
-size_t attn_packed_bwd_part_bytes(const AttnPackedArgs& a, const PackedPlan& p);
 hipError_t attn_packed_bwd(const AttnPackedArgs& a, const PackedPlan& p, const uint16_t* o,
                            const uint16_t* dout, const float* lse, float* delta, uint16_t* ds,
-                           float* part, uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_dqkv,
-                           hipStream_t s);
+                           uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_dqkv, hipStream_t s);
 
 // ----------------------------------------------------------------- MoE ----
 // Routing of fp32 logits [T, E] (E <= 256): idx / gates [T, k], probs [T, E];
