@@ -15,11 +15,10 @@
 namespace forge {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kLdsBins = 4096;   // tiles of a sequence whose counts fit LDS
 
 // Inclusive sum (or maximum) over the workgroup's threads; every thread gets the total too.
-template <bool MAX>
+template <int THREADS, bool MAX>
 __device__ __forceinline__ int scan(int x, int* lds, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const auto join = [](int a, int b) { return MAX ? max(a, b) : a + b; };
@@ -34,7 +33,7 @@ __device__ __forceinline__ int scan(int x, int* lds, int& total) {
   int before = MAX ? INT32_MIN : 0;
   total = before;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     const int y = lds[w];
     if (w < wave) before = join(before, y);
     total = join(total, y);
@@ -42,7 +41,8 @@ __device__ __forceinline__ int scan(int x, int* lds, int& total) {
   return join(before, x);
 }
 
-// The sequences, kThreads at a time, a thread to each.
+// The sequences, THREADS at a time, a thread to each.
+template <int THREADS>
 struct Sequences {
   const PackedPlan& p;
   const int32_t* offsets;
@@ -57,7 +57,7 @@ struct Sequences {
     // the offsets' running maximum; a sequence starts where that before it ends
     if (s0 == 0) end = offset(0);
     const int last = end;
-    const int e = scan<true>(max(offset(s + 1), last), lds, end);
+    const int e = scan<THREADS, true>(max(offset(s + 1), last), lds, end);
     int start = __shfl_up(e, 1, 64);
     __syncthreads();
     if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = e;
@@ -66,34 +66,42 @@ struct Sequences {
     const int len = s < p.n_seqs ? min(e - start, p.max_seq) : 0;
     const int blocks = len > 0 ? (int)DsPacked(len, p.window, 0, 0).blocks() : 0;
     int total;
-    const int b = base + scan<false>(blocks, lds, total) - blocks;
+    const int b = base + scan<THREADS, false>(blocks, lds, total) - blocks;
     base += total;
     return PackedTile{start, len, 0, b};
   }
 };
 
-// One workgroup for each kind of tile.
-template <bool LDS>
-__global__ __launch_bounds__(kThreads) void packed_plan_k(PackedPlan p,
+// One workgroup for each kind of tile. BINS, ORDER: the counts, the sequences in their order
+// lie in LDS and not behind the lists. Bound by latencies: a dozen barriers, the offsets'
+// load and the lists' stores.
+template <int THREADS, bool BINS, bool ORDER>
+__global__ __launch_bounds__(THREADS) void packed_plan_k(PackedPlan p,
                                                           const int32_t* __restrict__ offsets,
                                                           char* plan) {
-  __shared__ int lds[kWaves];
-  __shared__ int bins[LDS ? 2 * (kLdsBins + 1) : 1];
+  __shared__ int lds[THREADS / 64];
+  __shared__ int bins[BINS ? 2 * (kLdsBins + 1) : 1];
+  __shared__ PackedTile by_tiles[ORDER ? THREADS : 1];
   const int kind = (int)blockIdx.x, rows = packed_rows(kind), shift = 31 - __builtin_clz(rows);
   const bool by_place = kind == 4;
   const int nt = (p.max_seq + rows - 1) >> shift;   // tiles of a sequence, at most
   // per number of tiles k: how many sequences have exactly k, then how many have more;
   // the entries before those of k tiles (by_place: before tile k of any sequence)
-  int* count = LDS ? bins : reinterpret_cast<int*>(plan + p.bins[kind]);
+  int* count = BINS ? bins : reinterpret_cast<int*>(plan + p.bins[kind]);
   int* first = count + nt + 1;
-  PackedTile* order = reinterpret_cast<PackedTile*>(plan + p.order[kind]);
+  PackedTile* order = ORDER ? by_tiles : reinterpret_cast<PackedTile*>(plan + p.order[kind]);
   PackedTile* list = reinterpret_cast<PackedTile*>(plan + p.tiles[kind]);
-  for (int j = (int)threadIdx.x; j <= nt; j += kThreads) count[j] = 0;
+  // (in memory the atomics pass the vector cache, and so must what reads after them)
+  const auto counted = [&](int k) {
+    if constexpr (BINS) return count[k];
+    else return __hip_atomic_load(&count[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  for (int j = (int)threadIdx.x; j <= nt; j += THREADS) count[j] = 0;
   __syncthreads();
   PackedTile mine{};
   {
-    Sequences seqs{p, offsets, lds};
-    for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
+    Sequences<THREADS> seqs{p, offsets, lds};
+    for (int s0 = 0; s0 < p.n_seqs; s0 += THREADS) {
       mine = seqs.next(s0);
       if (mine.len > 0) atomicAdd(&count[(mine.len + rows - 1) >> shift], 1);
     }
@@ -101,14 +109,14 @@ __global__ __launch_bounds__(kThreads) void packed_plan_k(PackedPlan p,
   __syncthreads();
   // from the most tiles down: the sequences with more, and the entries before
   int longer = 0, entries = 0;
-  for (int k0 = 0; k0 <= nt; k0 += kThreads) {
+  for (int k0 = 0; k0 <= nt; k0 += THREADS) {
     const int k = nt - k0 - (int)threadIdx.x;
-    const int exactly = k >= 0 ? count[k] : 0;
+    const int exactly = k >= 0 ? counted(k) : 0;
     int total;
-    const int more = longer + scan<false>(exactly, lds, total) - exactly;
+    const int more = longer + scan<THREADS, false>(exactly, lds, total) - exactly;
     longer += total;
     const int tiles = k < 0 ? 0 : by_place ? more : exactly * k;
-    const int before = entries + scan<false>(tiles, lds, total) - tiles;
+    const int before = entries + scan<THREADS, false>(tiles, lds, total) - tiles;
     entries += total;
     if (k >= 0) {
       count[k] = more;
@@ -119,16 +127,16 @@ __global__ __launch_bounds__(kThreads) void packed_plan_k(PackedPlan p,
   // the sequences in that order (which of equals comes first decides nothing but the
   // blocks' order)
   {
-    Sequences seqs{p, offsets, lds};
-    for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
-      if (p.n_seqs > kThreads) mine = seqs.next(s0);
+    Sequences<THREADS> seqs{p, offsets, lds};
+    for (int s0 = 0; s0 < p.n_seqs; s0 += THREADS) {
+      if (p.n_seqs > THREADS) mine = seqs.next(s0);
       if (mine.len > 0) order[atomicAdd(&count[(mine.len + rows - 1) >> shift], 1)] = mine;
     }
   }
   __syncthreads();
   // (count[k] is now the sequences with k tiles and more: those with exactly k end there)
   const int total = min(entries, p.cap[kind]);
-  for (int e = (int)threadIdx.x; e < total; e += kThreads) {
+  for (int e = (int)threadIdx.x; e < total; e += THREADS) {
     int lo = by_place ? 0 : 1, hi = nt;   // the smallest k with first[k] <= e
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
@@ -141,7 +149,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_k(PackedPlan p,
       t = order[at];
       t.tile = lo;
     } else {
-      t = order[(lo < nt ? count[lo + 1] : 0) + at / lo];
+      t = order[(lo < nt ? counted(lo + 1) : 0) + at / lo];
       t.tile = lo - 1 - at % lo;
     }
     list[e] = t;
@@ -192,10 +200,17 @@ PackedPlan::PackedPlan(int tokens_, int n_seqs_, int max_seq_, int window_)
 hipError_t attn_packed_plan(const PackedPlan& p, const int32_t* offsets, void* plan, int32_t* pos,
                             hipStream_t s) {
   char* out = static_cast<char*>(plan);
-  const dim3 grid(kPackedKinds), block(kThreads);
-  if (p.max_seq <= 32 * (kLdsBins - 1))
-    hipLaunchKernelGGL(packed_plan_k<true>, grid, block, 0, s, p, offsets, out);
-  else hipLaunchKernelGGL(packed_plan_k<false>, grid, block, 0, s, p, offsets, out);
+  const bool bins = p.max_seq <= 32 * (kLdsBins - 1);
+  const auto build = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(kPackedKinds), dim3(threads), 0, s, p, offsets, out);
+  };
+  // Fewer threads wait less for each other, more fill long lists sooner: 5 sequences of 611
+  // rows 3.8 us (of 1024 threads 5.4), 41 of 16384 5.0 (5.6), 4 of 32768 6.8 (5.8).
+  if (bins && p.n_seqs <= 256 && p.cap[0] <= 768) build(packed_plan_k<256, true, true>, 256);
+  else if (bins && p.n_seqs <= 1024) build(packed_plan_k<1024, true, true>, 1024);
+  else if (bins) build(packed_plan_k<1024, true, false>, 1024);
+  else if (p.n_seqs <= 1024) build(packed_plan_k<1024, false, true>, 1024);
+  else build(packed_plan_k<1024, false, false>, 1024);
   if (pos)
     hipLaunchKernelGGL(packed_positions_k, dim3((unsigned)p.cap[1]), dim3(64), 0, s, p,
                        static_cast<const char*>(plan), pos);

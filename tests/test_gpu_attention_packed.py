@@ -367,3 +367,29 @@ def test_many_sequences_and_far_rows():
         o = (z.softmax(2) @ v).transpose(0, 1).reshape(n, nh * d)
         got = c.o[a:a + n].double()
         assert float((got - o).norm() / o.norm()) <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("more", [30, 600, 1500])
+@pytest.mark.parametrize("longest", [2100, 131100])
+def test_plans_of_every_size(more, longest):
+    """Sequences few or more than a workgroup's threads, of few tiles or of more than its
+    LDS has counts for: every row once, at its place (zero scores: its log-sum-exp is the
+    log of its keys, whose number fp32 holds)."""
+    import torch
+    banner(f"packed plan more={more} longest={longest}")
+    lens = [300, 0, longest, 65, 64, 1, 1900] + [(5 * i) % 97 for i in range(more)]
+    off = offsets_of(lens, 3)
+    T = int(off[-1]) + 7
+    qkv = torch.zeros((T, 3 * 64), dtype=torch.bfloat16, device="cuda")
+    c = Call(off, T, longest, 1, 1, 64, 0, qkv, fill=-9.0)
+    for _ in range(2):
+        c.pos.fill_(-7)
+        c.lse.fill_(-9.0)
+        c.run()
+        torch.cuda.synchronize()
+        pos = packed.positions(off, T, longest)
+        inside = packed.covered(off, T, longest)
+        assert np.array_equal(c.pos.cpu().numpy(), np.where(inside, pos, -7))
+        lse = c.lse[0].cpu().numpy()
+        assert np.all(lse[~inside] == -9.0)
+        assert np.max(np.abs(lse[inside] - np.log(pos[inside] + 1.0))) <= 1e-5
