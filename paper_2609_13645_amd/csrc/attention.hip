@@ -851,7 +851,7 @@ __global__ __launch_bounds__(256) void attn_bwd_prep_k(const bf16_t* __restrict_
 // loop). At the end the four waves' sums are added through LDS in wave
 // order, so the result does not depend on timing, and written as bf16 (or,
 // where a block holds one split of the pairs, as fp32 partial sums); K / V
-// are read once per GQA group.
+// are read once per GQA group. (PACKED: of NW waves, for short sequences.)
 template <int D>
 struct KvPlan {
   static constexpr int BK = 64, BQ = 32;
@@ -861,13 +861,13 @@ struct KvPlan {
 };
 // A wave's buffer (Q, dO slabs, -LSE log2 e | -delta) and its DMA instructions
 // per pair; behind the eight buffers, at D = 128, tiles of V and K.
-template <int D>
+template <int D, int NW>
 struct KvBuf {
   using P = KvPlan<D>;
   static constexpr int WBUF = 2 * P::SLAB + 16;
   static constexpr int DMA = 2 * P::PER + 1;
-  static constexpr int ALL = 8 * WBUF + (D == 128 ? 3 * P::SLAB : 0);   // V and half of K at D = 128
-  static constexpr int ARR = ALL > 4 * P::RED ? ALL : 4 * P::RED;
+  static constexpr int ALL = 2 * NW * WBUF + (D == 128 ? 3 * P::SLAB : 0);   // V and half of K at D = 128
+  static constexpr int ARR = ALL > NW * P::RED ? ALL : NW * P::RED;
 };
 // Key tile, batch row, kv head and split of a key-owned block: kv head fastest,
 // key tile slowest.
@@ -1081,6 +1081,46 @@ __device__ __forceinline__ void kv_reduce_store(const f32x16_t (&acc)[D / 32][2]
   }
 }
 
+// The same of one or two waves, whose rows are all tokens'.
+template <int D, int NW>
+__device__ __forceinline__ void kv_few_store(const f32x16_t (&acc)[D / 32][2], uint4* sm, int wave,
+                                             int lane, float scale, bf16_t* out, long ld,
+                                             int nkeys) {
+  using P = KvPlan<D>;
+  const int hh = lane >> 5, l32 = lane & 31;
+  float* red = reinterpret_cast<float*>(sm + wave * P::RED);
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));   // the unused last reload
+  __syncthreads();
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(red + (kb * 32 + l32) * (D + 4) + db * 32 + g * 8 + hh * 4) =
+            make_float4(acc[db][kb][g * 4], acc[db][kb][g * 4 + 1], acc[db][kb][g * 4 + 2],
+                        acc[db][kb][g * 4 + 3]);
+  __syncthreads();
+  const int piece = threadIdx.x & 3;
+#pragma unroll
+  for (int i = 0; i < 4 / NW; ++i) {
+    const int key = i * 16 * NW + (threadIdx.x >> 2);
+    if (key >= nkeys) continue;
+    const float* w = reinterpret_cast<const float*>(sm) + key * (D + 4) + piece * 8;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      float f[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        f[u] = w[j * 32 + u];
+        if constexpr (NW == 2) f[u] += w[P::RED * 4 + j * 32 + u];
+        f[u] *= scale;
+      }
+      *reinterpret_cast<uint4*>(out + (long)key * ld + piece * 8 + j * 32) = pack8(f);
+    }
+  }
+}
+
 // Per pair: S, P = exp2(S c - LSE log2 e), dP - delta, dS = P (dP - delta) stored,
 // dV^T += dO^T P, dK^T += Q^T dS. The block's K and V rows are held as two 32-key
 // column blocks, so every Q / dO fragment read from LDS feeds two MFMAs. dK comes
@@ -1132,8 +1172,8 @@ __device__ __forceinline__ f32x16_t rows16(const bf16x8_t (&r)[4]) {
   return x;
 }
 
-template <int D, typename Args, bool CACHED, bool STATS>
-__global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
+template <int D, typename Args, bool CACHED, bool STATS, int NW = 4>
+__global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
                                                        const bf16_t* __restrict__ dout,
                                                        const float* __restrict__ delta,
                                                        bf16_t* __restrict__ ds,
@@ -1142,7 +1182,7 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
                                                        float* __restrict__ pv,
                                                        float* __restrict__ pk, int splits) {
   using P = KvPlan<D>;
-  using B = KvBuf<D>;
+  using B = KvBuf<D, NW>;
   constexpr bool WIN = kWindow<Args>;
   constexpr bool VL = kVInLds<D>;
   constexpr int BK = P::BK, BQ = P::BQ, SLAB = P::SLAB, KK = D / 16, DB = D / 32;
@@ -1213,9 +1253,9 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
   const uint32_t ro = ros[0], to0 = tos[0][0], to1 = tos[0][1];
   // V rows of the block's keys, then K rows of the first 32: natural 32-row tiles
   // behind the waves' buffers
-  uint4* vt = sm + 8 * B::WBUF;
+  uint4* vt = sm + 2 * NW * B::WBUF;
   if constexpr (VL) {
-    for (int i = wave; i < 3 * P::PER; i += 4) {
+    for (int i = wave; i < 3 * P::PER; i += NW) {
       const int t = i / P::PER, row = (i % P::PER) * P::RPI + lane / P::LPR;
       const int r0 = k0 + (t == 1 ? 32 : 0);
       const bf16_t* src = t == 2 ? a.k : a.v;
@@ -1243,7 +1283,7 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
     int n, q0;
     const char *q, *o;   // the pair's rows of Q and dO
   };
-  const int p0 = wave + 4 * kb_.z, step = 4 * splits;
+  const int p0 = wave + NW * kb_.z, step = NW * splits;
   const int step_n = step % grp, step_q = step / grp * BQ;
   const int qrb = (int)(a.ld_qkv * 2), orb = (int)(ldo * 2);   // bytes of a row
   const long q_adv = (long)step_n * D * 2 - (long)step_q * qrb;
@@ -1567,6 +1607,12 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_kv_k(Args a,
     cur ^= 1;
   }
   if (dsblk) store_ds();
+  if constexpr (NW < 4) {
+    kv_few_store<D, NW>(acc, sm, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D, ld_d, S - k0);
+    kv_few_store<D, NW>(acck, sm, wave, lane, a.scale, dk + (rb + k0) * ld_d + (long)m * D, ld_d,
+                        S - k0);
+    return;
+  }
   kv_reduce_store<D>(acc, sm, sm + 2 * P::RED, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D,
                      ld_d, kv_part<D, true>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D,
                      rows_of(a, S) - k0, S - k0);
@@ -1673,10 +1719,10 @@ __global__ __launch_bounds__(256) void attn_window_sum_k(AttnWindowArgs a, long 
 // tile's DMA issued two tiles ahead, and each wave waits only for the
 // oldest stage's DMA. A wave whose queries all precede a tile skips it;
 // blocks of a tile that do not exist (queries before the keys) are fetched
-// as zeros.
-template <int D, int WAVES>
+// as zeros. (PACKED: or 128 and two stages, DMA one tile ahead, for short sequences.)
+template <int D, int WAVES, int STAGES>
 struct DqPlan {
-  static constexpr int NW = WAVES, BQ = 32 * NW, BKV = 64, NST = 3;
+  static constexpr int NW = WAVES, BQ = 32 * NW, BKV = 64, NST = STAGES;
   static constexpr int NAT = BKV * D / 8;      // K tile chunks
   static constexpr int NDS = BKV * BQ / 8;     // dS tile chunks (NW 4 KB blocks)
   static constexpr int STAGE = NAT + NDS;
@@ -1684,10 +1730,10 @@ struct DqPlan {
 };
 
 // (HW as in the forward)
-template <int D, typename Args, int WAVES, int KG, int HW = 1>
+template <int D, typename Args, int WAVES, int KG, int HW = 1, int STAGES = 3>
 __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
     Args a, const bf16_t* __restrict__ ds, bf16_t* __restrict__ dq, long ld_d) {
-  using Q = DqPlan<D, WAVES>;
+  using Q = DqPlan<D, WAVES, STAGES>;
   constexpr bool WIN = kWindow<Args>;
   constexpr int BQ = Q::BQ / HW, BKV = Q::BKV, NAT = Q::NAT, NW = Q::NW, NST = Q::NST, DB = D / 32;
   __shared__ uint4 sm_[KG * NST * Q::STAGE];   // (of each group of waves)
@@ -1859,14 +1905,18 @@ __global__ __launch_bounds__(64 * WAVES * KG, 1) void attn_bwd_dq_k(
   const int steps = (nkt + KG - 1) / KG;   // (the same for every group: the barriers)
   if (!WIN || nkt > 0) {
     if (KG == 1 || kg < nkt) dma(tile_of(0), 0);
-    if (at(1) < nkt) dma(tile_of(1), 1);
-    sync(at(1) < nkt);
+    if (NST == 3 && at(1) < nkt) dma(tile_of(1), 1);
+    sync(NST == 3 && at(1) < nkt);
   }
   int st = 0;
   for (int j = 0; j < steps; ++j) {
-    if (at(j + 2) < nkt) dma(tile_of(j + 2), st == 0 ? 2 : st - 1);
+    if constexpr (NST == 3) {
+      if (at(j + 2) < nkt) dma(tile_of(j + 2), st == 0 ? 2 : st - 1);
+    } else {
+      if (at(j + 1) < nkt) dma(tile_of(j + 1), 1 - st);
+    }
     if (KG == 1 || at(j) < nkt) tile(tile_of(j), st);
-    if (j + 1 < steps) sync(at(j + 2) < nkt);
+    if (j + 1 < steps) sync(NST == 3 && at(j + 2) < nkt);
     st = st == NST - 1 ? 0 : st + 1;
   }
   if constexpr (KG > 1) {
@@ -2246,12 +2296,40 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   const dim3 pgrid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
   hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
                      a.seq);
-  const dim3 kgrid((unsigned)(p.cap[1] * a.n_kv_heads));
-  hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, false, false>), kgrid, block, 0, s, a, dout,
-                     delta, ds, dv, dk, ld_d, static_cast<float*>(nullptr),
-                     static_cast<float*>(nullptr), 1);
+  const auto kv_pass = [&](auto waves) {
+    constexpr int NW = decltype(waves)::value;
+    const dim3 grid((unsigned)(p.cap[1] * a.n_kv_heads));
+    hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, false, false, NW>), grid, dim3(64 * NW), 0,
+                       s, a, dout, delta, ds, dv, dk, ld_d, static_cast<float*>(nullptr),
+                       static_cast<float*>(nullptr), 1);
+  };
+  // Heads of 64: blocks of one or two waves, four or two on a CU, whose starts and ends the
+  // others cover, while the longest block still ends in time (its pairs and a wave's share of
+  // all, sequences that differ taken to be of a geometric law): 512 documents of 32 tokens,
+  // 32/8 heads 95 us in blocks of four waves, 61 of two, 51 of one; 64 of 256 111, 94, 83; 32
+  // of 512 168, 125, 126; 4 of 4096 714, 701, 739; 41 documents of 7 to 1605, mean 400, the
+  // backward 365, 351, 409. (Heads of 128: two waves and the V and K tiles take 91 KB.)
+  const long length = std::min<long>(p.max_seq, std::max<long>(2 * T / p.n_seqs, 1));
+  const double grp = a.n_heads / a.n_kv_heads, share = (double)p.cap[1] * a.n_heads / 1024 *
+                   std::min<long>(length / 64 + 1, p.window / 32 + 1);
+  const double longest = grp * std::min((p.max_seq + 31) / 32, (62 + p.window) / 32 + 1);
+  if (D == 64 && 1.2 * longest <= share) kv_pass(std::integral_constant<int, D == 64 ? 1 : 4>{});
+  else if (D == 64 && 0.55 * longest <= share)
+    kv_pass(std::integral_constant<int, D == 64 ? 2 : 4>{});
+  else kv_pass(std::integral_constant<int, 4>{});
+  // dQ: blocks of 128 (row, head) pairs with two stages, two on a CU, where sequences are short
+  // and a block's start counts; with heads of 64, 128: 512 documents of 32 tokens, 32/8 heads
+  // 69 and 97 us in blocks of 256 with three, so 38 and 63; 32 of 512 88 and 118, 85 and 111;
+  // 16 of 1024 136 and 167, 145 and 167; 4 of 4096 406 and 463, 464 and 505.
+  const bool shortish = length <= 1024;
   packed_heads(a, [&](auto heads) {
     constexpr int HW = decltype(heads)::value;
+    if (shortish) {
+      const dim3 grid((unsigned)(p.cap[packed_kind(128 / HW)] * (a.n_heads / HW)));
+      hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, 4, 1, HW, 2>), grid, block, 0, s, a,
+                         ds, dq, ld_d);
+      return;
+    }
     const dim3 grid((unsigned)(p.cap[packed_kind(256 / HW)] * (a.n_heads / HW)));
     hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, 8, 1, HW>), grid, dim3(512), 0, s, a, ds,
                        dq, ld_d);

@@ -40,6 +40,11 @@ CASES = [
     ([1500, 60, 900], 0, 0, 20, 4, 64, 0),
     ([400] * 9, 0, 0, 48, 6, 128, 300),
     ([3500, 500], 0, 0, 20, 4, 64, 0),
+    # (many blocks of key tiles: of two waves, then of one)
+    ([5, 40, 1, 90, 0, 33, 70] * 15, 3, 3, 32, 8, 64, 0),
+    ([130, 200, 64, 5, 90] * 8, 0, 2, 48, 24, 64, 40),
+    ([5, 40, 1, 90, 0, 33, 70] * 15, 0, 5, 64, 16, 64, 0),
+    ([130, 200, 64, 5, 90] * 8, 1, 0, 64, 32, 64, 40),
 ]
 
 
