@@ -80,8 +80,8 @@ __device__ __forceinline__ uint32_t wave_top(uint32_t x) {
 __device__ __forceinline__ const AdamTensor& tensor_of(const AdamBatch& b, int64_t& first) {
   int i = 0;
 #pragma unroll
-  for (int step = kAdamBatch / 2; step; step /= 2)
-    if ((int)blockIdx.x >= b.end[i + step - 1]) i += step;
+  for (int step = 32; step; step /= 2)
+    if (i + step <= kAdamBatch && (int)blockIdx.x >= b.end[min(i + step, kAdamBatch) - 1]) i += step;
   first = (int64_t)((int)blockIdx.x - (i ? b.end[i - 1] : 0)) * b.chunk;
   return b.t[i];
 }

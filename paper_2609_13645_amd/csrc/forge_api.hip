@@ -1789,9 +1789,8 @@ forge_status check_adamw_buffer(const AdamwBuffer& b, int i) {
   return FORGE_OK;
 }
 forge::AdamTensor adamw_tensor(const forge_adamw_multi_tensor& t, int i) {
-  return {t.master,  t.param, t.grad,     t.m,           t.v,        t.m_scale,
-          t.v_scale, t.n,     t.lr_scale, t.decay_scale, (uint32_t)i,
-          nullptr,   nullptr};
+  return {{t.master}, {t.grad},  t.param, t.m,        t.v,
+          t.m_scale,  t.v_scale, t.n,     t.lr_scale, t.decay_scale, (uint32_t)i};
 }
 }  // namespace
 
