@@ -851,7 +851,8 @@ __global__ __launch_bounds__(256) void attn_bwd_prep_k(const bf16_t* __restrict_
 // loop). At the end the four waves' sums are added through LDS in wave
 // order, so the result does not depend on timing, and written as bf16 (or,
 // where a block holds one split of the pairs, as fp32 partial sums); K / V
-// are read once per GQA group. (PACKED: of NW waves, for short sequences.)
+// are read once per GQA group. (PACKED: of NW waves and KB 32-key blocks: fewer
+// waves for short sequences, half of the keys where there are few blocks.)
 template <int D>
 struct KvPlan {
   static constexpr int BK = 64, BQ = 32;
@@ -859,15 +860,18 @@ struct KvPlan {
   static constexpr int RED = BK * (D + 4) / 4;    // one wave's [64][D + 4] fp32 sums
   static constexpr int LPR = D / 8, RPI = 64 / LPR, PER = BQ / RPI;  // DMA of a slab
 };
+// Whether V and the first 32 keys of K stay in LDS.
+template <int D, int KB>
+constexpr bool kVInLds = D == 128 && KB == 2;
 // A wave's buffer (Q, dO slabs, -LSE log2 e | -delta) and its DMA instructions
-// per pair; behind the eight buffers, at D = 128, tiles of V and K.
-template <int D, int NW>
+// per pair; behind the waves' two buffers each, at D = 128, tiles of V and K.
+template <int D, int NW, int KB>
 struct KvBuf {
   using P = KvPlan<D>;
   static constexpr int WBUF = 2 * P::SLAB + 16;
   static constexpr int DMA = 2 * P::PER + 1;
-  static constexpr int ALL = 2 * NW * WBUF + (D == 128 ? 3 * P::SLAB : 0);   // V and half of K at D = 128
-  static constexpr int ARR = ALL > NW * P::RED ? ALL : NW * P::RED;
+  static constexpr int ALL = 2 * NW * WBUF + (kVInLds<D, KB> ? 3 * P::SLAB : 0);
+  static constexpr int ARR = ALL > NW * KB * P::RED / 2 ? ALL : NW * KB * P::RED / 2;
 };
 // Key tile, batch row, kv head and split of a key-owned block: kv head fastest,
 // key tile slowest.
@@ -937,13 +941,17 @@ __device__ __forceinline__ KvWindowBlock kv_block(const AttnWindowArgs& a, int s
 }
 // PACKED: the tiles of the list of 64 rows in turn, whose queries' tile qt has the most keys
 // first; key tile nkt - 1 - qt of the same sequence has as many queries. kv head fastest.
+// KB 1: a block for each half of a tile.
+template <int KB>
 struct KvPackedBlock {
-  int kt, m;   // as above
+  int kt, m, half;   // as above
   int j0, ns, len;
   static constexpr int b = 0, z = 0, step = 1, turn = 0;
   PackedTile t;
   __device__ __forceinline__ explicit KvPackedBlock(const AttnPackedArgs& a) {
-    t = packed_tile<64, true>(a, (int)blockIdx.x / a.n_kv_heads);
+    int i = (int)blockIdx.x / a.n_kv_heads;
+    half = KB == 1 ? i & 1 : 0;
+    t = packed_tile<64, true>(a, KB == 1 ? i >> 1 : i);
     m = (int)blockIdx.x % a.n_kv_heads;
     len = t.len;
     kt = (len + 63) / 64 - 1 - t.tile;
@@ -952,10 +960,8 @@ struct KvPackedBlock {
     ns = min(j0 + L.nwin, L.ns) - j0;
   }
 };
-__device__ __forceinline__ KvPackedBlock kv_block(const AttnPackedArgs& a, int) {
-  return KvPackedBlock(a);
-}
-__device__ __forceinline__ DsPacked ds_layout(const AttnPackedArgs& a, const KvPackedBlock& k) {
+template <int KB>
+__device__ __forceinline__ DsPacked ds_layout(const AttnPackedArgs& a, const KvPackedBlock<KB>& k) {
   return ds_layout(a, k.t);
 }
 // The batch row's first row (of a row of S tokens), its place in the statistics of a head
@@ -1002,13 +1008,6 @@ __device__ __forceinline__ float* kv_part(const AttnWindowArgs& a, float* part,
   }
   if (!part) return nullptr;
   return part + ((long)k.z * a.batch * a.seq + row) * width + k.m * D;
-}
-
-// PACKED: the pairs are not split.
-template <int D, bool V>
-__device__ __forceinline__ float* kv_part(const AttnPackedArgs&, float*, const KvPackedBlock&,
-                                          long) {
-  return nullptr;
 }
 
 // One DMA instruction: 16 bytes per lane from a buffer of `bytes` bytes (zeros
@@ -1081,39 +1080,40 @@ __device__ __forceinline__ void kv_reduce_store(const f32x16_t (&acc)[D / 32][2]
   }
 }
 
-// The same of one or two waves, whose rows are all tokens'.
-template <int D, int NW>
-__device__ __forceinline__ void kv_few_store(const f32x16_t (&acc)[D / 32][2], uint4* sm, int wave,
+// PACKED: the same of NW waves' [32 KB keys][D], all of it here, whose rows are all tokens'.
+template <int D, int NW, int KB>
+__device__ __forceinline__ void kv_packed_store(const f32x16_t (&acc)[D / 32][KB], uint4* sm, int wave,
                                              int lane, float scale, bf16_t* out, long ld,
                                              int nkeys) {
-  using P = KvPlan<D>;
+  constexpr int ROW = D + 4, RED = 32 * KB * ROW;
   const int hh = lane >> 5, l32 = lane & 31;
-  float* red = reinterpret_cast<float*>(sm + wave * P::RED);
+  float* red = reinterpret_cast<float*>(sm) + wave * RED;
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));   // the unused last reload
   __syncthreads();
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4*>(red + (kb * 32 + l32) * (D + 4) + db * 32 + g * 8 + hh * 4) =
+        *reinterpret_cast<float4*>(red + (kb * 32 + l32) * ROW + db * 32 + g * 8 + hh * 4) =
             make_float4(acc[db][kb][g * 4], acc[db][kb][g * 4 + 1], acc[db][kb][g * 4 + 2],
                         acc[db][kb][g * 4 + 3]);
   __syncthreads();
   const int piece = threadIdx.x & 3;
 #pragma unroll
-  for (int i = 0; i < 4 / NW; ++i) {
-    const int key = i * 16 * NW + (threadIdx.x >> 2);
-    if (key >= nkeys) continue;
-    const float* w = reinterpret_cast<const float*>(sm) + key * (D + 4) + piece * 8;
+  for (int k = 0; k < 32 * KB; k += 16 * NW) {
+    const int key = k + (threadIdx.x >> 2);
+    if (key >= min(nkeys, 32 * KB)) continue;
+    const float* w = reinterpret_cast<const float*>(sm) + key * ROW + piece * 8;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
       float f[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         f[u] = w[j * 32 + u];
-        if constexpr (NW == 2) f[u] += w[P::RED * 4 + j * 32 + u];
+#pragma unroll
+        for (int i = 1; i < NW; ++i) f[u] += w[i * RED + j * 32 + u];
         f[u] *= scale;
       }
       *reinterpret_cast<uint4*>(out + (long)key * ld + piece * 8 + j * 32) = pack8(f);
@@ -1135,29 +1135,27 @@ __device__ __forceinline__ void kv_few_store(const f32x16_t (&acc)[D / 32][2], u
 // 606 here (651 with every DMA instruction's address formed anew); 16384 tokens,
 // 32 / 8 heads, 6.52 ms and 4.62 (4.86); 4 x 2047 tokens, 32 / 8 heads of 64,
 // 337 us and 214 (240).
-template <int D>
-constexpr bool kVInLds = D == 128;
 
 // K and V fragments that step i of a pair takes from LDS.
-template <int D>
+template <int D, bool VL>
 constexpr int kv_extra(int i) {
-  return !kVInLds<D> ? 0 : i < D / 16 ? 1 : i < D / 8 ? 2 : 0;
+  return !VL ? 0 : i < D / 16 ? 1 : i < D / 8 ? 2 : 0;
 }
 // LDS reads issued after those that step i waits for: ahead of step 0 the first
 // w fragments and the K fragments of steps 0 and 1; at the end of step j fragment
 // j + w (two reads where it is transposed), then the K or V of step j + 2 and,
 // two steps before dP, the four reads of -delta.
-template <int D>
+template <int D, bool VL>
 constexpr int kv_behind(int i, int nst, int w) {
   constexpr int KK = D / 16;
   const auto frag = [=](int f) { return f >= nst ? 0 : f < 2 * KK ? 1 : 2; };
   const int late = i == KK - 1 ? 4 : 0;
-  if (i == 0 && kv_extra<D>(0) > 0) return kv_extra<D>(1);
-  if (kv_extra<D>(i) > 0 || i == KK) return frag(i - 1 + w) + kv_extra<D>(i + 1) + late;
+  if (i == 0 && kv_extra<D, VL>(0) > 0) return kv_extra<D, VL>(1);
+  if (kv_extra<D, VL>(i) > 0 || i == KK) return frag(i - 1 + w) + kv_extra<D, VL>(i + 1) + late;
   int n = late;
   for (int f = i + 1; f < i + w; ++f) n += frag(f);
   for (int j = i - w; j < i; ++j)
-    if (j >= 0) n += kv_extra<D>(j + 2);
+    if (j >= 0) n += kv_extra<D, VL>(j + 2);
   return n;
 }
 // Sixteen floats of four 16-byte pieces.
@@ -1172,8 +1170,8 @@ __device__ __forceinline__ f32x16_t rows16(const bf16x8_t (&r)[4]) {
   return x;
 }
 
-template <int D, typename Args, bool CACHED, bool STATS, int NW = 4>
-__global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
+template <int D, typename Args, bool CACHED, bool STATS, int NW = 4, int KB = 2>
+__global__ __launch_bounds__(64 * NW, D == 64 && KB == 1 ? 2 : 1) void attn_bwd_kv_k(Args a,
                                                        const bf16_t* __restrict__ dout,
                                                        const float* __restrict__ delta,
                                                        bf16_t* __restrict__ ds,
@@ -1182,9 +1180,9 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
                                                        float* __restrict__ pv,
                                                        float* __restrict__ pk, int splits) {
   using P = KvPlan<D>;
-  using B = KvBuf<D, NW>;
+  using B = KvBuf<D, NW, KB>;
   constexpr bool WIN = kWindow<Args>;
-  constexpr bool VL = kVInLds<D>;
+  constexpr bool VL = kVInLds<D, KB>;
   constexpr int BK = P::BK, BQ = P::BQ, SLAB = P::SLAB, KK = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(256))) uint4 sm[B::ARR];
 
@@ -1192,13 +1190,17 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
   const int grp = a.n_heads / a.n_kv_heads;
   // block order: key tile slowest, so the low key tiles (the most work)
   // are dispatched first
-  const auto kb_ = kv_block(a, splits);
   constexpr bool PACKED = kPacked<Args>;
+  const auto kb_ = [&] {
+    if constexpr (PACKED) return KvPackedBlock<KB>(a);
+    else return kv_block(a, splits);
+  }();
   if constexpr (PACKED) {
     if (kb_.len == 0) return;
   }
   const int kt = kb_.kt, m = kb_.m, b = kb_.b;
-  const int k0 = kt * BK;
+  int k0 = kt * BK;
+  if constexpr (KB == 1) k0 += kb_.half * 32;
   if constexpr (WIN) {
     S = kb_.len;
     splits = kb_.step;
@@ -1220,9 +1222,9 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
 
   // K and V rows of the lane's two keys k0 + l32 and k0 + 32 + l32: the
   // B operands of S and dP
-  bf16x8_t kf[2][KK], vf[2][VL ? 1 : KK];   // (VL: kf[1] only)
+  bf16x8_t kf[KB][KK], vf[KB][VL ? 1 : KK];   // (VL: kf[1] only)
 #pragma unroll
-  for (int kb = 0; kb < 2; ++kb) {
+  for (int kb = 0; kb < KB; ++kb) {
     const int key = k0 + kb * 32 + l32;
     const long r = (rb + key) * a.ld_qkv + (long)m * D + hh * 8;
 #pragma unroll
@@ -1231,11 +1233,11 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
       if constexpr (!VL) vf[kb][kk] = gload_frag(a.v + r + kk * 16, key < S);
     }
   }
-  f32x16_t acc[DB][2], acck[DB][2];
+  f32x16_t acc[DB][KB], acck[DB][KB];
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < KB; ++kb) {
       zero(acc[db][kb]);
       zero(acck[db][kb]);
     }
@@ -1361,8 +1363,8 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
   // separate phases (products, then all probabilities and dS, then dV) the
   // matrix unit stood still during the second.
   constexpr int NST = 2 * KK + 4 * DB, W = 4;
-  constexpr int EP = D == 128 ? 20 : 16;   // probabilities formed under dP
-  u32x4_t dsp[4];              // packed dS of the last pair (piece u of key block kb: 2 kb + u)
+  constexpr int EP = VL ? 20 : 8 * KB;   // probabilities formed under dP
+  u32x4_t dsp[2 * KB];              // packed dS of the last pair (piece u of key block kb: 2 kb + u)
   bf16_t* dsblk = nullptr;     // its block
   // dS is written in accumulator order: 16-byte stores, 1 KB per wave
   // instruction; nontemporal, since it is read back only after the pass (as
@@ -1370,7 +1372,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
   // are written back while the next pass reads dS: 7 % on that pass)
   // (CACHED: ordinary, where all of dS fits that cache)
   auto store_ds = [&]() __attribute__((always_inline)) {
-    static_for<4>([&](auto J) __attribute__((always_inline)) {
+    static_for<2 * KB>([&](auto J) __attribute__((always_inline)) {
       constexpr int j = J;
       u32x4_t* piece = reinterpret_cast<u32x4_t*>(dsblk + (j / 2) * 1024 + (j % 2) * 512 +
                                                   (pc0 ^ ((j % 2) * 32)));
@@ -1424,19 +1426,19 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
         vr[i % 2][1] = fa::rd_b128<SLAB * 16>(vb ^ (k * 32));
       }
     };
-    f32x16_t sc[2], dp[2];
-    bf16x8_t pf[2];      // P of 16 queries packed, per key block
+    f32x16_t sc[KB], dp[KB];
+    bf16x8_t pf[KB];      // P of 16 queries packed, per key block
     // probability of score x (of 32): the first 16 queries of both key blocks,
     // then the others
     auto prob = [&](auto X) __attribute__((always_inline)) {
-      constexpr int kb = (X % 16) / 8, i = (X / 16) * 8 + X % 8;
+      constexpr int kb = (X % (8 * KB)) / 8, i = (X / (8 * KB)) * 8 + X % 8;
       const f32x4_t lv = __builtin_bit_cast(f32x4_t, row[i >> 2]);
       sc[kb][i] = fast_exp2(__builtin_fmaf(sc[kb][i], c, lv[i & 3]));
     };
     // four values of dS (half of a piece): the first 16 queries of both key
     // blocks, then the others
     auto dscore = [&](auto H) __attribute__((always_inline)) {
-      constexpr int kb = (H / 2) % 2, u = H / 4, i = u * 8 + (H % 2) * 4;
+      constexpr int kb = (H / 2) % KB, u = H / (2 * KB), i = u * 8 + (H % 2) * 4;
       float v[4];
       static_for<4>([&](auto E) __attribute__((always_inline)) {
         constexpr int e = E;
@@ -1449,35 +1451,35 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
     // the vector work behind MFMA x
     auto under = [&](auto X) __attribute__((always_inline)) {
       constexpr int x = X;
-      if constexpr (x < 2 * KK) {
+      if constexpr (x < KB * KK) {
         if constexpr (x == 0) {
           if (dsblk) store_ds();
         }
-        constexpr int i0 = B::DMA * x / (2 * KK), i1 = B::DMA * (x + 1) / (2 * KK);
+        constexpr int i0 = B::DMA * x / (KB * KK), i1 = B::DMA * (x + 1) / (KB * KK);
         static_for<i1 - i0>([&](auto V) __attribute__((always_inline)) {
           dma(fa::ic<i0 + V>{}, wn, z, next);
         });
-      } else if constexpr (x < 4 * KK) {
-        constexpr int N = 2 * KK - 2, t = x - 2 * KK - 2;
+      } else if constexpr (x < 2 * KB * KK) {
+        constexpr int N = KB * KK - KB, t = x - KB * KK - KB;
         if constexpr (t >= 0) {
           constexpr int v0 = EP * t / N, v1 = EP * (t + 1) / N;
           static_for<v1 - v0>([&](auto V) __attribute__((always_inline)) { prob(fa::ic<v0 + V>{}); });
         }
         if constexpr (t == N - 1) {
           pf[0] = pack_frag(sc[0], 0);
-          pf[1] = pack_frag(sc[1], 0);
+          if constexpr (KB > 1) pf[KB - 1] = pack_frag(sc[KB - 1], 0);
         }
-      } else if constexpr (x < 4 * KK + 2 * DB) {
-        constexpr int N = 2 * DB, R = 32 - EP, t = x - 4 * KK;
+      } else if constexpr (x < 2 * KB * KK + KB * DB) {
+        constexpr int N = KB * DB, R = 16 * KB - EP, t = x - 2 * KB * KK;
         constexpr int v0 = EP + R * t / N, v1 = EP + R * (t + 1) / N;
         static_for<v1 - v0>([&](auto V) __attribute__((always_inline)) { prob(fa::ic<v0 + V>{}); });
         if constexpr (t == N - 1) {
           pf[0] = pack_frag(sc[0], 1);
-          pf[1] = pack_frag(sc[1], 1);
+          if constexpr (KB > 1) pf[KB - 1] = pack_frag(sc[KB - 1], 1);
         }
-      } else if constexpr (x < 4 * KK + 6 * DB) {
-        constexpr int N = 4 * DB, t = x - 4 * KK - 2 * DB;
-        constexpr int h0 = 8 * t / N, h1 = 8 * (t + 1) / N;
+      } else if constexpr (x < 2 * KB * KK + 3 * KB * DB) {
+        constexpr int N = 2 * KB * DB, t = x - 2 * KB * KK - KB * DB;
+        constexpr int h0 = 4 * KB * t / N, h1 = 4 * KB * (t + 1) / N;
         static_for<h1 - h0>([&](auto V) __attribute__((always_inline)) { dscore(fa::ic<h0 + V>{}); });
       }
     };
@@ -1488,18 +1490,18 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
     }
     static_for<NST>([&](auto I) __attribute__((always_inline)) {
       constexpr int i = I;
-      fa::wait_lds<kv_behind<D>(i, NST, W)>();
+      fa::wait_lds<kv_behind<D, VL>(i, NST, W)>();
       fa::bind(fr[i % W]);
-      if constexpr (kv_extra<D>(i) > 0) fa::bind(vr[i % 2][0]);
-      if constexpr (kv_extra<D>(i) > 1) fa::bind(vr[i % 2][1]);
+      if constexpr (kv_extra<D, VL>(i) > 0) fa::bind(vr[i % 2][0]);
+      if constexpr (kv_extra<D, VL>(i) > 1) fa::bind(vr[i % 2][1]);
       if constexpr (i == 0) {
         static_for<4>([&](auto G) __attribute__((always_inline)) { fa::bind(row[G]); });
       }
       if constexpr (i == KK) {
         static_for<4>([&](auto G) __attribute__((always_inline)) { fa::bind(nd[G]); });
       }
-      static_for<2>([&](auto KB) __attribute__((always_inline)) {
-        constexpr int kb = KB;
+      static_for<KB>([&](auto BLK) __attribute__((always_inline)) {
+        constexpr int kb = BLK;
         if constexpr (i < KK) {
           if constexpr (VL && kb == 0)
             sc[kb] = MFMA(fr[i % W], vr[i % 2][0], i == 0 ? f32x16_t{} : sc[kb]);
@@ -1519,9 +1521,9 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
                                 acck[db][kb]);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (kb == 1 && i + W < NST) read(fa::ic<i + W>{});
-        if constexpr (VL && kb == 1 && i + 2 < 2 * KK) read_kv(fa::ic<i + 2>{});
-        if constexpr (kb == 1 && i == KK - 2)
+        if constexpr (kb == KB - 1 && i + W < NST) read(fa::ic<i + W>{});
+        if constexpr (VL && kb == KB - 1 && i + 2 < 2 * KK) read_kv(fa::ic<i + 2>{});
+        if constexpr (kb == KB - 1 && i == KK - 2)
           static_for<4>([&](auto G) __attribute__((always_inline)) {
             nd[G] = fa::rd_b128<LO + BQ * 4 + G * 32>(lb);
           });
@@ -1531,10 +1533,10 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
           if constexpr (WIN) {
             // (and where the window's far edge crosses the block: the queries that see
             // a key are a range, one subtraction and one comparison each)
-            if (q0 < k0 + BK - 1 || q0 + BQ > S ||
-                (k0 <= q0 + BQ - 1 - a.window && k0 + BK - 1 >= a.sinks)) {
+            if (q0 < k0 + 32 * KB - 1 || q0 + BQ > S ||
+                (k0 <= q0 + BQ - 1 - a.window && k0 + 32 * KB - 1 >= a.sinks)) {
 #pragma unroll
-              for (int mb = 0; mb < 2; ++mb) {
+              for (int mb = 0; mb < KB; ++mb) {
                 const int key = k0 + mb * 32 + l32;
                 const int end = key < a.sinks ? S : min(S, key + a.window);
                 const int lo = key - q0 - hh * 4, n = max(0, end - key);
@@ -1545,9 +1547,9 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
                 }
               }
             }
-          } else if (q0 < k0 + BK - 1 || q0 + BQ > S) {
+          } else if (q0 < k0 + 32 * KB - 1 || q0 + BQ > S) {
 #pragma unroll
-            for (int mb = 0; mb < 2; ++mb)
+            for (int mb = 0; mb < KB; ++mb)
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
                 const int q = q0 + (e >> 2) * 8 + hh * 4 + (e & 3);
@@ -1555,7 +1557,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
               }
           }
         }
-        under(fa::ic<2 * i + kb>{});
+        under(fa::ic<KB * i + kb>{});
         __builtin_amdgcn_sched_barrier(0);
       });
     });
@@ -1603,23 +1605,25 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_bwd_kv_k(Args a,
     const Pair wn = p + step < total ? advance(w) : w;
     pair(mine + cur * B::WBUF, w, mine + (cur ^ 1) * B::WBUF, wn);
     dsblk = ds + ((long)b * a.n_heads + w.n) * L.head + L.block(kt, w.q0 / BQ);
+    if constexpr (KB == 1) dsblk += kb_.half * 1024;
     w = wn;
     cur ^= 1;
   }
   if (dsblk) store_ds();
-  if constexpr (NW < 4) {
-    kv_few_store<D, NW>(acc, sm, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D, ld_d, S - k0);
-    kv_few_store<D, NW>(acck, sm, wave, lane, a.scale, dk + (rb + k0) * ld_d + (long)m * D, ld_d,
-                        S - k0);
-    return;
+  if constexpr (PACKED) {
+    kv_packed_store<D, NW, KB>(acc, sm, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D, ld_d,
+                               S - k0);
+    kv_packed_store<D, NW, KB>(acck, sm, wave, lane, a.scale, dk + (rb + k0) * ld_d + (long)m * D,
+                               ld_d, S - k0);
+  } else {
+    kv_reduce_store<D>(acc, sm, sm + 2 * P::RED, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D,
+                       ld_d, kv_part<D, true>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D,
+                       rows_of(a, S) - k0, S - k0);
+    kv_reduce_store<D>(acck, sm, sm + 2 * P::RED, wave, lane, a.scale,
+                       dk + (rb + k0) * ld_d + (long)m * D, ld_d,
+                       kv_part<D, false>(a, pk, kb_, rb + k0), (long)a.n_kv_heads * D,
+                       rows_of(a, S) - k0, S - k0);
   }
-  kv_reduce_store<D>(acc, sm, sm + 2 * P::RED, wave, lane, 1.0f, dv + (rb + k0) * ld_d + (long)m * D,
-                     ld_d, kv_part<D, true>(a, pv, kb_, rb + k0), (long)a.n_kv_heads * D,
-                     rows_of(a, S) - k0, S - k0);
-  kv_reduce_store<D>(acck, sm, sm + 2 * P::RED, wave, lane, a.scale,
-                     dk + (rb + k0) * ld_d + (long)m * D, ld_d,
-                     kv_part<D, false>(a, pk, kb_, rb + k0), (long)a.n_kv_heads * D,
-                     rows_of(a, S) - k0, S - k0);
 }
 
 // dK and dV from the splits' partial sums, added in split order; eight columns
@@ -2296,27 +2300,43 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   const dim3 pgrid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
   hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
                      a.seq);
-  const auto kv_pass = [&](auto waves) {
-    constexpr int NW = decltype(waves)::value;
-    const dim3 grid((unsigned)(p.cap[1] * a.n_kv_heads));
-    hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, false, false, NW>), grid, dim3(64 * NW), 0,
-                       s, a, dout, delta, ds, dv, dk, ld_d, static_cast<float*>(nullptr),
+  const auto kv_pass = [&](auto waves, auto blocks) {
+    constexpr int NW = decltype(waves)::value, KB = decltype(blocks)::value;
+    const dim3 grid((unsigned)(p.cap[1] * a.n_kv_heads * (2 / KB)));
+    hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, false, false, NW, KB>), grid, dim3(64 * NW),
+                       0, s, a, dout, delta, ds, dv, dk, ld_d, static_cast<float*>(nullptr),
                        static_cast<float*>(nullptr), 1);
   };
-  // Heads of 64: blocks of one or two waves, four or two on a CU, whose starts and ends the
-  // others cover, while the longest block still ends in time (its pairs and a wave's share of
-  // all, sequences that differ taken to be of a geometric law): 512 documents of 32 tokens,
-  // 32/8 heads 95 us in blocks of four waves, 61 of two, 51 of one; 64 of 256 111, 94, 83; 32
-  // of 512 168, 125, 126; 4 of 4096 714, 701, 739; 41 documents of 7 to 1605, mean 400, the
-  // backward 365, 351, 409. (Heads of 128: two waves and the V and K tiles take 91 KB.)
+  using std::integral_constant;
   const long length = std::min<long>(p.max_seq, std::max<long>(2 * T / p.n_seqs, 1));
   const double grp = a.n_heads / a.n_kv_heads, share = (double)p.cap[1] * a.n_heads / 1024 *
                    std::min<long>(length / 64 + 1, p.window / 32 + 1);
   const double longest = grp * std::min((p.max_seq + 31) / 32, (62 + p.window) / 32 + 1);
-  if (D == 64 && 1.2 * longest <= share) kv_pass(std::integral_constant<int, D == 64 ? 1 : 4>{});
-  else if (D == 64 && 0.55 * longest <= share)
-    kv_pass(std::integral_constant<int, D == 64 ? 2 : 4>{});
-  else kv_pass(std::integral_constant<int, 4>{});
+  const long blocks = (long)p.cap[1] * a.n_kv_heads;
+  // Few key tiles: a block for each half of one, on a CU that would idle (heads of 64: two on
+  // a CU), of eight waves where they have pairs enough and LDS holds their buffers. The backward
+  // of 8/2 heads of 128: 611 rows in 4 documents 37.2 us in blocks of 64 keys, so 28.7; 2048
+  // rows 151.0, 107.6; 8/8 heads, 2048 rows (256 tiles) 76.3, 71.7, in 4 documents 31.6, 34.2.
+  // Heads of 64: 26.8, 22.4 (of eight waves 21.4); 97.8, 77.6 (65.3); 51.8, 48.2 (50.2); 19.8,
+  // 18.9 (24.2). From 512 tiles on 4 to 20 % slower.
+  const bool halves = blocks <= 128 || (blocks <= 256 && (D == 64 || longest >= 64));
+  // Many, heads of 64: blocks of one or two waves, four or two on a CU, whose starts and ends
+  // the others cover, while the longest block still ends in time (its pairs and a wave's share
+  // of all, sequences that differ taken to be of a geometric law): 512 documents of 32 tokens,
+  // 32/8 heads 95 us in blocks of four waves, 61 of two, 51 of one; 64 of 256 111, 94, 83; 32
+  // of 512 168, 125, 126; 4 of 4096 714, 701, 739; 41 documents of 7 to 1605, mean 400, the
+  // backward 365, 351, 409. (Heads of 128: two waves and the V and K tiles take 91 KB.)
+  if (halves) {
+    if (D == 64 && longest >= (blocks <= 128 ? 40 : 160))
+      kv_pass(integral_constant<int, D == 64 ? 8 : 4>{}, integral_constant<int, 1>{});
+    else kv_pass(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+  } else if (D == 64 && 1.2 * longest <= share) {
+    kv_pass(integral_constant<int, D == 64 ? 1 : 4>{}, integral_constant<int, 2>{});
+  } else if (D == 64 && 0.55 * longest <= share) {
+    kv_pass(integral_constant<int, D == 64 ? 2 : 4>{}, integral_constant<int, 2>{});
+  } else {
+    kv_pass(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  }
   // dQ: blocks of 128 (row, head) pairs with two stages, two on a CU, where sequences are short
   // and a block's start counts; with heads of 64, 128: 512 documents of 32 tokens, 32/8 heads
   // 69 and 97 us in blocks of 256 with three, so 38 and 63; 32 of 512 88 and 118, 85 and 111;
