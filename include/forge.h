@@ -911,8 +911,8 @@ forge_status forge_attention_window_bwd(const forge_attn_window_cfg* cfg, const 
  * rows [offsets[s], offsets[s + 1]); they are read on the device, so they may
  * change from call to call (and between replays of a graph) within the
  * configuration's bounds. An empty sequence is one; rows before the first and
- * behind the last sequence belong to none: they are not read, and their rows of
- * every output are left as they were. Offsets are taken as their running
+ * behind the last sequence belong to none: nothing comes of what they hold, and
+ * their rows of every output are left as they were. Offsets are taken as their running
  * maximum and cut to [0, tokens]; of a sequence longer than max_seq the first
  * max_seq rows are taken, the others belong to none.
  * Rules: n_heads a multiple of n_kv_heads, head_dim 64 or 128; 1 <= tokens, 1 <=

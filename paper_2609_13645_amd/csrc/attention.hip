@@ -228,7 +228,7 @@ __device__ __forceinline__ PackedTile packed_tile(const AttnPackedArgs& a, int i
   if (i >= h.count[KIND] || h.tokens != a.seq || h.n_seqs != a.n_seqs ||
       h.max_seq != a.max_seq || h.window != a.window || t.start < 0 || t.len < 0 || t.tile < 0 ||
       t.len > a.seq - t.start || t.tile > (t.len - 1) / ROWS)
-    t.len = 0;
+    t = PackedTile{0, 0, 0, 0};
   return t;
 }
 
@@ -2282,35 +2282,62 @@ hipError_t attn_bwd_d(Args a, const uint16_t* o, const uint16_t* dout, const flo
 namespace {
 // The plan's list of tiles of so many rows.
 constexpr int packed_kind(int rows) { return rows == 32 ? 0 : rows == 64 ? 1 : rows == 128 ? 2 : 3; }
-// f of the query heads in a block.
-template <typename F>
+// f of the query heads in a block of so many waves, as a constant.
+template <int WAVES, typename F>
 void packed_heads(const AttnPackedArgs& a, F&& f) {
   const int grp = a.n_heads / a.n_kv_heads;
-  if (grp % 4 == 0) f(std::integral_constant<int, 4>{});
-  else if (grp % 2 == 0) f(std::integral_constant<int, 2>{});
+  if constexpr (WAVES >= 4) {
+    if (grp % 4 == 0) return f(std::integral_constant<int, 4>{});
+  }
+  if (grp % 2 == 0) f(std::integral_constant<int, 2>{});
   else f(std::integral_constant<int, 1>{});
 }
+// Blocks of so many waves, a query head's 32 rows each.
+template <int WAVES>
+long packed_blocks(const AttnPackedArgs& a, const PackedPlan& p) {
+  long n = 0;
+  packed_heads<WAVES>(a, [&](auto heads) {
+    constexpr int HW = decltype(heads)::value;
+    n = (long)p.cap[packed_kind(32 * WAVES / HW)] * (a.n_heads / HW);
+  });
+  return n;
+}
+// Key tiles that a sequence's last block has.
+int most_tiles(const PackedPlan& p) { return (std::min(p.max_seq, p.window) + 63) / 64; }
+// The length of the sequences that most tokens are in, taken to be of a geometric law where
+// they differ; whether one sequence has most tokens, whose tiles are of all sizes.
+long packed_length(const PackedPlan& p) {
+  return std::min<long>(p.max_seq, std::max(2L * p.tokens / p.n_seqs, 1L));
+}
+bool packed_one(const PackedPlan& p) { return 2 * packed_length(p) > p.tokens; }
+
 template <int D>
 hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16_t* o,
                              const uint16_t* dout, const float* lse, float* delta, uint16_t* ds,
-                             uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_d,
-                             hipStream_t s) {
-  const long T = a.seq, rows = T * a.n_heads;
-  const dim3 block(256);
-  const dim3 pgrid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
-  hipLaunchKernelGGL(attn_bwd_prep_k<D>, pgrid, block, 0, s, o, dout, lse, delta, rows, a.n_heads,
-                     a.seq);
-  const auto kv_pass = [&](auto waves, auto blocks) {
-    constexpr int NW = decltype(waves)::value, KB = decltype(blocks)::value;
-    const dim3 grid((unsigned)(p.cap[1] * a.n_kv_heads * (2 / KB)));
-    hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, false, false, NW, KB>), grid, dim3(64 * NW),
-                       0, s, a, dout, delta, ds, dv, dk, ld_d, static_cast<float*>(nullptr),
-                       static_cast<float*>(nullptr), 1);
-  };
+                             uint16_t* dq, uint16_t* dk, uint16_t* dv, long ld_d, hipStream_t s) {
+  using std::false_type;
   using std::integral_constant;
-  const long length = std::min<long>(p.max_seq, std::max<long>(2 * T / p.n_seqs, 1));
-  const double grp = a.n_heads / a.n_kv_heads, share = (double)p.cap[1] * a.n_heads / 1024 *
-                   std::min<long>(length / 64 + 1, p.window / 32 + 1);
+  const long T = a.seq, rows = T * a.n_heads;
+  a.o = o;
+  a.lse = lse;
+  const auto kv_pass = [&](auto waves, auto blocks, auto stats) {
+    constexpr int NW = decltype(waves)::value, KB = decltype(blocks)::value;
+    constexpr bool STATS = decltype(stats)::value;
+    if constexpr (!STATS) {
+      const dim3 grid((unsigned)(D == 64 ? (T + 31) / 32 * a.n_heads : (rows + 15) / 16));
+      hipLaunchKernelGGL(attn_bwd_prep_k<D>, grid, dim3(256), 0, s, o, dout, lse, delta, rows,
+                         a.n_heads, a.seq);
+    }
+    const dim3 grid((unsigned)(p.cap[1] * a.n_kv_heads * (2 / KB)));
+    hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, KB == 1, STATS, NW, KB>), grid,
+                       dim3(64 * NW), 0, s, a, dout, delta, ds, dv, dk, ld_d,
+                       static_cast<float*>(nullptr), static_cast<float*>(nullptr), 1);
+  };
+  // a block's pairs at most, a wave's share of all
+  const long length = packed_length(p);
+  const double grp = a.n_heads / a.n_kv_heads;
+  const double share = (double)p.cap[1] * a.n_heads / 1024 *
+                       std::min<long>(length / 64 + 1, p.window / 32 + 1);
   const double longest = grp * std::min((p.max_seq + 31) / 32, (62 + p.window) / 32 + 1);
   const long blocks = (long)p.cap[1] * a.n_kv_heads;
   // Few key tiles: a block for each half of one, on a CU that would idle (heads of 64: two on
@@ -2320,51 +2347,78 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   // Heads of 64: 26.8, 22.4 (of eight waves 21.4); 97.8, 77.6 (65.3); 51.8, 48.2 (50.2); 19.8,
   // 18.9 (24.2). From 512 tiles on 4 to 20 % slower.
   const bool halves = blocks <= 128 || (blocks <= 256 && (D == 64 || longest >= 64));
+  const bool eight = D == 64 && longest >= (blocks <= 128 ? 40 : 160);
+  // With two pairs to a wave at most (heads of 128: one) it forms the statistics itself, one
+  // launch fewer: one row, 4/2 heads of 64 10.1 us, so 8.0; 257 rows in three, 8/8 heads 12.6,
+  // 11.5. (Heads of 128, two pairs to a wave 16.8, 17.9.)
+  const bool stats = longest <= (D == 64 ? 8 : 4);
   // Many, heads of 64: blocks of one or two waves, four or two on a CU, whose starts and ends
-  // the others cover, while the longest block still ends in time (its pairs and a wave's share
-  // of all, sequences that differ taken to be of a geometric law): 512 documents of 32 tokens,
+  // the others cover, while the longest block still ends in time: 512 documents of 32 tokens,
   // 32/8 heads 95 us in blocks of four waves, 61 of two, 51 of one; 64 of 256 111, 94, 83; 32
   // of 512 168, 125, 126; 4 of 4096 714, 701, 739; 41 documents of 7 to 1605, mean 400, the
   // backward 365, 351, 409. (Heads of 128: two waves and the V and K tiles take 91 KB.)
-  if (halves) {
-    if (D == 64 && longest >= (blocks <= 128 ? 40 : 160))
-      kv_pass(integral_constant<int, D == 64 ? 8 : 4>{}, integral_constant<int, 1>{});
-    else kv_pass(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-  } else if (D == 64 && 1.2 * longest <= share) {
-    kv_pass(integral_constant<int, D == 64 ? 1 : 4>{}, integral_constant<int, 2>{});
-  } else if (D == 64 && 0.55 * longest <= share) {
-    kv_pass(integral_constant<int, D == 64 ? 2 : 4>{}, integral_constant<int, 2>{});
-  } else {
-    kv_pass(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-  }
-  // dQ: blocks of 128 (row, head) pairs with two stages, two on a CU, where sequences are short
-  // and a block's start counts; with heads of 64, 128: 512 documents of 32 tokens, 32/8 heads
-  // 69 and 97 us in blocks of 256 with three, so 38 and 63; 32 of 512 88 and 118, 85 and 111;
-  // 16 of 1024 136 and 167, 145 and 167; 4 of 4096 406 and 463, 464 and 505.
-  const bool shortish = length <= 1024;
-  packed_heads(a, [&](auto heads) {
-    constexpr int HW = decltype(heads)::value;
-    if (shortish) {
-      const dim3 grid((unsigned)(p.cap[packed_kind(128 / HW)] * (a.n_heads / HW)));
-      hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, 4, 1, HW, 2>), grid, block, 0, s, a,
-                         ds, dq, ld_d);
-      return;
-    }
-    const dim3 grid((unsigned)(p.cap[packed_kind(256 / HW)] * (a.n_heads / HW)));
-    hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, 8, 1, HW>), grid, dim3(512), 0, s, a, ds,
-                       dq, ld_d);
-  });
+  constexpr integral_constant<int, 4> four{};
+  constexpr integral_constant<int, D == 64 ? 8 : 4> most{};
+  constexpr integral_constant<int, D == 64 ? 2 : 4> two{};
+  constexpr integral_constant<int, D == 64 ? 1 : 4> one{};
+  constexpr integral_constant<int, 1> half{};
+  constexpr integral_constant<int, 2> whole{};
+  if (halves && stats) kv_pass(four, half, std::true_type{});
+  else if (halves && eight) kv_pass(most, half, false_type{});
+  else if (halves) kv_pass(four, half, false_type{});
+  else if (D == 64 && 1.2 * longest <= share) kv_pass(one, whole, false_type{});
+  else if (D == 64 && 0.55 * longest <= share) kv_pass(two, whole, false_type{});
+  else kv_pass(four, whole, false_type{});
+  // dQ. Few blocks: of 64 (row, head) pairs, their key tiles in two groups (the backward of
+  // 4096 rows, 8/8 heads of 128 150.7 us in blocks of 256, so 128.7; of 64 104.8, 82.2; 12/4,
+  // 2048 rows 94.9, 77.2 and 61.0, 48.1; 1024 blocks 136.0, 139.2). Else blocks of 128 with two
+  // stages, two on a CU, where sequences are short and a block's start counts, or blocks of 256
+  // were few; with heads of 64, 128 the pass of 512 documents of 32 tokens, 32/8 heads, 69 and 97
+  // us in blocks of 256 with three, so 38 and 63; 32 of 512 88 and 118, 85 and 111; 16 of 1024
+  // 136 and 167, 145 and 167; 4 of 4096 406 and 463, 464 and 505.
+  const auto dq_pass = [&](auto waves, auto groups, auto stages) {
+    constexpr int W = decltype(waves)::value, G = decltype(groups)::value;
+    constexpr int ST = decltype(stages)::value;
+    packed_heads<W>(a, [&](auto heads) {
+      constexpr int HW = decltype(heads)::value;
+      const dim3 grid((unsigned)packed_blocks<W>(a, p));
+      hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, W, G, HW, ST>), grid, dim3(64 * W * G),
+                         0, s, a, ds, dq, ld_d);
+    });
+  };
+  const long small = packed_blocks<2>(a, p);
+  if (p.max_seq > 64 && (small <= 528 || (small <= 768 && packed_one(p))))
+    dq_pass(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{});
+  else if (length <= 1024 || packed_blocks<8>(a, p) <= 256)
+    dq_pass(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  else
+    dq_pass(integral_constant<int, 8>{}, integral_constant<int, 1>{}, integral_constant<int, 3>{});
   return hipGetLastError();
+}
+template <int D, int NW, int KG>
+void attn_packed_fwd_n(const AttnPackedArgs& a, const PackedPlan& p, uint16_t* o, float* lse,
+                       hipStream_t s) {
+  packed_heads<NW>(a, [&](auto heads) {
+    constexpr int HW = decltype(heads)::value;
+    const dim3 grid((unsigned)packed_blocks<NW>(a, p)), block(64 * NW * KG);
+    hipLaunchKernelGGL((attn_fwd_k<D, AttnPackedArgs, NW, KG, HW>), grid, block, 0, s, a, o, lse);
+  });
 }
 template <int D>
 hipError_t attn_packed_fwd_d(const AttnPackedArgs& a, const PackedPlan& p, uint16_t* o, float* lse,
                              hipStream_t s) {
-  packed_heads(a, [&](auto heads) {
-    constexpr int HW = decltype(heads)::value;
-    const dim3 grid((unsigned)(p.cap[packed_kind(128 / HW)] * (a.n_heads / HW)));
-    hipLaunchKernelGGL((attn_fwd_k<D, AttnPackedArgs, 4, 1, HW>), grid, dim3(256), 0, s, a, o,
-                       lse);
-  });
+  // Few blocks: of 64 (row, head) pairs, their key tiles in two groups of waves. 611 rows in 4
+  // documents, 12/4 heads of 64 10.0 us as blocks of 128, so 7.0; 4096 rows, 8/8 heads 62.2, 36.3,
+  // 32/8 92.5, 99.9. Heads of 128: 2048 rows, 8/8 heads 40.4, 27.0; 4096 of one 75.8, 55.6, of four
+  // 23.9, 29.2; and in blocks of 128 with two groups (one on a CU): 4096 rows, 12/4 81.2, 71.4.
+  const long small = packed_blocks<2>(a, p), large = packed_blocks<4>(a, p);
+  if (p.max_seq > 64 && small <= (D == 64 ? 1024 : packed_one(p) ? 512 : 288)) {
+    attn_packed_fwd_n<D, 2, 2>(a, p, o, lse, s);
+  } else if (D == 128 && large <= (packed_one(p) ? 512 : 256) && most_tiles(p) >= 8) {
+    attn_packed_fwd_n<128, 4, 2>(a, p, o, lse, s);
+  } else {
+    attn_packed_fwd_n<D, 4, 1>(a, p, o, lse, s);
+  }
   return hipGetLastError();
 }
 }  // namespace

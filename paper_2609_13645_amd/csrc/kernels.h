@@ -318,6 +318,9 @@ struct AttnPackedArgs : AttnArgs {
   const PackedTile* tiles[kPackedKinds];
   int n_seqs, max_seq;
   long ds_head;                          // elements of a head's dS
+  // the forward's outputs
+  const uint16_t* o = nullptr;
+  const float* lse = nullptr;
 };
 // pos (may be NULL): every token's place in its sequence.
 hipError_t attn_packed_plan(const PackedPlan& p, const int32_t* offsets, void* plan, int32_t* pos,

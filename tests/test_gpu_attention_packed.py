@@ -48,6 +48,16 @@ CASES = [
     # (many of four waves)
     ([2500, 60, 900, 40], 2, 3, 16, 8, 64, 0),
     ([1300, 60, 900, 40], 0, 0, 16, 16, 128, 0),
+    # (one long sequence: blocks of 128 whose key tiles are in two groups, for every group of heads)
+    ([1500, 700, 300], 0, 1, 16, 4, 128, 0),
+    ([3500, 700], 0, 0, 8, 4, 128, 0),
+    ([3500, 700], 2, 0, 9, 3, 128, 0),
+    # (and dQ blocks of 256)
+    ([1500, 1300], 0, 0, 32, 8, 128, 0),
+    ([2500, 900, 700], 0, 0, 16, 8, 128, 0),
+    ([1300, 1100], 0, 5, 36, 12, 128, 0),
+    ([1500, 1300], 3, 0, 32, 8, 64, 0),
+    ([2500, 900, 700], 0, 0, 16, 8, 64, 0),
 ]
 
 
