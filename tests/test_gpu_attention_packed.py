@@ -265,6 +265,34 @@ def test_what_is_not_finite_stays_in_its_sequence(where, bad, d, W):
         assert same[0][70:150].all() and same[1][:, 70:150].all()
 
 
+@pytest.mark.parametrize("nh,nkv,d", [(32, 8, 64), (64, 16, 64), (32, 8, 128)])
+def test_what_is_not_finite_among_many_sequences(nh, nkv, d):
+    """The same where blocks are many: each of four sequences has a NaN somewhere, the others
+    keep their bits, and of the four every kv head's group but the first."""
+    import torch
+    banner(f"packed NaN among many {nh}/{nkv}x{d}")
+    lens = [70, 130, 200, 1, 60] * 20
+    off = offsets_of(lens, 0)
+    T, hq = int(off[-1]), nh * d
+    qkv = torch.randn((T, (nh + 2 * nkv) * d), device="cuda").to(torch.bfloat16)
+    do = torch.randn((T, hq), device="cuda").to(torch.bfloat16)
+    clean = Call(off, T, 200, nh, nkv, d, 0, qkv.clone(), do.clone(), fill=0.0).run()
+    others = np.ones(T, bool)
+    for i, (buf, col) in enumerate([(qkv, 0), (qkv, hq), (qkv, hq + nkv * d), (do, 0)]):
+        s = 5 * i + 1                               # of 130 tokens
+        buf[int(off[s]) + 80, col + 3] = float("nan")
+        others[off[s]:off[s + 1]] = False
+    c = Call(off, T, 200, nh, nkv, d, 0, qkv, do, fill=0.0).run()
+    torch.cuda.synchronize()
+    o, lse, g = [(a == b).cpu().numpy() for a, b in zip(c.results(), clean.results())]
+    assert o[others].all() and lse[:, others].all() and g[others].all()
+    grp = nh // nkv
+    assert o[:, grp * d:].all() and lse[grp:].all()
+    g = g.reshape(T, nh + 2 * nkv, d)
+    assert g[:, grp:nh].all() and g[:, nh + 1:nh + nkv].all() and g[:, nh + nkv + 1:].all()
+    assert not o.all() and not g.all()
+
+
 def test_a_plan_of_other_sizes_writes_nothing():
     import torch
     banner("packed plan of other sizes")
