@@ -2329,7 +2329,7 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
                          a.n_heads, a.seq);
     }
     const dim3 grid((unsigned)(p.cap[1] * a.n_kv_heads * (2 / KB)));
-    hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, KB == 1, STATS, NW, KB>), grid,
+    hipLaunchKernelGGL((attn_bwd_kv_k<D, AttnPackedArgs, KB == 1 && NW >= 4, STATS, NW, KB>), grid,
                        dim3(64 * NW), 0, s, a, dout, delta, ds, dv, dk, ld_d,
                        static_cast<float*>(nullptr), static_cast<float*>(nullptr), 1);
   };
@@ -2352,21 +2352,23 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   // launch fewer: one row, 4/2 heads of 64 10.1 us, so 8.0; 257 rows in three, 8/8 heads 12.6,
   // 11.5. (Heads of 128, two pairs to a wave 16.8, 17.9.)
   const bool stats = longest <= (D == 64 ? 8 : 4);
-  // Many, heads of 64: blocks of one or two waves, four or two on a CU, whose starts and ends
-  // the others cover, while the longest block still ends in time: 512 documents of 32 tokens,
-  // 32/8 heads 95 us in blocks of four waves, 61 of two, 51 of one; 64 of 256 111, 94, 83; 32
-  // of 512 168, 125, 126; 4 of 4096 714, 701, 739; 41 documents of 7 to 1605, mean 400, the
-  // backward 365, 351, 409. (Heads of 128: two waves and the V and K tiles take 91 KB.)
+  // Many: blocks of one or two waves, four or two on a CU, whose starts and ends the others
+  // cover, while the longest block still ends in time: 512 documents of 32 tokens, 32/8 heads
+  // of 64 95 us in blocks of four waves, 61 of two, 51 of one; 64 of 256 111, 94, 83; 32 of 512
+  // 168, 125, 126; 4 of 4096 714, 701, 739; 41 documents of 7 to 1605, mean 400, the backward
+  // 365, 351, 409. Heads of 128 (two on a CU, their LDS): halves of one wave, 161 us in blocks
+  // of four, so 107; 203, 192; 282, 263; 16 of 1024 382, 424; of two waves 144, 200, 308, 458.
   constexpr integral_constant<int, 4> four{};
   constexpr integral_constant<int, D == 64 ? 8 : 4> most{};
   constexpr integral_constant<int, D == 64 ? 2 : 4> two{};
-  constexpr integral_constant<int, D == 64 ? 1 : 4> one{};
+  constexpr integral_constant<int, 1> one{};
   constexpr integral_constant<int, 1> half{};
   constexpr integral_constant<int, 2> whole{};
+  constexpr integral_constant<int, D == 64 ? 2 : 1> of_one{};
   if (halves && stats) kv_pass(four, half, std::true_type{});
   else if (halves && eight) kv_pass(most, half, false_type{});
   else if (halves) kv_pass(four, half, false_type{});
-  else if (D == 64 && 1.2 * longest <= share) kv_pass(one, whole, false_type{});
+  else if (1.2 * longest <= share) kv_pass(one, of_one, false_type{});
   else if (D == 64 && 0.55 * longest <= share) kv_pass(two, whole, false_type{});
   else kv_pass(four, whole, false_type{});
   // dQ. Few blocks: of 64 (row, head) pairs, their key tiles in two groups (the backward of

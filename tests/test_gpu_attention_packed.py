@@ -45,6 +45,8 @@ CASES = [
     ([130, 200, 64, 5, 90] * 8, 0, 2, 48, 24, 64, 40),
     ([5, 40, 1, 90, 0, 33, 70] * 15, 0, 5, 64, 16, 64, 0),
     ([130, 200, 64, 5, 90] * 8, 1, 0, 64, 32, 64, 40),
+    ([5, 40, 1, 90, 0, 33, 70] * 15, 0, 5, 64, 16, 128, 0),
+    ([130, 200, 64, 5, 90] * 8, 1, 0, 64, 32, 128, 40),
     # (many of four waves)
     ([2500, 60, 900, 40], 2, 3, 16, 8, 64, 0),
     ([1300, 60, 900, 40], 0, 0, 16, 16, 128, 0),
