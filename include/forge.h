@@ -915,6 +915,8 @@ forge_status forge_attention_window_bwd(const forge_attn_window_cfg* cfg, const 
  * their rows of every output are left as they were. Offsets are taken as their running
  * maximum and cut to [0, tokens]; of a sequence longer than max_seq the first
  * max_seq rows are taken, the others belong to none.
+ * Blocks are chosen by tokens, n_seqs and max_seq, not by the lengths: bounds near
+ * them (max_seq the longest's length) are the faster ones, any are right.
  * Rules: n_heads a multiple of n_kv_heads, head_dim 64 or 128; 1 <= tokens, 1 <=
  * max_seq (values beyond tokens are as tokens), 1 <= n_seqs, window >= 0 (else
  * INVALID_ARG); tokens <= 2^22, n_seqs <= 2^22, n_heads * tokens <= 2^27,

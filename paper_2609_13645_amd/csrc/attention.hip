@@ -2292,24 +2292,38 @@ void packed_heads(const AttnPackedArgs& a, F&& f) {
   if (grp % 2 == 0) f(std::integral_constant<int, 2>{});
   else f(std::integral_constant<int, 1>{});
 }
-// Blocks of so many waves, a query head's 32 rows each.
-template <int WAVES>
-long packed_blocks(const AttnPackedArgs& a, const PackedPlan& p) {
-  long n = 0;
-  packed_heads<WAVES>(a, [&](auto heads) {
-    constexpr int HW = decltype(heads)::value;
-    n = (long)p.cap[packed_kind(32 * WAVES / HW)] * (a.n_heads / HW);
-  });
-  return n;
-}
 // Key tiles that a sequence's last block has.
 int most_tiles(const PackedPlan& p) { return (std::min(p.max_seq, p.window) + 63) / 64; }
 // The length of the sequences that most tokens are in, taken to be of a geometric law where
-// they differ; whether one sequence has most tokens, whose tiles are of all sizes.
+// they differ; and whether one sequence has most tokens (a max_seq below the tokens is taken
+// to be the longest's length) and tiles of all sizes: those of the others are then as good as
+// none (6045 tokens in 67 documents, 4533 of them in one, 6/2 heads of 128: forward 84.0 us by
+// all tiles, by the long one's 64.7, backward 249.9, 158.3; with a window of 25 11.4, 20.4).
 long packed_length(const PackedPlan& p) {
   return std::min<long>(p.max_seq, std::max(2L * p.tokens / p.n_seqs, 1L));
 }
-bool packed_one(const PackedPlan& p) { return 2 * packed_length(p) > p.tokens; }
+bool packed_one(const PackedPlan& p) {
+  return 2L * (p.max_seq < p.tokens ? p.max_seq : packed_length(p)) > p.tokens &&
+         2L * p.window > p.max_seq;
+}
+// Tiles of a list that do most of the work.
+long packed_tiles(const PackedPlan& p, int kind) {
+  const int rows = packed_rows(kind);
+  return packed_one(p) ? (p.max_seq + rows - 1) / rows : p.cap[kind];
+}
+// Blocks of so many waves, a query head's 32 rows each: in the launch, and those that do most
+// of the work.
+template <int WAVES>
+struct PackedBlocks {
+  long all = 0, busy = 0;
+  PackedBlocks(const AttnPackedArgs& a, const PackedPlan& p) {
+    packed_heads<WAVES>(a, [&](auto heads) {
+      constexpr int HW = decltype(heads)::value, KIND = packed_kind(32 * WAVES / HW);
+      all = (long)p.cap[KIND] * (a.n_heads / HW);
+      busy = packed_tiles(p, KIND) * (a.n_heads / HW);
+    });
+  }
+};
 
 template <int D>
 hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16_t* o,
@@ -2339,7 +2353,7 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   const double share = (double)p.cap[1] * a.n_heads / 1024 *
                        std::min<long>(length / 64 + 1, p.window / 32 + 1);
   const double longest = grp * std::min((p.max_seq + 31) / 32, (62 + p.window) / 32 + 1);
-  const long blocks = (long)p.cap[1] * a.n_kv_heads;
+  const long blocks = packed_tiles(p, 1) * a.n_kv_heads;
   // Few key tiles: a block for each half of one, on a CU that would idle (heads of 64: two on
   // a CU), of eight waves where they have pairs enough and LDS holds their buffers. The backward
   // of 8/2 heads of 128: 611 rows in 4 documents 37.2 us in blocks of 64 keys, so 28.7; 2048
@@ -2383,15 +2397,15 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
     constexpr int ST = decltype(stages)::value;
     packed_heads<W>(a, [&](auto heads) {
       constexpr int HW = decltype(heads)::value;
-      const dim3 grid((unsigned)packed_blocks<W>(a, p));
+      const dim3 grid((unsigned)PackedBlocks<W>(a, p).all);
       hipLaunchKernelGGL((attn_bwd_dq_k<D, AttnPackedArgs, W, G, HW, ST>), grid, dim3(64 * W * G),
                          0, s, a, ds, dq, ld_d);
     });
   };
-  const long small = packed_blocks<2>(a, p);
+  const long small = PackedBlocks<2>(a, p).busy;
   if (p.max_seq > 64 && (small <= 528 || (small <= 768 && packed_one(p))))
     dq_pass(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{});
-  else if (length <= 1024 || packed_blocks<8>(a, p) <= 256)
+  else if (length <= 1024 || PackedBlocks<8>(a, p).busy <= 256)
     dq_pass(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
   else
     dq_pass(integral_constant<int, 8>{}, integral_constant<int, 1>{}, integral_constant<int, 3>{});
@@ -2402,7 +2416,7 @@ void attn_packed_fwd_n(const AttnPackedArgs& a, const PackedPlan& p, uint16_t* o
                        hipStream_t s) {
   packed_heads<NW>(a, [&](auto heads) {
     constexpr int HW = decltype(heads)::value;
-    const dim3 grid((unsigned)packed_blocks<NW>(a, p)), block(64 * NW * KG);
+    const dim3 grid((unsigned)PackedBlocks<NW>(a, p).all), block(64 * NW * KG);
     hipLaunchKernelGGL((attn_fwd_k<D, AttnPackedArgs, NW, KG, HW>), grid, block, 0, s, a, o, lse);
   });
 }
@@ -2413,7 +2427,7 @@ hipError_t attn_packed_fwd_d(const AttnPackedArgs& a, const PackedPlan& p, uint1
   // documents, 12/4 heads of 64 10.0 us as blocks of 128, so 7.0; 4096 rows, 8/8 heads 62.2, 36.3,
   // 32/8 92.5, 99.9. Heads of 128: 2048 rows, 8/8 heads 40.4, 27.0; 4096 of one 75.8, 55.6, of four
   // 23.9, 29.2; and in blocks of 128 with two groups (one on a CU): 4096 rows, 12/4 81.2, 71.4.
-  const long small = packed_blocks<2>(a, p), large = packed_blocks<4>(a, p);
+  const long small = PackedBlocks<2>(a, p).busy, large = PackedBlocks<4>(a, p).busy;
   if (p.max_seq > 64 && small <= (D == 64 ? 1024 : packed_one(p) ? 512 : 288)) {
     attn_packed_fwd_n<D, 2, 2>(a, p, o, lse, s);
   } else if (D == 128 && large <= (packed_one(p) ? 512 : 256) && most_tiles(p) >= 8) {

@@ -60,6 +60,15 @@ CASES = [
     ([1300, 1100], 0, 5, 36, 12, 128, 0),
     ([1500, 1300], 3, 0, 32, 8, 64, 0),
     ([2500, 900, 700], 0, 0, 16, 8, 64, 0),
+    # (the same of sequences alike; a long one among many; and within a window)
+    ([1300] * 3, 0, 0, 32, 8, 128, 0),
+    ([1290, 1300, 1300], 1, 0, 16, 8, 128, 0),
+    ([1300] * 3, 0, 2, 36, 12, 128, 0),
+    ([1300] * 3, 0, 0, 32, 8, 64, 0),
+    ([1300] * 3, 0, 0, 16, 8, 64, 0),
+    ([400] * 9, 0, 0, 24, 8, 128, 0),
+    ([40, 3, 61] * 12 + [2100] + [17, 29] * 5, 0, 0, 6, 2, 128, 0),
+    ([40, 3, 61] * 12 + [2100] + [17, 29] * 5, 0, 0, 16, 8, 128, 25),
 ]
 
 
