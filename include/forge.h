@@ -921,7 +921,10 @@ forge_status forge_attention_window_bwd(const forge_attn_window_cfg* cfg, const 
  * max_seq (values beyond tokens are as tokens), 1 <= n_seqs, window >= 0 (else
  * INVALID_ARG); tokens <= 2^22, n_seqs <= 2^22, n_heads * tokens <= 2^27,
  * n_heads * (tokens / 64 + n_seqs) < 2^23, (n_heads + 2 n_kv_heads) * head_dim <=
- * 2^22 (else UNSUPPORTED).
+ * 2^22 (else UNSUPPORTED). And a head's score gradient, at the lengths that make it
+ * largest, below 2^31 blocks of 64 keys x 32 queries: one row of 2965760 tokens as one
+ * sequence, any with max_seq <= 2^20 or window <= 2^14 (else UNSUPPORTED, by every call,
+ * so that what has a forward has a backward).
  */
 typedef struct {
   int32_t tokens, n_seqs, max_seq, n_heads, n_kv_heads, head_dim;

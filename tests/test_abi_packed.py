@@ -267,3 +267,24 @@ def test_packed_workspace_holds_whatever_the_lengths(tokens, n_seqs, max_seq, wi
     full = -(-m // 64)
     assert got <= 8 * heads * tokens + 4096 * heads * tiles * (_blocks(full * 64, w) // full + 1) \
         + 1024 + (64 << 20)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(tokens=1 << 21, max_seq=1 << 21, n_seqs=1 << 16),
+    dict(tokens=92680 * 32, max_seq=92680 * 32, n_seqs=1),
+    dict(tokens=1 << 22, max_seq=1 << 20, n_seqs=1 << 16),
+    dict(tokens=1 << 22, max_seq=1 << 22, n_seqs=1 << 16, window=1 << 14)])
+def test_long_rows_whose_score_gradient_can_be_addressed(kw):
+    """s slabs of 32 queries make (s + 1)^2 / 4 blocks of 64 keys, below 2^31 up to 92680 slabs;
+    shorter sequences, however many, make fewer in the same rows."""
+    assert status(_lib.forge_attention_packed_plan_bytes, pcfg(**kw)) == OK
+    assert status(_lib.forge_attention_packed_bwd_workspace_bytes, pcfg(**kw)) == OK
+
+
+def test_rows_whose_score_gradient_can_not_be_addressed():
+    """By every call: what has a forward has a backward."""
+    for kw in (dict(tokens=92680 * 32 + 1, max_seq=92680 * 32 + 1, n_seqs=1),
+               dict(tokens=1 << 22, max_seq=1 << 21, n_seqs=2)):
+        assert status(_lib.forge_attention_packed_plan_bytes, pcfg(**kw)) == UNSUPPORTED
+        assert status(_lib.forge_attention_packed_bwd_workspace_bytes, pcfg(**kw)) == UNSUPPORTED
+        assert status(_lib.forge_attention_packed_fwd, pcfg(**kw), P, X, Y, C, 0) == UNSUPPORTED
