@@ -960,8 +960,9 @@ forge_status forge_attention_packed_fwd(const forge_attn_packed_cfg* cfg, const 
 
 /* Scratch bytes of forge_attention_packed_bwd: per-query statistics, and the score
  * gradient in bf16, of each head 4 KB for every 64 keys x 32 queries that see
- * each other, at most: of full sequences of max_seq (or the window's band of
- * them). Host only. */
+ * each other, at the lengths that make them most: of as many sequences of max_seq as
+ * fit and one of the rest (or the window's band of them), and 4 KB a sequence. It
+ * grows with tokens * max_seq, so a near max_seq saves memory. Host only. */
 forge_status forge_attention_packed_bwd_workspace_bytes(const forge_attn_packed_cfg* cfg,
                                                         size_t* bytes);
 

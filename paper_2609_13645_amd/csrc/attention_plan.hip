@@ -181,16 +181,17 @@ __global__ __launch_bounds__(64) void packed_positions_k(PackedPlan p, const cha
 // Blocks of dS of a head that n sequences of at most max_seq rows can come to in `tokens` rows.
 // One of s slabs of 32 queries has f(s) blocks and 32 (s - 1) + 1 rows or more. f(s + 1) - f(s)
 // does not fall with s where a window's keys are seen by an even number of slabs (else one more
-// is taken), so the most come of as many sequences of max_seq as fit, one of the slabs that
-// are left, and a block for each of the others.
+// is taken): a slab of a shorter sequence is worth no less in a longer one. So the most come of
+// as many sequences of max_seq as fit, one of the slabs that are left, and a block for each
+// of the others.
 static long most_ds_blocks(int tokens, long n, int max_seq, int window) {
   const int even = (62 + window) / 32 % 2 ? window : window + 32;
   const auto more = [&](long slabs) {   // f(slabs + 1) - f(1)
     return DsPacked((int)(32 * (slabs + 1)), even, 0, 0).blocks() - 1;
   };
-  const long slabs = (tokens - 1) / 32, each = (max_seq - 1) / 32;   // beyond the first of each
-  const long full = each > 0 ? std::min(n, slabs / each) : 0;
-  const long rest = full < n && each > 0 ? slabs - full * each : 0;
+  const long each = (max_seq - 1) / 32;   // slabs beyond the first
+  const long full = std::min(n, tokens / (32 * each + 1)), rows = tokens - full * (32 * each + 1);
+  const long rest = full < n && rows > 0 ? (rows - 1) / 32 : 0;
   return n + full * more(each) + more(rest);
 }
 
@@ -208,12 +209,11 @@ PackedPlan::PackedPlan(int tokens_, int n_seqs_, int max_seq_, int window_)
     bins[k] = order[k] + up((size_t)n * sizeof(PackedTile));
     bytes = bins[k] + up((size_t)(nt + 1) * 8);
   }
-  // a tile has on average no more blocks than one of a sequence of max_seq, whose later
-  // tiles the end cuts least
+  // (nor more than those of every tile at the average of a sequence of max_seq, whose later
+  // tiles the end cuts least)
   const long nt = (max_seq + 63) / 64;
   const long full = DsPacked((int)(nt * 64), window, 0, 0).blocks();
-  ds_blocks = cap[1] * ((full + nt - 1) / nt);
-  ds_most = most_ds_blocks(tokens, n, max_seq, window);
+  ds_blocks = std::min(most_ds_blocks(tokens, n, max_seq, window), cap[1] * ((full + nt - 1) / nt));
 }
 
 hipError_t attn_packed_plan(const PackedPlan& p, const int32_t* offsets, void* plan, int32_t* pos,

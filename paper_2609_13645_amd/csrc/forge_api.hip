@@ -2227,7 +2227,7 @@ forge_status check_attn_packed(const forge_attn_packed_cfg* c) {
   FORGE_CHECK(((int64_t)c->tokens / 64 + c->n_seqs) * c->n_heads < (1 << 23),
               FORGE_ERR_UNSUPPORTED, "n_heads * (tokens / 64 + n_seqs) exceeds 2^23");
   const forge::PackedPlan p(c->tokens, c->n_seqs, c->max_seq, c->window);
-  FORGE_CHECK(p.ds_most < 1LL << 31, FORGE_ERR_UNSUPPORTED,
+  FORGE_CHECK(p.ds_blocks < 1LL << 31, FORGE_ERR_UNSUPPORTED,
               "a head's score gradient exceeds 2^31 blocks");
   return FORGE_OK;
 }

@@ -308,8 +308,7 @@ struct PackedPlan {
   int cap[kPackedKinds];                 // entries of each list
   // bytes: where the lists lie, the sequences by their tiles, and how many have them
   size_t tiles[kPackedKinds], order[kPackedKinds], bins[kPackedKinds], bytes;
-  long ds_blocks;                        // blocks of dS of a head that there is room for
-  long ds_most;                          // those that the sequences can come to
+  long ds_blocks;                        // blocks of dS of a head, at most
   __host__ PackedPlan(int tokens_, int n_seqs_, int max_seq_, int window_);
 };
 // batch 1, seq the tokens of the packed row.

@@ -288,3 +288,44 @@ def test_rows_whose_score_gradient_can_not_be_addressed():
         assert status(_lib.forge_attention_packed_plan_bytes, pcfg(**kw)) == UNSUPPORTED
         assert status(_lib.forge_attention_packed_bwd_workspace_bytes, pcfg(**kw)) == UNSUPPORTED
         assert status(_lib.forge_attention_packed_fwd, pcfg(**kw), P, X, Y, C, 0) == UNSUPPORTED
+
+
+def _worst(tokens, n_seqs, max_seq, window):
+    """Most blocks of a head that any lengths come to: a knapsack of sequences by their slabs,
+    each with the fewest rows that it can have."""
+    sizes = [(32 * s + 1, _blocks(32 * s + 1, window)) for s in range(1, -(-max_seq // 32))]
+    # (sequences of one slab last: one row and one block each)
+    best = {0: {0: 0}}                               # sequences -> rows -> blocks
+    for n in range(1, n_seqs + 1):
+        best[n] = {}
+        for rows, blocks in best[n - 1].items():
+            for r, b in sizes:
+                if rows + r <= tokens:
+                    best[n][rows + r] = max(best[n].get(rows + r, 0), blocks + b)
+    return max(b + min(n_seqs - n, tokens - rows) for n in best for rows, b in best[n].items())
+
+
+def _room(cfg):
+    got = _lib.forge_attention_packed_bwd_workspace_bytes(cfg)
+    up = lambda n: -(-n // 256) * 256
+    return (got - up(8 * cfg.n_heads * cfg.tokens)) // (4096 * cfg.n_heads)
+
+
+@pytest.mark.parametrize("window", [0, 1, 3, 40, 100, 130, 260])
+@pytest.mark.parametrize("tokens,n_seqs,max_seq", [
+    (1, 1, 1), (33, 4, 33), (97, 3, 64), (300, 1, 300), (300, 5, 299), (321, 2, 200), (321, 9, 33),
+    (640, 6, 640), (640, 4, 129), (700, 3, 320), (700, 7, 97), (500, 40, 32)])
+def test_packed_workspace_is_that_of_the_worst_lengths(tokens, n_seqs, max_seq, window):
+    """Not below them, and above by a block for each sequence at most, times (k + 1) / k where
+    a window's keys are seen by an odd number of slabs k, of which one more is counted."""
+    room = _room(_lib.AttnPackedCfg(tokens, n_seqs, max_seq, 4, 2, 64, window))
+    worst = _worst(tokens, n_seqs, min(max_seq, tokens), window or tokens)
+    k = (62 + (window or tokens)) // 32 + 1
+    assert worst <= room <= (worst * (k + k % 2)) / k + n_seqs
+
+
+@pytest.mark.parametrize("n_seqs", [1, 41, 1024, 4096])
+def test_packed_workspace_of_loose_bounds(n_seqs):
+    """Many sequences and max_seq = tokens: splitting a row only lowers what it takes."""
+    assert _room(_lib.AttnPackedCfg(16384, n_seqs, 16384, 32, 8, 128, 0)) <= \
+        _blocks(16384, 16384) + n_seqs

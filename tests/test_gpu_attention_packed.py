@@ -450,3 +450,28 @@ def test_plans_of_every_size(more, longest):
         lse = c.lse[0].cpu().numpy()
         assert np.all(lse[~inside] == -9.0)
         assert np.max(np.abs(lse[inside] - np.log(pos[inside] + 1.0))) <= 1e-5
+
+
+@pytest.mark.parametrize("lens,n_seqs,max_seq,nh,nkv,d,W", [
+    ([641], 1, 641, 4, 2, 64, 0), ([33] * 5 + [1, 1], 7, 33, 4, 2, 64, 0),
+    ([1] * 7, 7, 1, 4, 1, 128, 0), ([320, 320, 58, 1, 1], 5, 320, 8, 2, 128, 0),
+    ([1500], 1, 1500, 4, 2, 128, 66), ([2100, 2100, 33], 3, 2100, 16, 8, 64, 0)])
+def test_workspace_at_the_lengths_that_need_most(lens, n_seqs, max_seq, nh, nkv, d, W):
+    """... or all but a block for each sequence: nothing is written behind it, and the gradients
+    are those that a workspace with room behind gives."""
+    import torch
+    banner(f"packed workspace {lens[:5]} d={d} W={W}")
+    off = offsets_of(lens, 0)
+    T = int(off[-1])
+    qkv = torch.randn((T, (nh + 2 * nkv) * d), device="cuda").to(torch.bfloat16)
+    do = torch.randn((T, nh * d), device="cuda").to(torch.bfloat16)
+    c = Call(off, T, max_seq, nh, nkv, d, W, qkv, do, fill=3.0).run()
+    want = c.dqkv.clone()
+    n = c.ws.numel()
+    room = torch.full((n + 65536,), 5.0, device="cuda")
+    c.ws = room[:n]
+    c.dqkv.fill_(3.0)
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(c.dqkv, want) and not bool(want.isnan().any())
+    assert bool((room[n:] == 5.0).all())
