@@ -617,13 +617,17 @@ typedef struct {
 
 /* Elements that share a scale (state_bits 8). */
 #define FORGE_ADAMW_BLOCK 256
+/* The smallest eps with state_bits 8: 2^-40. A block of v below 2^-94 is kept as zeros while
+ * its m, about the root of it, is kept: eps then stands in for a root below 2^-47 (below
+ * 2^-40 with a bias correction of 2^-14), and the step stays as small as it was. */
+#define FORGE_ADAMW_MIN_EPS_8BIT 9.094947017729282e-13f
 
 /*
  * tensors: host array [n_tensors], read during the call (a captured graph keeps
  * the pointers). Every buffer that is written has to be a tensor's own. n may be
  * 0 (the tensor is skipped, its pointers may be NULL); n <= 2^33 each, n_tensors
  * <= 2^20 (else UNSUPPORTED). hp, dev_scalars: as in forge_adamw_step. state_bits other than 8 and
- * 32: INVALID_ARG.
+ * 32, or 8 with hp->eps < FORGE_ADAMW_MIN_EPS_8BIT: INVALID_ARG.
  */
 forge_status forge_adamw_multi_step(const forge_adamw_multi_tensor* tensors, int32_t n_tensors,
                                     int32_t state_bits, int32_t grad_bf16,

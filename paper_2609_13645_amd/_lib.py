@@ -86,6 +86,7 @@ class AdamwMultiTensor(ctypes.Structure):
 
 
 ADAMW_BLOCK = 256      # elements that share a scale (moments in 8 bits)
+ADAMW_MIN_EPS_8BIT = 2.0 ** -40
 
 
 class LayerOptim(ctypes.Structure):

@@ -21,7 +21,9 @@ namespace forge {
 namespace {
 
 constexpr int kBlock = 256;             // elements that share a scale
-constexpr float kTiny = 0x1p-94f;       // blocks below are kept as zeros (255^4 / kTiny is finite)
+// Blocks below are kept as zeros (255^4 / kTiny is finite); eps, FORGE_ADAMW_MIN_EPS_8BIT at
+// least, stands in for the roots of such a v.
+constexpr float kTiny = 0x1p-94f;
 
 __host__ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
   x = (x ^ (x >> 16)) * 0xE699D49Du;

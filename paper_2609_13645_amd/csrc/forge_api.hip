@@ -1801,6 +1801,8 @@ forge_status forge_adamw_multi_step(const forge_adamw_multi_tensor* tensors, int
   FORGE_CHECK(state_bits == 8 || state_bits == 32, FORGE_ERR_INVALID_ARG,
               "state_bits must be 8 or 32 (got %d)", state_bits);
   if (forge_status e = check_hparams(hp)) return e;
+  FORGE_CHECK(state_bits != 8 || hp->eps >= FORGE_ADAMW_MIN_EPS_8BIT, FORGE_ERR_INVALID_ARG,
+              "state_bits 8 needs eps >= 2^-40 (got %g)", (double)hp->eps);
   if (forge_status e = check_adamw_list(tensors, n_tensors)) return e;
   bool any = false;
   for (int i = 0; i < n_tensors; ++i) {

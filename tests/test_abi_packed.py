@@ -329,3 +329,21 @@ def test_packed_workspace_of_loose_bounds(n_seqs):
     """Many sequences and max_seq = tokens: splitting a row only lowers what it takes."""
     assert _room(_lib.AttnPackedCfg(16384, n_seqs, 16384, 32, 8, 128, 0)) <= \
         _blocks(16384, 16384) + n_seqs
+
+
+def test_adamw_multi_8_bits_need_an_eps_above_the_roots_that_are_lost():
+    """A v below 2^-94 is kept as zero: 2^-40 or more has to stand in for its root."""
+    least = 2.0 ** -40
+    assert _lib.ADAMW_MIN_EPS_8BIT == least
+    for eps in (0.0, 1e-30, 1e-15, least * (1 - 2.0 ** -23)):
+        hp = _lib.AdamwHparams(0.9, 0.95, eps, 0.1)
+        assert step([T8], hp=hp) == INVALID and step([], hp=hp) == INVALID
+        assert step([], 32, hp=hp) == OK
+    for eps in (least, 1e-12, 1e-8):
+        assert step([], hp=_lib.AdamwHparams(0.9, 0.95, eps, 0.1)) == OK
+
+
+def test_adamw_min_eps_matches_the_c_header(tmp_path):
+    """(as 2^60 times it: layout prints integers)"""
+    got = layout(tmp_path, {}, ["(FORGE_ADAMW_MIN_EPS_8BIT * 1152921504606846976.0)"])
+    assert got == [_lib.ADAMW_MIN_EPS_8BIT * 2.0 ** 60]

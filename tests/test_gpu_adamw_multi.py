@@ -306,3 +306,45 @@ def test_drawn_codes_follow_a_falling_gradient():
     keep = fall < 1
     ratio = (v[keep].double() / a["v"][keep].double()).mean().item()
     assert abs(ratio - 1) <= 0.12, ratio
+
+
+@pytest.mark.parametrize("beta2", [0.95, 0.999])
+def test_moments_whose_v_is_lost(beta2):
+    """Gradients below 2^-47, then none, with the smallest eps that 8 bits take: v of the first
+    step, (1 - beta2) 2^-94 at most, is kept as zero, m is not. The second update is m' / eps where
+    the 32-bit one is m / (r + eps), r = sqrt(v') below 2^-47 (bias-corrected: (beta2 (1 - beta2) /
+    (1 - beta2^2))^(1/2) |g|, below 0.71 2^-47). So they differ by r / eps of themselves, below
+    0.71 2^-7, and by m' - m, half a code at most: (2 * 127 + 1) / 2 / 127^2 of the largest |m|. Both steps
+    also by the hardware's root and quotient, below 2^-20. With m-hat = 0.9 * 0.1 / 0.19 |g| below
+    0.474 2^-47, and a first update below 2^-47 / 2^-40."""
+    import torch
+    from paper_2609_13645_amd import _lib
+    banner(f"adamw multi lost v beta2={beta2}")
+    n, lr, eps = 3000, 1.0, _lib.ADAMW_MIN_EPS_8BIT
+    hp = _lib.AdamwHparams(0.9, beta2, eps, 0.0)
+    rng = np.random.default_rng(9)
+    g = (2.0 ** -47 * (0.5 + 0.49 * rng.random(n)) * rng.choice([-1, 1], n)).astype(np.float32)
+    z = lambda dt, k=n: torch.zeros(k, dtype=dt, device="cuda")
+    f = torch.float32
+    runs = {}
+    for bits in (32, 8):
+        t = dict(master=z(f), param=z(torch.bfloat16), grad=torch.from_numpy(g).cuda())
+        blocks = -(-n // _lib.ADAMW_BLOCK)
+        t.update(dict(m=z(f), v=z(f)) if bits == 32 else dict(
+            m=z(torch.int8), v=z(torch.uint8), m_scale=z(f, blocks), v_scale=z(f, blocks)))
+        sc, step = torch.tensor([lr, 1, 1, 1.0], device="cuda"), z(torch.int32, 1)
+        lst = _lib.adamw_multi_tensors([t])
+        for k in range(2):
+            _lib.forge_adamw_advance(sc, step, lr, 0.9, beta2)
+            _lib.forge_adamw_multi_step(lst, bits, False, hp, sc)
+            torch.cuda.synchronize()
+            if bits == 8:
+                assert not bool(t["v"].any()) and not bool(t["v_scale"].any())
+                assert bool((t["m"] != 0).all()) and bool((t["m_scale"] > 0).all())
+            t["grad"].zero_()
+        runs[bits] = t["master"].double().cpu().numpy()
+    assert np.isfinite(runs[8]).all()
+    second = 0.474 * 2.0 ** -7
+    bound = lr * (second * (0.71 * 2.0 ** -7 + 255 / 2 / 127.0 ** 2) + 2 * 2.0 ** -7 * 2.0 ** -20)
+    # (the new masters, below 2^-6, are rounded to 2^-24 of themselves, twice)
+    assert np.max(np.abs(runs[8] - runs[32])) <= bound + 2 * 2.0 ** -30
