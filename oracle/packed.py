@@ -124,7 +124,7 @@ def encode_v(v, u):
     q = np.floor(np.sqrt(np.sqrt(x)))
     lo, hi = (q * q) * (q * q), ((q + F32(1)) * (q + F32(1))) * ((q + F32(1)) * (q + F32(1)))
     q = q + (u * (hi - lo) < x - lo)
-    return np.where(x > 0, np.clip(q, 1, 255), 0).astype(np.uint8), s
+    return np.where((v > 0) & (_spread(s, v.size) > 0), np.clip(q, 1, 255), 0).astype(np.uint8), s
 
 
 def moments_step(g, qm, sm, qv, sv, beta1, beta2, clip):

@@ -51,13 +51,14 @@ __device__ __forceinline__ int encode_m(float m, float inv, float u) {
   const int c = (int)fminf(q, up ? 126.0f : 127.0f) + up;
   return m < 0.0f ? -c : c;
 }
-// Code of v: x = v / scale * 255^4 lies between q^4 and (q + 1)^4.
-__device__ __forceinline__ float encode_v(float v, float inv, float u) {
+// Code of v: x = v / scale * 255^4 lies between q^4 and (q + 1)^4. Above zero, also where x is
+// too small for fp32, for a v > least (0; where the block is kept as zeros infinity).
+__device__ __forceinline__ float encode_v(float v, float inv, float least, float u) {
 #pragma clang fp contract(off)
   const float x = v * inv, q = floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(x)));
   const float q1 = q + 1.0f, lo2 = q * q, hi2 = q1 * q1, lo = lo2 * lo2, hi = hi2 * hi2;
   const float c = u * (hi - lo) < x - lo ? q1 : q;
-  return x > 0.0f ? __builtin_amdgcn_fmed3f(c, 1.0f, 255.0f) : 0.0f;
+  return v > least ? __builtin_amdgcn_fmed3f(c, 1.0f, 255.0f) : 0.0f;
 }
 
 // Largest of the wave's 64 unsigned values, in every lane: the rows of 16 by shifted
@@ -233,6 +234,7 @@ __global__ __launch_bounds__(256) void adamw_multi_8_k(AdamBatch bt, AdamHyper h
   const float top_v = __builtin_bit_cast(float, bits_v >> 1);
   const float inv_m = top_m < kTiny ? 0.0f : 16129.0f * (1.0f / top_m);
   const float inv_v = top_v < kTiny ? 0.0f : 4228250625.0f * (1.0f / top_v);
+  const float least_v = top_v < kTiny ? INFINITY : 0.0f;
   qm = qv = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -240,7 +242,7 @@ __global__ __launch_bounds__(256) void adamw_multi_8_k(AdamBatch bt, AdamHyper h
     const float um = __builtin_fmaf((float)(r & 0xFFFF), u_step, u_first);
     const float uv = __builtin_fmaf((float)(r >> 16), u_step, u_first);
     qm |= (uint32_t)(encode_m(m[e], inv_m, um) & 255) << 8 * e;
-    qv = __builtin_amdgcn_cvt_pk_u8_f32(encode_v(v[e], inv_v, uv), e, qv);
+    qv = __builtin_amdgcn_cvt_pk_u8_f32(encode_v(v[e], inv_v, least_v, uv), e, qv);
   }
   store4(static_cast<uint8_t*>(t.m), i, n, bad ? 0u : qm);
   store4(static_cast<uint8_t*>(t.v), i, n, bad ? 0u : qv);

@@ -348,3 +348,29 @@ def test_moments_whose_v_is_lost(beta2):
     bound = lr * (second * (0.71 * 2.0 ** -7 + 255 / 2 / 127.0 ** 2) + 2 * 2.0 ** -7 * 2.0 ** -20)
     # (the new masters, below 2^-6, are rounded to 2^-24 of themselves, twice)
     assert np.max(np.abs(runs[8] - runs[32])) <= bound + 2 * 2.0 ** -30
+
+
+@pytest.mark.parametrize("seed", [None, 77])
+def test_a_small_v_beside_a_huge_one_keeps_a_code(seed):
+    """Shares of the block's largest v below what fp32 holds: the lowest code, not none; the
+    oracle's codes."""
+    import torch
+    banner(f"adamw multi huge v seed={seed}")
+    t = Tensors([700], 8, False, 8)
+    d, h = t.dev[0], t.host[0]
+    for name in ("m", "v", "m_scale", "v_scale"):
+        d[name].zero_()
+        h[name][:] = 0
+    g = np.float32(2.0) ** np.random.default_rng(1).integers(-60, -20, 700).astype(np.float32)
+    g[5::64] = 2.0 ** 61
+    g[9::10] = 0.0
+    h["grad"] = g
+    d["grad"].copy_(torch.from_numpy(g))
+    t.call(None if seed is None else torch.tensor([seed], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    m, v = packed.moments_step(g, h["m"], h["m_scale"], h["v"], h["v_scale"], B1, B2, 0.7)
+    um, uv = packed.moment_draws(700, 0, seed)
+    for name, (q, s) in dict(m=packed.encode_m(m, um), v=packed.encode_v(v, uv)).items():
+        assert np.array_equal(t.got(0, name), q) and np.array_equal(t.got(0, name + "_scale"), s), name
+    assert np.array_equal(t.got(0, "v") > 0, v > 0) and (v > 0).sum() > 500
+    t.check_guards()

@@ -227,3 +227,12 @@ def test_packed_attention_backward_finite_differences(window):
             assert not diff.any() and np.abs(got).max() <= 4 * 20 * 2.0 ** -52
         else:
             assert rel_err(got.ravel(), diff) <= 1e-6
+
+
+def test_a_small_v_beside_a_huge_one_keeps_a_code():
+    """... though its share of it, in 255^-4ths, is below what fp32 holds."""
+    v = np.zeros(256, np.float32)
+    v[0], v[1], v[2] = 2.0 ** 117, 2.0 ** -70, 2.0 ** -149
+    for u in (0.01, 0.5, 0.99):
+        q, s = packed.encode_v(v, np.full(256, np.float32(u)))
+        assert s[0] == v[0] and q[0] == 255 and q[1] == 1 and q[2] == 1 and not q[3:].any()
