@@ -25,6 +25,8 @@ constexpr int kBlock = 256;             // elements that share a scale
 // least, stands in for the roots of such a v.
 constexpr float kTiny = 0x1p-94f;
 
+// A permutation of 32 bits (odd multipliers, chosen by test: over 2^20 drawn x and over x below
+// 2^20 each bit of x, flipped, flips each bit of the result in 0.497 to 0.503 of the cases).
 __host__ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
   x = (x ^ (x >> 16)) * 0xE699D49Du;
   x = (x ^ (x >> 15)) * 0xC570DA33u;

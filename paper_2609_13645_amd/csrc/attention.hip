@@ -202,8 +202,6 @@ struct WindowTiles {
 // per sequence: a block takes a tile from the plan's list, whose sequence's rows start
 // anywhere and end at its length, cut off by the buffers' sizes as a batch row's are, so
 // that tiles of two sequences never share a row and nothing is read past a sequence.
-// Entry i of the list of ROWS rows (KEYS: of the kv pass' order); len 0 where there is none, or where the plan is
-// one of other sizes (or what stands there is no plan).
 __device__ __forceinline__ long first_row_of(const AttnPackedArgs&, const PackedTile& t, int, int) {
   return t.start;
 }
@@ -219,6 +217,8 @@ template <typename Args>
 __device__ __forceinline__ long stat_row(const Args& a, int b, int n, int S, long) {
   return ((long)b * a.n_heads + n) * S;
 }
+// Entry i of the list of ROWS rows (KEYS: of the kv pass' order); len 0 where there is none,
+// or where the plan is one of other sizes (or what stands there is no plan).
 template <int ROWS, bool KEYS = false>
 __device__ __forceinline__ PackedTile packed_tile(const AttnPackedArgs& a, int i) {
   constexpr int KIND = KEYS ? 4 : ROWS == 32 ? 0 : ROWS == 64 ? 1 : ROWS == 128 ? 2 : 3;
@@ -337,6 +337,9 @@ __device__ __forceinline__ float sum_xor32(float v) {
 // NW waves of 32 queries; KG groups of them share the block's key tiles (group g takes
 // tiles g, g + KG, ..) and add up their softmaxes at the end.
 // HW: query heads of one kv head in a block, NW / HW waves each (PACKED; else one).
+// PACKED, heads of 64, one group: held to three waves a SIMD, 168 registers, of which seven
+// spill. 35 documents of 8000 tokens, 32/8 heads, window 300 33.6 us (with two waves and no
+// spills 37.0), 32 of 512 71.0 (78.6), 4 of 4096 330 (344), 512 of 32 42.0 (41.9).
 template <int D, typename Args, int NW, int KG, int HW = 1>
 __global__ __launch_bounds__(64 * NW * KG, KG * D > 128                          ? 1
                                            : kPacked<Args> && D == 64 && KG == 1 ? 3
@@ -1370,7 +1373,8 @@ __global__ __launch_bounds__(64 * NW, D == 64 && KB == 1 ? 2 : 1) void attn_bwd_
   // instruction; nontemporal, since it is read back only after the pass (as
   // ordinary stores, the dirty lines the memory-side cache holds at the end
   // are written back while the next pass reads dS: 7 % on that pass)
-  // (CACHED: ordinary, where all of dS fits that cache)
+  // (CACHED: ordinary; of a window where all of dS fits that cache, PACKED in the half tiles'
+  // blocks of four waves and more, which are taken where there are few, whatever dS comes to)
   auto store_ds = [&]() __attribute__((always_inline)) {
     static_for<2 * KB>([&](auto J) __attribute__((always_inline)) {
       constexpr int j = J;
@@ -2359,7 +2363,14 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   // of 8/2 heads of 128: 611 rows in 4 documents 37.2 us in blocks of 64 keys, so 28.7; 2048
   // rows 151.0, 107.6; 8/8 heads, 2048 rows (256 tiles) 76.3, 71.7, in 4 documents 31.6, 34.2.
   // Heads of 64: 26.8, 22.4 (of eight waves 21.4); 97.8, 77.6 (65.3); 51.8, 48.2 (50.2); 19.8,
-  // 18.9 (24.2). From 512 tiles on 4 to 20 % slower.
+  // 18.9 (24.2). From 512 tiles on 4 to 20 % slower. Their dS leaves by ordinary stores, the
+  // other blocks' nontemporal: by the blocks' form and not, as a window's, by dS's bytes. The
+  // backward by ordinary stores and by nontemporal ones: halves, 8 of 500 tokens, 32/2 heads of 64
+  // (72 MB) 69.9 and 77.6 us, of 128 117 and 123, 24/2, 3000 tokens (212 MB) 192 and 189, 356 and
+  // 367; but 32/1 heads, 4096 (521 MB) 699 and 550, 1217 and 1134, 8192 (2.1 GB) 1839 and 1446, 3053
+  // and 2639. Others, heads of 64: 64 of 256, 32/8 heads (164 MB) 169 and 172, 8 of 1000, 16/4 (136
+  // MB) 91.6 and 103, 16 of 1000, 32/8 (547 MB) 402 and 397; of 128 336 and 327, 156 and 159, 621
+  // and 605.
   const bool halves = blocks <= 128 || (blocks <= 256 && (D == 64 || longest >= 64));
   const bool eight = D == 64 && longest >= (blocks <= 128 ? 40 : 160);
   // With two pairs to a wave at most (heads of 128: one) it forms the statistics itself, one
@@ -2372,6 +2383,12 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   // 168, 125, 126; 4 of 4096 714, 701, 739; 41 documents of 7 to 1605, mean 400, the backward
   // 365, 351, 409. Heads of 128 (two on a CU, their LDS): halves of one wave, 161 us in blocks
   // of four, so 107; 203, 192; 282, 263; 16 of 1024 382, 424; of two waves 144, 200, 308, 458.
+  // Borders by longest / share, the backward of 32/8 heads. Heads of 64, one wave and two: 64 of
+  // 250 (0.82) 166 and 177, 32 of 500 (0.91) 236 and 243, 16 of 1000 (0.97) 386 and 387, 16 of 800
+  // (1.14) 255 and 244; two and four: 16 of 800 244 and 256, 6 of 2000 (1.31) 433 and 439, 16 of
+  // 500 (1.83) 113 and 126, 48 of 100 (2.10) 52 and 56, but 4 of 4000 (1.00) 1114 and 1082. Heads
+  // of 128, halves of one wave and four: 64 of 250 304 and 316, 32 of 500 398 and 412, 16 of 1000
+  // 611 and 579, 6 of 2000 773 and 690, but 16 of 500 191 and 196.
   constexpr integral_constant<int, 4> four{};
   constexpr integral_constant<int, D == 64 ? 8 : 4> most{};
   constexpr integral_constant<int, D == 64 ? 2 : 4> two{};
@@ -2392,6 +2409,11 @@ hipError_t attn_packed_bwd_d(AttnPackedArgs a, const PackedPlan& p, const uint16
   // were few; with heads of 64, 128 the pass of 512 documents of 32 tokens, 32/8 heads, 69 and 97
   // us in blocks of 256 with three, so 38 and 63; 32 of 512 88 and 118, 85 and 111; 16 of 1024
   // 136 and 167, 145 and 167; 4 of 4096 406 and 463, 464 and 505.
+  // Borders: two blocks of 64 a CU and a few partial tiles, three of one sequence, whose later
+  // ones are short. 8/8 heads, the backward in two groups and else: of 64, 2 of 2000 (512 blocks)
+  // 51.3 and 60.5 us, 8 of 500 (560) 31.6 and 31.4, 10 (696) 42.1 and 40.0, one of 6144 (768)
+  // 173 and 189, of 7000 (880) 216 and 241; of 128, 6 of 500 (416) 41.1 and 40.0, 2 of 2000 77.3
+  // and 85.3, 8 of 500 46.2 and 43.9, one of 6144 262 and 280, of 7000 322 and 338.
   const auto dq_pass = [&](auto waves, auto groups, auto stages) {
     constexpr int W = decltype(waves)::value, G = decltype(groups)::value;
     constexpr int ST = decltype(stages)::value;
@@ -2427,6 +2449,13 @@ hipError_t attn_packed_fwd_d(const AttnPackedArgs& a, const PackedPlan& p, uint1
   // documents, 12/4 heads of 64 10.0 us as blocks of 128, so 7.0; 4096 rows, 8/8 heads 62.2, 36.3,
   // 32/8 92.5, 99.9. Heads of 128: 2048 rows, 8/8 heads 40.4, 27.0; 4096 of one 75.8, 55.6, of four
   // 23.9, 29.2; and in blocks of 128 with two groups (one on a CU): 4096 rows, 12/4 81.2, 71.4.
+  // Borders, in two groups and else: heads of 64, 8/8, 6 of 1024 (808 blocks) 20.6 and 25.7, 8
+  // (1080) 27.2 and 27.0, 12 (1624) 36.8 and 35.3, one of 8192 (1024) 101 and 123, of 9216 (1152)
+  // 122 and 140, 8/2, 24 of 250 (840) 13.0 and 11.5, 32 (1124) 15.3 and 12.1. Of 128, one block a CU
+  // and a few partial tiles, two of one sequence: 8/8, 4 of 500 (280) 11.2 and 14.5, 5 (344) 18.3 and
+  // 14.7, one of 4096 (512) 56 and 65, of 4608 (576) 76 and 74. Of 128 rows, one a CU, two of one
+  // sequence: 8/4, 4 of 1000 (264) 22.8 and 23.4, 5 (332) 36.4 and 31.3, 8/8, one of 8192 (512)
+  // 148 and 167, 12/4, of 6144 (576) 139 and 133.
   const long small = PackedBlocks<2>(a, p).busy, large = PackedBlocks<4>(a, p).busy;
   if (p.max_seq > 64 && small <= (D == 64 ? 1024 : packed_one(p) ? 512 : 288)) {
     attn_packed_fwd_n<D, 2, 2>(a, p, o, lse, s);
